@@ -4,13 +4,14 @@ from __future__ import annotations
 import pathlib
 import shutil
 import subprocess
+import tempfile
 
 HERE = pathlib.Path(__file__).resolve().parent
-SRC = HERE / "csrc" / "lorann.hip"
+SRCS = [HERE / "csrc" / "lorann.hip", HERE / "csrc" / "states.hip"]      # the search; the state store and its attention
 LIB = HERE / "liblorann.so"
 
 FLAGS = [
-    "--offload-arch=gfx950", "-O3", "-std=c++17", "-shared", "-fPIC",
+    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     # packed fp32 instructions are kept off: some of their forms have produced wrong results on the test machines
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     # matrix-core results go to ordinary vector registers: the epilogues read every result register once, and
@@ -23,6 +24,27 @@ FLAGS = [
 SAN_LIB = HERE / "liblorann_san.so"
 
 
+def _compile_and_link(hipcc: str, flags: list, out: pathlib.Path, link=(), verbose: bool = False) -> str:
+    """One object per source, compiled side by side, linked into `out`; the compiler's messages."""
+    with tempfile.TemporaryDirectory() as tmp:
+        objs = [str(pathlib.Path(tmp) / (src.stem + ".o")) for src in SRCS]
+        cmds = [[hipcc, *flags, "-c", "-o", obj, str(src)] for src, obj in zip(SRCS, objs)]
+        runs = []
+        for cmd in cmds:
+            if verbose:
+                print(" ".join(cmd))
+            runs.append(subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True))
+        said = "".join(r.communicate()[0] for r in runs)
+        ok = all(r.returncode == 0 for r in runs)
+        if ok:
+            res = subprocess.run([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", *link, "-o", str(out), *objs], capture_output=True, text=True)
+            said, ok = said + res.stderr, res.returncode == 0
+    said = "\n".join(l for l in said.splitlines() if "packed-fp32-ops" not in l)
+    if not ok:
+        raise RuntimeError(f"hipcc failed:\n{said}")
+    return said
+
+
 def build_sanitized() -> pathlib.Path:
     """The same library with AddressSanitizer and UndefinedBehaviorSanitizer in its HOST code (argument checks, index
     loading, workspace planning; device code is compiled as usual).  Load it with LORANN_LIB=<path> and clang's
@@ -30,9 +52,7 @@ def build_sanitized() -> pathlib.Path:
     hipcc = shutil.which("hipcc") or "/opt/rocm/bin/hipcc"
     flags = [f for f in FLAGS if f != "-O3"] + ["-O1", "-g", "-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=undefined",
                                                  "-Xarch_host", "-fno-sanitize-recover=all", "-Xarch_host", "-fno-omit-frame-pointer"]
-    res = subprocess.run([hipcc, *flags, "-o", str(SAN_LIB), str(SRC)], capture_output=True, text=True)
-    if res.returncode != 0:
-        raise RuntimeError("hipcc failed:\n" + "\n".join(l for l in res.stderr.splitlines() if "packed-fp32-ops" not in l))
+    _compile_and_link(hipcc, flags, SAN_LIB, link=[f for f in flags if "sanitize" in f or f == "-Xarch_host"])
     return SAN_LIB
 
 
@@ -44,21 +64,14 @@ def sanitizer_runtime() -> str:
 
 
 def sources():
-    return [SRC] + sorted((HERE / "csrc").glob("*.hpp")) + [HERE.parent / "include" / "lorann.h"]
+    return SRCS + sorted((HERE / "csrc").glob("*.hpp")) + sorted((HERE.parent / "include").glob("*.h"))
 
 
 def build(force: bool = True, verbose: bool = False) -> pathlib.Path:
     hipcc = shutil.which("hipcc") or "/opt/rocm/bin/hipcc"
     if not force and LIB.exists() and all(LIB.stat().st_mtime >= s.stat().st_mtime for s in sources()):
         return LIB
-    cmd = [hipcc, *FLAGS, "-o", str(LIB), str(SRC)]
-    if verbose:
-        print(" ".join(cmd))
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    noise = "packed-fp32-ops"
-    err = "\n".join(l for l in res.stderr.splitlines() if noise not in l)
-    if res.returncode != 0:
-        raise RuntimeError(f"hipcc failed:\n{err}")
+    err = _compile_and_link(hipcc, FLAGS, LIB, verbose=verbose)
     if verbose and err.strip():
         print(err)
     return LIB

@@ -15,6 +15,7 @@
 
 #include "../../include/lorann.h"
 #include "common.hpp"
+#include "error.hpp"
 #include "gemm_f64.hpp"
 #include "rerank.hpp"
 #include "rerank_group.hpp"
@@ -41,7 +42,9 @@ namespace {
 
 thread_local std::string g_err;
 
-int fail(int code, const char* fmt, ...) {
+}  // namespace
+
+int lorann::fail(int code, const char* fmt, ...) {
     char buf[512];
     va_list ap;
     va_start(ap, fmt);
@@ -51,15 +54,7 @@ int fail(int code, const char* fmt, ...) {
     return code;
 }
 
-#define HIP_TRY(expr)                                                                                      \
-    do {                                                                                                   \
-        hipError_t e_ = (expr);                                                                            \
-        if (e_ != hipSuccess)                                                                              \
-            return fail(e_ == hipErrorOutOfMemory ? LORANN_E_NOMEM : LORANN_E_DEVICE, "%s failed: %s", #expr, \
-                        hipGetErrorString(e_));                                                            \
-    } while (0)
-
-bool is_device_ptr(const void* p) {
+bool lorann::is_device_ptr(const void* p) {
     hipPointerAttribute_t at;
     hipError_t e = hipPointerGetAttributes(&at, p);
     if (e != hipSuccess) {
@@ -68,6 +63,8 @@ bool is_device_ptr(const void* p) {
     }
     return at.type == hipMemoryTypeDevice || at.type == hipMemoryTypeManaged;
 }
+
+namespace {
 
 // A fixed region of device memory that buffers are carved from, one after the other (no allocation).
 struct Arena {
