@@ -78,12 +78,12 @@ __device__ __forceinline__ bool find_tile(const AttendArgs& a, int x, RowTile& t
         if (past) {
             const int src = __ffsll((long long)past) - 1;
             t.s = s0 + src;
-            t.first = __shfl(first, src, 64);
-            t.count = __shfl(count, src, 64);
-            t.row0 = (x - base - (__shfl(upto, src, 64) - __shfl(n, src, 64))) * ROWS;
+            t.first = __builtin_amdgcn_readlane(first, src);         // (scalar, so that everything that follows from them is)
+            t.count = __builtin_amdgcn_readlane(count, src);
+            t.row0 = (x - base - (__builtin_amdgcn_readlane(upto, src) - __builtin_amdgcn_readlane(n, src))) * ROWS;
             return true;
         }
-        base += __shfl(upto, 63, 64);
+        base += __builtin_amdgcn_readlane(upto, 63);
     }
     return false;
 }
@@ -114,18 +114,19 @@ template <> struct Bits16<__bf16> {
     static __device__ __forceinline__ uint16_t narrow(float f) { union { uint16_t u; __bf16 h; } x; x.h = (__bf16)f; return x.u; }
 };
 
-// Eight consecutive elements at p, widened.
-template <typename T>
-__device__ __forceinline__ void load8(const void* base, int64_t at, bool wide, float (&f)[8]) {
+// Eight consecutive 16-bit elements, two to a register.
+__device__ __forceinline__ i32x4 load8_raw(const void* base, int64_t at, bool wide) {
     const uint16_t* p = (const uint16_t*)base + at;
-    if (wide) {
-        const i32x4 v = *(const i32x4*)p;
+    if (wide) return *(const i32x4*)p;
+    i32x4 v;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) f[j] = Bits16<T>::widen((uint16_t)((uint32_t)v[j >> 1] >> (16 * (j & 1))));
-    } else {
+    for (int j = 0; j < 4; ++j) v[j] = (int)((uint32_t)p[2 * j] | (uint32_t)p[2 * j + 1] << 16);
+    return v;
+}
+template <typename T>
+__device__ __forceinline__ void widen8(const i32x4 v, float (&f)[8]) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) f[j] = Bits16<T>::widen(p[j]);
-    }
+    for (int j = 0; j < 8; ++j) f[j] = Bits16<T>::widen((uint16_t)((uint32_t)v[j >> 1] >> (16 * (j & 1))));
 }
 
 template <typename T>
@@ -163,7 +164,7 @@ __device__ __forceinline__ KeySteps key_steps(float ks, float vs, float c, float
     KeySteps k;
     k.product = have ? ks * c : 0.0f;
     k.add = have ? lg + bias : -INFINITY;
-    k.inverse = have && vs == vs ? 1.0f / vs : 1.0f;
+    k.inverse = have && vs == vs ? __builtin_amdgcn_rcpf(vs) : 1.0f;       // (1 ulp)
     k.wild = have && fabsf(lg) > kTameLog2;
     return k;
 }
@@ -215,7 +216,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves) k_attend_rows(AttendArgs a)
 #pragma unroll
         for (int i = 0; i < 2 * C; ++i) {
             const int d = 32 * (i >> 1) + 16 * half + 8 * (i & 1);
-            if (live) load8<T>(a.q, (int64_t)(tile.first + tok) * a.q_token + (int64_t)qh * a.q_head + d, a.q_wide, f[i]);
+            if (live) widen8<T>(load8_raw(a.q, (int64_t)(tile.first + tok) * a.q_token + (int64_t)qh * a.q_head + d, a.q_wide), f[i]);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 if (!live) f[i][j] = 0.0f;
@@ -412,30 +413,47 @@ __global__ void __launch_bounds__(64 * kAttendWaves) k_attend_rows(AttendArgs a)
     }
 }
 
-// Joins the splits of each row.
+// Joins the splits of each row: a block per row, D / 4 threads for the row's values and as many splits side by side as the block has room for.
 template <typename T, int D>
 __global__ void __launch_bounds__(256) k_attend_join(AttendArgs a) {
-    constexpr int Q = D / 4;
+    constexpr int Q = D / 4, SIDE = 256 / Q;
+    __shared__ __align__(16) f32x4 lds_o[SIDE][Q];
+    __shared__ float lds_l[SIDE], lds_m[4];
     const int heads = a.st.heads * a.group;
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, all = a.tokens * heads;
-    const int64_t row = i / Q;
-    const int d = (int)(i - row * Q) * 4;
-    if (row >= all) return;
-    const int64_t t = row / heads;
+    const int64_t all = a.tokens * heads, row = blockIdx.x, t = row / heads;
     if (a.q_start && (t < a.q_start[0] || t >= a.q_start[a.sequences])) return;      // no sequence's: nothing was computed
     float m = -INFINITY;
-    for (int s = 0; s < a.splits; ++s) m = fmaxf(m, a.part_m[(int64_t)s * all + row]);
+    for (int s = threadIdx.x; s < a.splits; s += 256) m = fmaxf(m, a.part_m[(int64_t)s * all + row]);
+    m = wave_max_f32(m);
+    if ((threadIdx.x & 63) == 0) lds_m[threadIdx.x >> 6] = m;
+    __syncthreads();
+    m = fmaxf(fmaxf(lds_m[0], lds_m[1]), fmaxf(lds_m[2], lds_m[3]));
     const float m_use = m == -INFINITY ? 0.0f : m;
+    const int side = threadIdx.x / Q, d = threadIdx.x - side * Q;
+    if (side < SIDE) {
+        float l = 0.0f;
+        f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+        for (int s = side; s < a.splits; s += SIDE) {
+            const int64_t at = (int64_t)s * all + row;
+            const float dm = a.part_m[at] - m_use;
+            l += times_exp2(a.part_l[at], dm);
+            o += *(const f32x4*)&a.part_acc[at * D + 4 * d] * __builtin_amdgcn_exp2f(dm);
+        }
+        lds_o[side][d] = o;
+        if (d == 0) lds_l[side] = l;
+    }
+    __syncthreads();
+    if (threadIdx.x >= Q) return;
     float l = 0.0f;
     f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int s = 0; s < a.splits; ++s) {
-        const int64_t at = (int64_t)s * all + row;
-        const float dm = a.part_m[at] - m_use, f = __builtin_amdgcn_exp2f(dm);
-        l += times_exp2(a.part_l[at], dm);
-        o += *(const f32x4*)&a.part_acc[at * D + d] * f;
+#pragma unroll
+    for (int i = 0; i < SIDE; ++i) {
+        l += lds_l[i];
+        o += lds_o[i][d];
     }
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-    store4<T>(a.out, t * a.out_token + (row - t * heads) * a.out_head + d, a.out_wide, o * inv);
+    store4<T>(a.out, t * a.out_token + (row - t * heads) * a.out_head + 4 * d, a.out_wide, o * inv);
 }
 
 }  // namespace lorann

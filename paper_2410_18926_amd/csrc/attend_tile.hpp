@@ -1,0 +1,595 @@
+// Attention of many query rows (a chunk of new tokens, questions over passages): bound by the matrix cores and the exponentials.  Mathematics in attend.hpp.
+#pragma once
+#include "attend.hpp"
+
+namespace lorann {
+
+// A tile of 64 keys: keys k .. k + 63 of a table of `length` keys.  All values are the same in every thread of a block.
+struct KeyTile {
+    const int32_t* pages;
+    int k, length;
+    float bias;
+    bool have;
+};
+
+// The key tiles of one split, in order: units of tables (attend.hpp), 64 keys at a time.
+struct KeyTiles {
+    int r, sub, left, k_end;
+    KeyTile t;
+
+    __device__ __forceinline__ void start(const AttendArgs& a, int split) {
+        const int u = split * a.per_split;
+        left = min(a.found * a.units, u + a.per_split) - u;
+        r = u / a.units;
+        sub = u - r * a.units - 1;
+        k_end = 0;
+        t = KeyTile{nullptr, 0, 0, 0.0f, true};
+    }
+    // Moves on to the next tile (t.have: there is one).  `behind`: tokens of the sequence after the last one that any row of the block sees (causal only).
+    __device__ __forceinline__ void next(const AttendArgs& a, int s, int behind) {
+        if (!t.have) return;
+        t.k += kTileKeys;
+        if (__builtin_expect(t.k < k_end, 1)) return;
+        while (t.k >= k_end) {
+            if (--left < 0) { t.have = false; return; }
+            if (++sub == a.units) { sub = 0; ++r; }
+            int64_t table = s;
+            t.bias = 0.0f;
+            if (a.ids) {
+                table = a.ids[(int64_t)s * a.found + r];
+                t.k = k_end = 0;
+                if ((uint64_t)table >= (uint64_t)a.passages) continue;
+                if (a.scores) t.bias = a.weight * a.scores[(int64_t)s * a.found + r];
+                if (t.bias == -INFINITY) continue;
+            }
+            t.pages = a.tables + table * a.width;
+            t.length = min(max(a.lengths[table], 0), a.width << a.st.shift);
+            t.k = sub * a.unit;
+            k_end = min(a.ids ? t.length : t.length - behind, t.k + a.unit);
+        }
+    }
+};
+
+__device__ __forceinline__ int pick4(const i32x4 v, int i) { return i & 2 ? (i & 1 ? v[3] : v[2]) : (i & 1 ? v[1] : v[0]); }
+
+// f(0) .. f(N - 1) with the number as a constant of its type (array elements picked by it stay in registers).
+template <int I, int N, typename F>
+__device__ __forceinline__ void unrolled(F&& f) {
+    if constexpr (I < N) {
+        f(std::integral_constant<int, I>{});
+        unrolled<I + 1, N>(f);
+    }
+}
+
+// A block has NW * RT * 32 query rows of one head; a wavefront RT * 32 of them.  The block's threads convert each tile of 64 keys and values once to
+// binary16 in LDS, in the order of the matrix operands (next tile's codes are in flight and are converted into the other buffer while this one
+// is used; one barrier per tile).  As in k_attend_rows the scores come out transposed, a lane holds scores of one row, and the weights
+// are the second product's operand as they stand.
+// The reference M of the weights is raised only when a score passes it by more than kSlack (weights stay below 2^kSlack, which binary16 holds with the same relative
+// rounding), so the answer's registers are rarely rescaled.
+constexpr float kSlack = 6.0f;
+
+template <typename T, int D, int NW, int RT, bool WHOLE>
+__global__ void __launch_bounds__(64 * NW, RT == 1 ? 2 : 1) k_attend_tile(AttendArgs a) {
+    constexpr int C = D / 32, ROWS = NW * RT * 32, THREADS = 64 * NW;
+    constexpr int KS = D + 8, VS = kTileKeys + 8;               // row strides in LDS (16 bytes of padding: rows start in other banks)
+    constexpr int PIECES = kTileKeys * D / 16;                  // 16-code pieces of the keys, and of the values
+    constexpr int PER = (PIECES + THREADS - 1) / THREADS;
+    __shared__ __align__(16) _Float16 lds_k[2][kTileKeys * KS];
+    __shared__ __align__(16) _Float16 lds_v[2][D * VS];
+    __shared__ __align__(16) float lds_step[3][3][kTileKeys];
+    __shared__ int lds_flag[NW], lds_wild[3][NW];
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int n = lane & 31, half = lane >> 5;
+    const int head = blockIdx.x % a.st.heads, split = blockIdx.y;
+    RowTile tile;
+    if (!find_tile<ROWS>(a, blockIdx.x / a.st.heads, tile)) return;
+    const int rows = tile.count * a.group;
+    const int P = 1 << a.st.shift;
+
+    // queries
+    int tok[RT], see_after[RT];
+    f16x8 qf[RT][2 * C];
+    float row_up[RT];                                           // of rows whose power of two is not the block's
+    int e_block;
+    bool mixed;
+    {
+        i32x4 raw[RT][2 * C];
+        int e_row[RT];
+        int e_max = -1000, e_min = 1000;
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+            const int row = tile.row0 + (wave * RT + t) * 32 + n;
+            const bool live = row < rows;
+            tok[t] = live ? row / a.group : 0;
+            see_after[t] = tile.count - 1 - tok[t];
+            const int qh = head * a.group + (live ? row - tok[t] * a.group : 0);
+            const int64_t at = (int64_t)(tile.first + tok[t]) * a.q_token + (int64_t)qh * a.q_head;
+            float top = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 2 * C; ++i) {
+                float f[8];
+                raw[t][i] = load8_raw(a.q, at + 16 * i + 8 * half, a.q_wide);
+                if (!live) raw[t][i] = i32x4{0, 0, 0, 0};
+                widen8<T>(raw[t][i], f);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float m = fabsf(f[j]);
+                    if (m <= 3.4028235e38f) top = fmaxf(top, m);
+                }
+            }
+            top = fmaxf(top, __shfl_xor(top, 32, 64));
+            e_row[t] = top < kTinyRow ? -1000 : (int)((__float_as_uint(top) >> 23) & 255) - 127;
+            if (e_row[t] > -1000) { e_max = max(e_max, e_row[t]); e_min = min(e_min, e_row[t]); }
+        }
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) { e_max = max(e_max, __shfl_xor(e_max, o, 64)); e_min = min(e_min, __shfl_xor(e_min, o, 64)); }
+        if (lane == 0) lds_flag[wave] = (e_max + 1000) << 12 | (e_min + 1000);
+        __syncthreads();
+        e_max = -1000; e_min = 1000;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) { e_max = max(e_max, (lds_flag[w] >> 12) - 1000); e_min = min(e_min, (lds_flag[w] & 4095) - 1000); }
+        e_max = __builtin_amdgcn_readfirstlane(e_max);
+        e_min = __builtin_amdgcn_readfirstlane(e_min);
+        e_block = e_max > -1000 ? e_max : 14;
+        mixed = e_max - e_min > 12 && e_max > -1000;
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+            const int e = mixed && e_row[t] > -1000 ? e_row[t] : e_block;
+            const float up = ldexpf(1.0f, 14 - e);
+            row_up[t] = ldexpf(1.0f, e - e_block);
+#pragma unroll
+            for (int i = 0; i < 2 * C; ++i) {
+                float f[8];
+                widen8<T>(raw[t][i], f);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) qf[t][i][j] = (_Float16)(f[j] * up);
+            }
+        }
+    }
+    const float c = ldexpf(a.c, e_block - 14);
+
+    f32x16 acc[RT][C];
+    float M[RT], L[RT];
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+        M[t] = -INFINITY;
+        L[t] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < C; ++i)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) acc[t][i][j] = 0.0f;
+    }
+
+    // Pages of a tile, requested one tile before they are used.  Pages of 64 tokens and more (WHOLE) hold a tile in one piece; smaller ones are looked up
+    // for each 16-key group.  A page number outside the store becomes page 0, its keys get no weight.
+    // (Vector loads, all lanes the same: scalar loads would have to return before the next wait for LDS does.)
+    int lane_zero;
+    asm volatile("v_mov_b32 %0, 0" : "=v"(lane_zero));
+    i32x4 pg = {0, 0, 0, 0};
+    auto find_pages = [&](const KeyTile& kt) {
+        if (!kt.have) return;
+        pg[0] = kt.pages[(kt.k >> a.st.shift) + lane_zero];
+        if constexpr (WHOLE) return;
+#pragma unroll
+        for (int i = 1; i < 4; ++i) pg[i] = kt.pages[(min(kt.k + 16 * i, kt.length - 1) >> a.st.shift) + lane_zero];
+    };
+    // Loading: the thread's pieces of the keys (a key, 16 of its values) and of the values (a component, 16 keys), and one key's steps.
+    // The values are requested one tile after the keys: they are used later.
+    i32x4 ck[PER], cv[PER];
+    float rks = 0.0f, rvs = 0.0f;
+    bool rhave = false;
+    const int skey = tid % kTileKeys;                           // (several threads form the same key's steps: all wavefronts do the same work)
+    const int page_bytes = D << a.st.shift;
+    struct Place { i32x4 row; int off; bool have; };            // page * heads + head of each group; place in the page
+    auto place = [&](const KeyTile& kt) {
+        Place pl;
+        pl.have = kt.have;
+        pl.off = kt.k & (P - 1);                                // (a tile starts at a multiple of 64: within a page, or at a page's start)
+#pragma unroll
+        for (int i = 0; i < (WHOLE ? 1 : 4); ++i) pg[i] = __builtin_amdgcn_readfirstlane(pg[i]);
+#pragma unroll
+        for (int i = 0; i < (WHOLE ? 1 : 4); ++i) pl.row[i] = ((uint32_t)pg[i] < (uint64_t)a.st.pages ? pg[i] : 0) * a.st.heads + head;
+        return pl;
+    };
+    auto fetch_keys = [&](const Place& pl, const KeyTile& kt) {
+        if (!pl.have) return;
+        const int8_t* base = a.st.kc + (uint64_t)(uint32_t)pl.row[0] * (uint32_t)page_bytes + (uint32_t)(pl.off * D);
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int p = tid + i * THREADS;
+            if (PIECES % THREADS && p >= PIECES) break;
+            const int key = p / (D / 16), part = p % (D / 16);
+            if constexpr (WHOLE) ck[i] = *(const i32x4*)(base + (uint32_t)(key * D + 16 * part));
+            else ck[i] = *(const i32x4*)(a.st.kc + (uint64_t)(uint32_t)pick4(pl.row, key >> 4) * (uint32_t)page_bytes + (uint32_t)((key & (P - 1)) * D + 16 * part));
+        }
+        const int p = WHOLE ? pg[0] : pick4(pg, skey >> 4);
+        rhave = kt.k + skey < kt.length && (uint32_t)p < (uint64_t)a.st.pages;
+        const uint64_t at = ((uint64_t)(uint32_t)(WHOLE ? pl.row[0] : pick4(pl.row, skey >> 4)) << a.st.shift) + (uint32_t)(WHOLE ? pl.off + skey : skey & (P - 1));
+        rks = a.st.ks[at];
+        rvs = a.st.vs[at];
+    };
+    auto fetch_values = [&](const Place& pl) {
+        if (!pl.have) return;
+        const int8_t* base = a.st.vc + (uint64_t)(uint32_t)pl.row[0] * (uint32_t)page_bytes + (uint32_t)pl.off;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int p = tid + i * THREADS;
+            if (PIECES % THREADS && p >= PIECES) break;
+            const int comp = p / 4, grp = p % 4;
+            if constexpr (WHOLE) cv[i] = *(const i32x4*)(base + (uint32_t)((comp << a.st.shift) + 16 * grp));
+            else cv[i] = *(const i32x4*)(a.st.vc + (uint64_t)(uint32_t)pick4(pl.row, grp) * (uint32_t)page_bytes + (uint32_t)((comp << a.st.shift) + ((16 * grp) & (P - 1))));
+        }
+    };
+    auto put = [&](_Float16* to, const i32x4 codes) {
+        f16x8 lo, hi;
+        codes_to_half(codes, lo, hi);
+        *(f16x8*)to = lo;
+        *(f16x8*)(to + 8) = hi;
+    };
+    auto stage_keys = [&](int kb, int i) {
+        const int p = tid + i * THREADS;
+        if (PIECES % THREADS && p >= PIECES) return;
+        const int key = p / (D / 16), part = p % (D / 16);
+        // key 32 h + 16 b + 4 g + q is row 32 b + 8 g + 4 h + q of the first product
+        const int krow = (key & 16) * 2 + (key >> 2 & 3) * 8 + (key >> 5) * 4 + (key & 3);
+        put(&lds_k[kb][krow * KS + 16 * part], ck[i]);
+    };
+    auto stage_values = [&](int kb, int i) {
+        const int p = tid + i * THREADS;
+        if (PIECES % THREADS && p >= PIECES) return;
+        put(&lds_v[kb][p / 4 * VS + 16 * (p % 4)], cv[i]);
+    };
+    auto stage_steps = [&](int vb, const KeyTile& kt) {
+        const KeySteps ks = key_steps(rks, rvs, c, kt.bias, rhave);
+        lds_step[vb][0][skey] = ks.product;
+        lds_step[vb][1][skey] = ks.add;
+        lds_step[vb][2][skey] = ks.inverse;
+        lds_wild[vb][wave] = __ballot(ks.wild) != 0;
+    };
+    const int last_row = min(rows, tile.row0 + ROWS) - 1;
+    const int behind = tile.count - 1 - last_row / a.group;
+    const int first_behind = tile.count - 1 - tile.row0 / a.group;
+
+    // first product of a tile
+    auto scores = [&](int kb, f32x16 (&s)[RT][2]) {
+#pragma unroll
+        for (int t = 0; t < RT; ++t)
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) s[t][b][j] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 2 * C; ++i)
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                const f16x8 k = *(const f16x8*)&lds_k[kb][(32 * b + n) * KS + 16 * i + 8 * half];
+#pragma unroll
+                for (int t = 0; t < RT; ++t) s[t][b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, qf[t][i], s[t][b], 0, 0, 0);
+            }
+    };
+    // what a row does not see becomes -inf
+    auto hide = [&](const KeyTile& kt, f32x16 (&s)[RT][2]) -> bool {
+        if (a.ids || kt.k + kTileKeys <= kt.length - first_behind) return false;
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+            const int see = kt.length - see_after[t] - kt.k - 32 * half;
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) s[t][b][j] = 16 * b + j < see ? s[t][b][j] : -INFINITY;
+        }
+        return true;
+    };
+    // y of a tile from its products; what a row does not see is -inf
+    auto logits = [&](int vb, const KeyTile& kt, f32x16 (&s)[RT][2], bool mixed_now) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int at = 32 * half + 16 * b + 4 * g;
+                const f32x4 sk = *(const f32x4*)&lds_step[vb][0][at], lv = *(const f32x4*)&lds_step[vb][1][at];
+#pragma unroll
+                for (int t = 0; t < RT; ++t)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float x = mixed_now ? s[t][b][4 * g + j] * row_up[t] : s[t][b][4 * g + j];
+                        s[t][b][4 * g + j] = fmaf(x, sk[j], lv[j]);
+                    }
+            }
+        hide(kt, s);
+    };
+    auto top_of = [&](const f32x16 (&s)[2]) {
+        float top = s[0][0];
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) top = fmaxf(top, s[b][j]);
+        return top;
+    };
+    // raises M where a row's largest score passes it by more than kSlack
+    auto raise = [&](const float (&tops)[RT]) {
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+            float top = tops[t];
+            if (__ballot(top > M[t] + kSlack)) {
+                top = fmaxf(top, __shfl_xor(top, 32, 64));
+                const float m_new = fmaxf(M[t], top), d = M[t] - (m_new == -INFINITY ? 0.0f : m_new);
+                const float shrink = __builtin_amdgcn_exp2f(d);
+                L[t] = times_exp2(L[t], d);
+                M[t] = m_new;
+#pragma unroll
+                for (int i = 0; i < C; ++i)
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) acc[t][i][j] *= shrink;
+            }
+        }
+    };
+    // the weights of a tile and their sum
+    auto weights = [&](int vb, const f32x16 (&y)[RT][2], f16x8 (&w)[RT][2][2], bool wild_now) {
+        float m_use[RT];
+#pragma unroll
+        for (int t = 0; t < RT; ++t) m_use[t] = M[t] == -INFINITY ? 0.0f : M[t];
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const f32x4 iv = *(const f32x4*)&lds_step[vb][2][32 * half + 16 * b + 4 * g];
+#pragma unroll
+                for (int t = 0; t < RT; ++t)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float e = __builtin_amdgcn_exp2f(y[t][b][4 * g + j] - m_use[t]);
+                        L[t] = wild_now ? L[t] + sum_term(y[t][b][4 * g + j], m_use[t], iv[j]) : fmaf(e, iv[j], L[t]);
+                        w[t][b][g >> 1][4 * (g & 1) + j] = (_Float16)e;
+                    }
+            }
+    };
+    // second product
+    auto gather = [&](int kb, const f16x8 (&w)[RT][2][2]) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int i = 0; i < C; ++i) {
+                    const f16x8 v = *(const f16x8*)&lds_v[kb][(32 * i + n) * VS + 32 * half + 16 * b + 8 * j];
+#pragma unroll
+                    for (int t = 0; t < RT; ++t) acc[t][i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, w[t][b][j], acc[t][i], 0, 0, 0);
+                }
+    };
+
+    // Pipeline, for tile t in turn: the first product of t + 1 runs beside the exponentials of t; the second product of t beside the conversion of the keys
+    // of t + 2 and the values of t + 1 into LDS and the scores of t + 1; then the codes of the tiles after those are requested.
+    KeyTiles it;
+    KeyTile d0, d1, d2;
+    Place pk, pv;
+    it.start(a, split);
+    it.next(a, tile.s, behind);
+    d0 = it.t;
+    find_pages(d0);
+    pk = place(d0);
+    fetch_keys(pk, d0);
+    fetch_values(pk);
+#pragma unroll
+    for (int i = 0; i < PER; ++i) { stage_keys(0, i); stage_values(0, i); }
+    stage_steps(0, d0);
+    it.next(a, tile.s, behind);
+    d1 = it.t;
+    find_pages(d1);
+    pk = place(d1);
+    fetch_keys(pk, d1);
+    fetch_values(pk);
+#pragma unroll
+    for (int i = 0; i < PER; ++i) stage_keys(1, i);
+    stage_steps(1, d1);
+    it.next(a, tile.s, behind);
+    d2 = it.t;
+    find_pages(d2);
+    pk = place(d2);
+    fetch_keys(pk, d2);
+    pv = pk;
+    it.next(a, tile.s, behind);
+    find_pages(it.t);
+    __syncthreads();
+    auto wild_at = [&](int vb) {
+        int any = 0;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) any |= lds_wild[vb][w];
+        return any;
+    };
+    int kb = 0, vb = 0;                  // buffers of tile t: keys and values, steps
+    // requests the keys of t + 3 and the values of t + 2 and moves on
+    auto advance = [&]() {
+        fetch_values(pv);
+        pk = place(it.t);
+        fetch_keys(pk, it.t);
+        pv = pk;
+        d0 = d1;
+        d1 = d2;
+        d2 = it.t;
+        it.next(a, tile.s, behind);
+        find_pages(it.t);
+        kb ^= 1;
+        vb = vb == 2 ? 0 : vb + 1;
+    };
+    if (!mixed && d0.have) {
+        f32x16 y[RT][2];
+        scores(0, y);
+        logits(0, d0, y, false);
+        float top[RT];
+#pragma unroll
+        for (int t = 0; t < RT; ++t) top[t] = top_of(y[t]);
+        raise(top);
+        int wild_now = wild_at(0);
+        __syncthreads();
+        while (d0.have && !__builtin_amdgcn_readfirstlane(wild_now)) {
+            const int v1 = vb == 2 ? 0 : vb + 1, v2 = v1 == 2 ? 0 : v1 + 1;
+            f32x16 s[RT][2];
+            f16x8 w[RT][2][2];
+            {
+                float m_use[RT];
+#pragma unroll
+                for (int t = 0; t < RT; ++t) m_use[t] = M[t] == -INFINITY ? 0.0f : M[t];
+                __builtin_amdgcn_sched_barrier(0);
+                // operands are read from LDS two steps ahead of the products that use them
+                constexpr int STEPS = 4 * C;
+                f16x8 k[3];
+                f32x4 iv[2];
+                auto read_k = [&](auto xc) {
+                    constexpr int x = decltype(xc)::value, b = x / (2 * C), i = x % (2 * C);
+                    if constexpr (x < STEPS) k[x % 3] = *(const f16x8*)&lds_k[kb ^ 1][(32 * b + n) * KS + 16 * i + 8 * half];
+                };
+                auto read_iv = [&](auto xc) {
+                    constexpr int x = decltype(xc)::value;
+                    if constexpr (x < 8) iv[x % 2] = *(const f32x4*)&lds_step[vb][2][32 * half + 16 * (x >> 2) + 4 * (x & 3)];
+                };
+                read_k(std::integral_constant<int, 0>{});
+                read_iv(std::integral_constant<int, 0>{});
+                read_k(std::integral_constant<int, 1>{});
+                unrolled<0, STEPS>([&](auto xc) {
+                    constexpr int x = decltype(xc)::value, b = x / (2 * C), i = x % (2 * C);
+                    read_k(std::integral_constant<int, x + 2>{});
+                    if constexpr (i == 0) {
+#pragma unroll
+                        for (int t = 0; t < RT; ++t)
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) s[t][b][j] = 0.0f;
+                    }
+#pragma unroll
+                    for (int t = 0; t < RT; ++t) s[t][b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k[x % 3], qf[t][i], s[t][b], 0, 0, 0);
+                    unrolled<8 * i / (2 * C), 8 * (i + 1) / (2 * C)>([&](auto pc) {      // pairs of scores
+                        constexpr int pr = decltype(pc)::value, g = 4 * b + pr / 2;
+                        if constexpr (pr % 2 == 0) read_iv(std::integral_constant<int, g + 1>{});
+#pragma unroll
+                        for (int t = 0; t < RT; ++t)
+#pragma unroll
+                            for (int j = 2 * pr; j < 2 * pr + 2; ++j) {
+                                const float e = __builtin_amdgcn_exp2f(y[t][b][j] - m_use[t]);
+                                L[t] = fmaf(e, iv[g % 2][j % 4], L[t]);
+                                w[t][b][j / 8][j % 8] = (_Float16)e;
+                            }
+                    });
+#pragma unroll
+                    for (int t = 0; t < RT; ++t) asm volatile("" : "+v"(L[t]));       // (the sum is formed here, not where it is next used)
+                    __builtin_amdgcn_sched_barrier(0);
+                });
+            }
+            wild_now = wild_at(v1);
+            {
+                // (pieces and steps of a tile that is not there are converted all the same, into a buffer that nothing reads)
+                constexpr int STEPS = 4 * C, AHEAD = 2, FIRST = STEPS / 2;
+#pragma unroll
+                for (int t = 0; t < RT; ++t) top[t] = -INFINITY;
+                f16x8 v[AHEAD + 1];
+                f32x4 sk[2], lv[2];
+                auto read_v = [&](auto xc) {
+                    constexpr int x = decltype(xc)::value;
+                    if constexpr (x < STEPS) v[x % (AHEAD + 1)] = *(const f16x8*)&lds_v[kb][(32 * (x % C) + n) * VS + 32 * half + 8 * (x / C)];
+                };
+                auto read_step = [&](auto bg) {
+                    constexpr int x = decltype(bg)::value;
+                    if constexpr (x < 8) {
+                        sk[x % 2] = *(const f32x4*)&lds_step[v1][0][32 * half + 16 * (x >> 2) + 4 * (x & 3)];
+                        lv[x % 2] = *(const f32x4*)&lds_step[v1][1][32 * half + 16 * (x >> 2) + 4 * (x & 3)];
+                    }
+                };
+                unrolled<0, AHEAD>(read_v);
+                unrolled<0, STEPS>([&](auto xc) {
+                    constexpr int x = decltype(xc)::value, bj = x / C, i = x % C;
+                    read_v(std::integral_constant<int, x + AHEAD>{});
+                    if constexpr (x == 0) stage_steps(v2, d2);
+                    if constexpr (x == FIRST - 1) read_step(std::integral_constant<int, 0>{});
+#pragma unroll
+                    for (int t = 0; t < RT; ++t) acc[t][i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v[x % (AHEAD + 1)], w[t][bj >> 1][bj & 1], acc[t][i], 0, 0, 0);
+                    // beside the products: first the conversions, then the scores of the next tile
+                    if constexpr (x < FIRST) {
+                        unrolled<2 * PER * x / FIRST, 2 * PER * (x + 1) / FIRST>([&](auto uc) {
+                            constexpr int u = decltype(uc)::value;
+                            if constexpr (u & 1) stage_values(kb ^ 1, u >> 1); else stage_keys(kb, u >> 1);
+                        });
+                    } else {
+                        unrolled<8 * (x - FIRST) / (STEPS - FIRST), 8 * (x - FIRST + 1) / (STEPS - FIRST)>([&](auto bg) {
+                            constexpr int z = decltype(bg)::value, b = z >> 2, g = z & 3;
+                            read_step(std::integral_constant<int, z + 1>{});
+#pragma unroll
+                            for (int t = 0; t < RT; ++t)
+#pragma unroll
+                                for (int j = 0; j < 4; ++j) {
+                                    s[t][b][4 * g + j] = fmaf(s[t][b][4 * g + j], sk[z % 2][j], lv[z % 2][j]);
+                                    top[t] = fmaxf(top[t], s[t][b][4 * g + j]);
+                                }
+#pragma unroll
+                            for (int t = 0; t < RT; ++t) asm volatile("" : "+v"(top[t]));
+                        });
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                });
+            }
+            if (hide(d1, s)) {
+#pragma unroll
+                for (int t = 0; t < RT; ++t) top[t] = top_of(s[t]);
+            }
+            advance();
+            if (d0.have) raise(top);
+#pragma unroll
+            for (int t = 0; t < RT; ++t)
+#pragma unroll
+                for (int b = 0; b < 2; ++b) y[t][b] = s[t][b];
+            __syncthreads();
+        }
+    }
+    // Queries of very different sizes in one block, or steps of the values that are not tame (key_steps): the same step by step, for the tiles that are left.
+    bool wild = false;
+    while (d0.have) {
+        const int v1 = vb == 2 ? 0 : vb + 1, v2 = v1 == 2 ? 0 : v1 + 1;
+        wild = wild || __builtin_amdgcn_readfirstlane(wild_at(vb));
+        f32x16 s[RT][2];
+        f16x8 w[RT][2][2];
+        scores(kb, s);
+        logits(vb, d0, s, true);
+        float top[RT];
+#pragma unroll
+        for (int t = 0; t < RT; ++t) top[t] = top_of(s[t]);
+        raise(top);
+        weights(vb, s, w, wild);
+        gather(kb, w);
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < PER; ++i) { stage_keys(kb, i); stage_values(kb ^ 1, i); }
+        stage_steps(v2, d2);
+        advance();
+        __syncthreads();
+    }
+
+    const int heads = a.st.heads * a.group;
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+        const float l = L[t] + __shfl_xor(L[t], 32, 64);
+        const int row = tile.row0 + (wave * RT + t) * 32 + n;
+        if (row >= rows) continue;
+        const int64_t at_tok = tile.first + tok[t];
+        const int qh = head * a.group + row - tok[t] * a.group;
+        if (a.splits == 1) {
+            const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+#pragma unroll
+            for (int i = 0; i < C; ++i)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const f32x4 o = {acc[t][i][4 * g] * inv, acc[t][i][4 * g + 1] * inv, acc[t][i][4 * g + 2] * inv, acc[t][i][4 * g + 3] * inv};
+                    store4<T>(a.out, at_tok * a.out_token + (int64_t)qh * a.out_head + 32 * i + 8 * g + 4 * half, a.out_wide, o);
+                }
+        } else {
+            const int64_t at = ((int64_t)split * a.tokens + at_tok) * heads + qh;
+#pragma unroll
+            for (int i = 0; i < C; ++i)
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+                    *(f32x4*)&a.part_acc[at * D + 32 * i + 8 * g + 4 * half] = f32x4{acc[t][i][4 * g], acc[t][i][4 * g + 1], acc[t][i][4 * g + 2], acc[t][i][4 * g + 3]};
+            if (half == 0) { a.part_m[at] = M[t]; a.part_l[at] = l; }
+        }
+    }
+}
+
+}  // namespace lorann

@@ -6,6 +6,7 @@
 
 #include "../../include/lorann_states.h"
 #include "attend.hpp"
+#include "attend_tile.hpp"
 #include "error.hpp"
 #include "states_store.hpp"
 
@@ -26,7 +27,7 @@ int check_sizes(const lorann_states* st) {
         return fail(LORANN_E_UNSUPPORTED, "page_size %d is outside %d .. %d", st->page_size, LORANN_MIN_PAGE, LORANN_MAX_PAGE);
     if (st->dim % 32 || st->dim > LORANN_MAX_DIM) return fail(LORANN_E_UNSUPPORTED, "dim %d is not a multiple of 32 up to %d", st->dim, LORANN_MAX_DIM);
     if (st->heads > LORANN_MAX_HEADS) return fail(LORANN_E_UNSUPPORTED, "%d heads are more than %d", st->heads, LORANN_MAX_HEADS);
-    if (st->pages > 0x7fffffff) return fail(LORANN_E_UNSUPPORTED, "%lld pages are more than page numbers of 32 bits hold", (long long)st->pages);
+    if (st->pages > 0x7fffffff / st->heads) return fail(LORANN_E_UNSUPPORTED, "%lld pages of %d heads are more than 32 bits count", (long long)st->pages, st->heads);
     return LORANN_OK;
 }
 
@@ -65,13 +66,20 @@ int check_tokens(const lorann_states* st, int32_t type, int64_t tokens) {
 
 // ---- attention ----
 
+constexpr int kTileWaves = 4, kTileRows = kTileWaves * 32;      // block of k_attend_tile
+
 struct Plan {
+    bool tiled;                      // k_attend_tile, else k_attend_rows
     int64_t tiles;                   // row tiles over all sequences, at most
     int32_t unit, units, splits, per_split;
     int64_t workspace;
 };
 
 constexpr int64_t kBlocksWanted = 2048;         // eight blocks a CU: what keeps the memory system busy with ragged lengths
+constexpr int64_t kTileBlocksWanted = 512;
+#ifndef TILED_FROM
+#define TILED_FROM 64
+#endif
 constexpr int64_t kKeysPerBlock = 64 * kAttendWaves;
 
 int check_questions(const lorann_states* st, const lorann_questions* qs, int32_t found, int32_t width) {
@@ -91,10 +99,13 @@ int check_questions(const lorann_states* st, const lorann_questions* qs, int32_t
 Plan plan_of(const lorann_states* st, const lorann_questions* qs, int32_t found, int32_t width) {
     Plan p{};
     const int64_t group = qs->heads / st->heads;
-    p.tiles = qs->q_start ? qs->tokens * group / kRows + qs->sequences : qs->sequences * ceil_div(qs->tokens / std::max<int64_t>(qs->sequences, 1) * group, kRows);
+    const int64_t sequences = std::max<int64_t>(qs->sequences, 1), mean_rows = qs->tokens * group / sequences;
+    p.tiled = mean_rows > TILED_FROM;
+    const int64_t rows_block = p.tiled ? kTileRows : kRows;
+    p.tiles = qs->q_start ? qs->tokens * group / rows_block + sequences : sequences * ceil_div(mean_rows, rows_block);
     const int64_t table_keys = std::max<int64_t>((int64_t)width * st->page_size, 1), tables = std::max(found, 1), keys = tables * table_keys;
     const int64_t blocks = std::max<int64_t>(p.tiles * st->heads, 1);
-    const int64_t want = std::max<int64_t>(1, std::min(kBlocksWanted / blocks, ceil_div(keys, kKeysPerBlock)));
+    const int64_t want = std::max<int64_t>(1, std::min((p.tiled ? kTileBlocksWanted : kBlocksWanted) / blocks, ceil_div(keys, kKeysPerBlock)));
     if (want <= tables) {              // whole tables per split
         p.unit = (int32_t)(ceil_div(table_keys, kTileKeys) * kTileKeys);
         p.units = 1;
@@ -145,10 +156,13 @@ int attend(const lorann_states* st, const lorann_questions* qs, const int64_t* i
     a.q_wide = aligned(qs->q, 16) && qs->q_token % 8 == 0 && qs->q_head % 8 == 0;
     a.out_wide = aligned(qs->out, 8) && qs->out_token % 4 == 0 && qs->out_head % 4 == 0;
     const dim3 grid((unsigned)p.tiles, (unsigned)st->heads, (unsigned)p.splits), block(64 * kAttendWaves);
-    const dim3 join((unsigned)ceil_div(rows * (st->dim / 4), 256));
+    const dim3 tile_grid((unsigned)(p.tiles * st->heads), (unsigned)p.splits);
+    const dim3 join((unsigned)rows);
 #define LAUNCH(T_, D_)                                                                              \
     do {                                                                                            \
-        hipLaunchKernelGGL((k_attend_rows<T_, D_>), grid, block, 0, stream, a);                     \
+        if (p.tiled && a.st.shift >= 6) hipLaunchKernelGGL((k_attend_tile<T_, D_, kTileWaves, 1, true>), tile_grid, dim3(64 * kTileWaves), 0, stream, a); \
+        else if (p.tiled) hipLaunchKernelGGL((k_attend_tile<T_, D_, kTileWaves, 1, false>), tile_grid, dim3(64 * kTileWaves), 0, stream, a); \
+        else hipLaunchKernelGGL((k_attend_rows<T_, D_>), grid, block, 0, stream, a);                \
         if (p.splits > 1) hipLaunchKernelGGL((k_attend_join<T_, D_>), join, dim3(256), 0, stream, a); \
     } while (0)
 #define LAUNCH_DIM(D_) do { if (qs->type == LORANN_F16) LAUNCH(_Float16, D_); else LAUNCH(__bf16, D_); } while (0)
