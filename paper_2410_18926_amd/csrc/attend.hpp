@@ -13,7 +13,7 @@
 namespace lorann {
 
 constexpr int kTileKeys = 64;          // keys a wavefront takes at a time
-constexpr int kRows = 32;              // query rows (token, head of the group) of a block
+constexpr int kRows = 16;              // query rows (token, head of the group) of a block of k_attend_rows
 constexpr int kAttendWaves = 4;
 
 struct AttendArgs {
@@ -186,19 +186,79 @@ __device__ __forceinline__ void wave_lds_order() {
     __builtin_amdgcn_wave_barrier();
 }
 
-// Few query rows: bound by reading the states.  A block has up to 32 rows of one head and a range of keys; its wavefronts take tiles of 64 keys in turn,
+// A tile of 64 keys: keys k .. k + 63 of a table of `length` keys.  All values are the same in every thread of a block.
+struct KeyTile {
+    const int32_t* pages;
+    int k, length;
+    float bias;
+    bool have;
+};
+
+// The key tiles of one split, in order: units of tables (attend.hpp), 64 keys at a time.
+struct KeyTiles {
+    int r, sub, left, k_end;
+    KeyTile t;
+
+    __device__ __forceinline__ void start(const AttendArgs& a, int split) {
+        const int u = split * a.per_split;
+        left = min(a.found * a.units, u + a.per_split) - u;
+        r = u / a.units;
+        sub = u - r * a.units - 1;
+        k_end = 0;
+        t = KeyTile{nullptr, 0, 0, 0.0f, true};
+    }
+    // Moves on by `n` tiles.
+    __device__ __forceinline__ void skip(const AttendArgs& a, int s, int behind, int n) {
+        if (__builtin_expect(t.k + n * kTileKeys < k_end, 1)) { t.k += n * kTileKeys; return; }
+#pragma unroll 1
+        for (int i = 0; i < n; ++i) next(a, s, behind);
+    }
+    // Moves on to the next tile (t.have: there is one).  `behind`: tokens of the sequence after the last one that any row of the block sees (causal only).
+    __device__ __forceinline__ void next(const AttendArgs& a, int s, int behind) {
+        if (!t.have) return;
+        t.k += kTileKeys;
+        if (__builtin_expect(t.k < k_end, 1)) return;
+        while (t.k >= k_end) {
+            if (--left < 0) { t.have = false; return; }
+            if (++sub == a.units) { sub = 0; ++r; }
+            int64_t table = s;
+            t.bias = 0.0f;
+            if (a.ids) {
+                table = a.ids[(int64_t)s * a.found + r];
+                t.k = k_end = 0;
+                if ((uint64_t)table >= (uint64_t)a.passages) continue;
+                if (a.scores) t.bias = a.weight * a.scores[(int64_t)s * a.found + r];
+                if (t.bias == -INFINITY) continue;
+            }
+            t.pages = a.tables + table * a.width;
+            t.length = min(max(a.lengths[table], 0), a.width << a.st.shift);
+            t.k = sub * a.unit;
+            k_end = min(a.ids ? t.length : t.length - behind, t.k + a.unit);
+        }
+    }
+};
+
+// The reference M of the weights is raised only when a score passes it by more than kSlack (weights stay below 2^kSlack, which binary16 holds with the same relative
+// rounding), so the answer's registers are rarely rescaled.
+constexpr float kSlack = 6.0f;
+
+// Few query rows: bound by reading the states.  A block has up to 16 rows of one head and a range of keys; its wavefronts take tiles of 64 keys in turn,
 // codes straight from memory into registers in the order of the matrix operands (no LDS: the order of the contracted axis is free), and
-// their sums are joined in LDS at the end.  The first product is formed transposed (keys x rows), so a lane holds 32 scores of ONE row: statistics are
-// in-lane but for one exchange between the halves of the wavefront, and the weights are the second product's operand as they stand.
-template <typename T, int D>
-__global__ void __launch_bounds__(64 * kAttendWaves) k_attend_rows(AttendArgs a) {
-    constexpr int C = D / 32;                                   // 16-byte pieces of a lane's half of a key row; 32-value tiles of the answer
+// their sums are joined in LDS at the end.  The first product is formed transposed (keys x rows), so a lane holds 16 scores of ONE row: statistics are
+// in-lane but for exchanges between the four quarters of the wavefront, and the weights are the second product's operand as they stand.
+// The next tile's keys are requested as soon as the first product has used this one's, its values after the second product, its page number one tile
+// earlier: a wavefront always has 8 to 16 KiB in flight.  WHOLE: pages of 64 tokens and more, a tile lies in one.
+template <typename T, int D, bool WHOLE>
+__global__ void __launch_bounds__(64 * kAttendWaves, 2) k_attend_rows(AttendArgs a) {
+    constexpr int S32 = D / 32;                                 // steps of the first product, 32 values each
+    constexpr int C = D / 64, ODD = S32 & 1;                    // 16-byte pieces of a lane's key row (two steps each), and one of 8 bytes
+    constexpr int DT = D / 16;                                  // 16-value tiles of the answer
     __shared__ __align__(16) float lds_step[kAttendWaves][3][kTileKeys];
     __shared__ __align__(16) float lds_acc[kAttendWaves][kRows][D + 4];
     __shared__ float lds_m[kAttendWaves][kRows], lds_l[kAttendWaves][kRows];
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int n = lane & 31, half = lane >> 5;
+    const int n = lane & 15, quarter = lane >> 4;
     const int head = blockIdx.y, split = blockIdx.z;
     RowTile tile;
     if (!find_tile<kRows>(a, blockIdx.x, tile)) return;
@@ -206,167 +266,201 @@ __global__ void __launch_bounds__(64 * kAttendWaves) k_attend_rows(AttendArgs a)
     const int row = tile.row0 + n;
     const bool live = row < rows;
     const int tok = live ? row / a.group : 0;
-    const int qh = head * a.group + (live ? row - tok * a.group : 0);
+    const int see_after = tile.count - 1 - tok;                 // tokens of the sequence that the lane's row does not see
+    const int behind = tile.count - 1 - (min(rows, tile.row0 + kRows) - 1) / a.group, first_behind = tile.count - 1 - tile.row0 / a.group;
+    const int P = 1 << a.st.shift;
+
+    // the wavefront's tiles: every fourth of the block's
+    KeyTiles it;
+    it.start(a, split);
+    int page = 0;                                               // lane = key of a tile: its page
+    auto find_page = [&](const KeyTile& kt) {
+        if (kt.have) page = kt.pages[min(kt.k + lane, kt.length - 1) >> a.st.shift];
+    };
+    // Operands: row i of the first product's tile b (of four) is key 16 (i >> 2) + 4 b + (i & 3), so that a quarter's 16 results are 16 consecutive keys -
+    // the 16 consecutive bytes of a component in the transposed values.
+    const int my_key = 16 * (n >> 2) + (n & 3);                 // (+ 4 b)
+    const uint32_t page_bytes = (uint32_t)D << a.st.shift;
+    i32x4 kr[4][C > 0 ? C : 1], vr[DT];
+    uint2 ko[4];
+    float rks = 0.0f, rvs = 0.0f;
+    bool rhave = false;
+    int row_of_key = 0, row_of_tile = 0, place = 0;             // page * heads + head, per lane and (WHOLE) for the tile; place in the page
+    auto fetch_keys = [&](const KeyTile& kt) {
+        if (!kt.have) return;
+        const bool known = (uint32_t)page < (uint64_t)a.st.pages;
+        rhave = known && kt.k + lane < kt.length;
+        row_of_key = (known ? page : 0) * a.st.heads + head;     // (a page number outside the store becomes page 0, its keys get no weight)
+        place = kt.k & (P - 1);
+        if constexpr (WHOLE) row_of_tile = __builtin_amdgcn_readfirstlane(row_of_key);
+        const uint64_t at = ((uint64_t)(uint32_t)(WHOLE ? row_of_tile : row_of_key) << a.st.shift) + (uint32_t)((place + lane) & (P - 1));
+        rks = a.st.ks[at];
+        rvs = a.st.vs[at];
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            const int key = my_key + 4 * b;
+            const int8_t* kp;
+            if constexpr (WHOLE) kp = a.st.kc + (uint64_t)(uint32_t)row_of_tile * page_bytes + (uint32_t)(place * D) + (uint32_t)(key * D);
+            else kp = a.st.kc + (uint64_t)(uint32_t)__shfl(row_of_key, key, 64) * page_bytes + (uint32_t)((key & (P - 1)) * D);
+#pragma unroll
+            for (int i = 0; i < C; ++i) kr[b][i] = *(const i32x4*)(kp + (uint32_t)(64 * i + 16 * quarter));
+            if constexpr (ODD) ko[b] = *(const uint2*)(kp + (uint32_t)(64 * C + 8 * quarter));
+        }
+    };
+    auto fetch_values = [&](bool have, int row_tile, int row_key, int at) {
+        if (!have) return;
+        const int key = 16 * quarter;
+        const int8_t* vp;
+        if constexpr (WHOLE) vp = a.st.vc + (uint64_t)(uint32_t)row_tile * page_bytes + (uint32_t)at + (uint32_t)((n << a.st.shift) + key);
+        else vp = a.st.vc + (uint64_t)(uint32_t)__shfl(row_key, key, 64) * page_bytes + (uint32_t)((n << a.st.shift) + (key & (P - 1)));
+#pragma unroll
+        for (int i = 0; i < DT; ++i) vr[i] = *(const i32x4*)(vp + ((uint32_t)(16 * i) << a.st.shift));
+    };
+    it.skip(a, tile.s, behind, 1 + wave);
+    KeyTile cur = it.t;
+    find_page(cur);
+    fetch_keys(cur);
+    const int first_row_tile = row_of_tile, first_row_key = row_of_key, first_place = place;
+    it.skip(a, tile.s, behind, kAttendWaves);
+    find_page(it.t);
+    fetch_values(cur.have, first_row_tile, first_row_key, first_place);
 
     // queries, normalised to binary16 by a power of two per row
-    f16x8 qf[2 * C];
+    f16x8 qf[S32];
     float q_back;
     {
-        float f[2 * C][8], top = 0.0f;
+        const int qh = head * a.group + (live ? row - tok * a.group : 0);
+        const int64_t at = (int64_t)(tile.first + tok) * a.q_token + (int64_t)qh * a.q_head;
+        i32x4 raw[S32];
+        float top = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 2 * C; ++i) {
-            const int d = 32 * (i >> 1) + 16 * half + 8 * (i & 1);
-            if (live) widen8<T>(load8_raw(a.q, (int64_t)(tile.first + tok) * a.q_token + (int64_t)qh * a.q_head + d, a.q_wide), f[i]);
+        for (int i = 0; i < S32; ++i) raw[i] = load8_raw(a.q, at + (i < 2 * C ? 64 * (i >> 1) + 16 * quarter + 8 * (i & 1) : 64 * C + 8 * quarter), a.q_wide);
+#pragma unroll
+        for (int i = 0; i < S32; ++i) {
+            if (!live) raw[i] = i32x4{0, 0, 0, 0};
+            float f[8];
+            widen8<T>(raw[i], f);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                if (!live) f[i][j] = 0.0f;
-                const float m = fabsf(f[i][j]);
+                const float m = fabsf(f[j]);
                 if (m <= 3.4028235e38f) top = fmaxf(top, m);
             }
         }
         top = fmaxf(top, __shfl_xor(top, 32, 64));
+        top = fmaxf(top, __shfl_xor(top, 16, 64));
         float up;
         row_power(top, up, q_back);
 #pragma unroll
-        for (int i = 0; i < 2 * C; ++i)
+        for (int i = 0; i < S32; ++i) {
+            float f[8];
+            widen8<T>(raw[i], f);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) qf[i][j] = (_Float16)(f[i][j] * up);
+            for (int j = 0; j < 8; ++j) qf[i][j] = (_Float16)(f[j] * up);
+        }
     }
 
-    f32x16 acc[C];
+    f32x4 acc[DT];
 #pragma unroll
-    for (int i = 0; i < C; ++i)
-#pragma unroll
-        for (int j = 0; j < 16; ++j) acc[i][j] = 0.0f;
+    for (int i = 0; i < DT; ++i) acc[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     float M = -INFINITY, L = 0.0f;
-    bool wild = false;                                           // some step so far is not tame
+    bool wild = false;                                          // some step so far is not tame
 
-    const int P = 1 << a.st.shift;
-    const int all_units = a.found * a.units;
-    const int u_begin = split * a.per_split, u_end = min(all_units, u_begin + a.per_split);
-    int turn = 0;
-    for (int u = u_begin; u < u_end; ++u) {
-        const int r = u / a.units, sub = u - r * a.units;
-        int64_t table = tile.s;
-        float bias = 0.0f;
-        int see = 0x7fffffff, last_see = 0x7fffffff;             // keys the lane's row sees, and the tile's last row
-        if (a.ids) {
-            const int64_t id = a.ids[(int64_t)tile.s * a.found + r];
-            if ((uint64_t)id >= (uint64_t)a.passages) continue;
-            table = id;
-            if (a.scores) bias = a.weight * a.scores[(int64_t)tile.s * a.found + r];
-            if (bias == -INFINITY) continue;
+    while (cur.have) {
+        {
+            wave_lds_order();                                   // the previous tile's steps have been read
+            const KeySteps ks = key_steps(rks, rvs, a.c, cur.bias, rhave);
+            lds_step[wave][0][lane] = ks.product;
+            lds_step[wave][1][lane] = ks.add;
+            lds_step[wave][2][lane] = ks.inverse;
+            wild = wild || __ballot(ks.wild);
+            wave_lds_order();
         }
-        const int length = min(max(a.lengths[table], 0), a.width << a.st.shift);
-        if (!a.ids) {
-            see = length - tile.count + tok + 1;
-            const int last = min(rows, tile.row0 + kRows) - 1;
-            last_see = length - tile.count + last / a.group + 1;
+        f32x4 s[4];
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            s[b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int i = 0; i < C; ++i) {
+                f16x8 lo, hi;
+                codes_to_half(kr[b][i], lo, hi);
+                s[b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo, qf[2 * i], s[b], 0, 0, 0);
+                s[b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi, qf[2 * i + 1], s[b], 0, 0, 0);
+            }
+            if constexpr (ODD) {
+                f16x8 lo, hi;
+                codes_to_half(i32x4{(int)ko[b].x, (int)ko[b].y, 0, 0}, lo, hi);
+                s[b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo, qf[2 * C], s[b], 0, 0, 0);
+            }
         }
-        const int k_begin = sub * a.unit, k_end = min(min(length, last_see), k_begin + a.unit);
-        const int32_t* pages = a.tables + table * a.width;
-        for (int k0 = k_begin; k0 < k_end; k0 += kTileKeys) {
-            if ((turn++ & (kAttendWaves - 1)) != wave) continue;
-            wave_lds_order();                                    // the previous tile's steps have been read
-            // lane = key of the tile: its page, its steps
-            const int key = k0 + lane;
-            int32_t page = key < length ? pages[key >> a.st.shift] : -1;
-            const bool have = (uint32_t)page < (uint64_t)a.st.pages;
-            if (!have) page = 0;
-            {
-                const int64_t at = a.st.row(page, head) + (key & (P - 1));
-                const KeySteps ks = key_steps(a.st.ks[at], a.st.vs[at], a.c, bias, have);
-                lds_step[wave][0][lane] = ks.product;
-                lds_step[wave][1][lane] = ks.add;
-                lds_step[wave][2][lane] = ks.inverse;
-                wild = wild || __ballot(ks.wild);
-                wave_lds_order();
-            }
-            // operands: row i of the first product's tile b is key 32 (i >> 2 & 1) + 16 b + 4 (i >> 3) + (i & 3), so that a half's 16 results of a
-            // tile are 16 consecutive keys - the 16 consecutive bytes of a component in the transposed values
-            i32x4 kr[2][C], vr[2][C];
+        __builtin_amdgcn_sched_barrier(0);
+        const KeyTile nxt = it.t;
+        fetch_keys(nxt);
+        it.skip(a, tile.s, behind, kAttendWaves);
+        find_page(it.t);
+        __builtin_amdgcn_sched_barrier(0);
+        float top = -INFINITY;
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                const int kk = 32 * (n >> 2 & 1) + 16 * b + 4 * (n >> 3) + (n & 3), kv = 32 * half + 16 * b;
-                const int64_t pk = __shfl(page, kk, 64), pv = __shfl(page, kv, 64);
-                const int8_t* kp = a.st.kc + (a.st.row(pk, head) + ((k0 + kk) & (P - 1))) * D + 16 * half;
-                const int8_t* vp = a.st.vc + a.st.row(pv, head) * D + ((int64_t)n << a.st.shift) + ((k0 + kv) & (P - 1));
+        for (int b = 0; b < 4; ++b) {
+            const f32x4 sk = *(const f32x4*)&lds_step[wave][0][16 * quarter + 4 * b], lv = *(const f32x4*)&lds_step[wave][1][16 * quarter + 4 * b];
 #pragma unroll
-                for (int i = 0; i < C; ++i) {
-                    kr[b][i] = *(const i32x4*)(kp + 32 * i);
-                    vr[b][i] = *(const i32x4*)(vp + ((int64_t)(32 * i) << a.st.shift));
-                }
-            }
-            f32x16 s[2];
+            for (int j = 0; j < 4; ++j) s[b][j] = fmaf(s[b][j] * q_back, sk[j], lv[j]);
+        }
+        if (!a.ids && cur.k + kTileKeys > cur.length - first_behind) {       // some row may not see all of it
+            const int see = cur.length - see_after - cur.k - 16 * quarter;
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
+            for (int b = 0; b < 4; ++b)
 #pragma unroll
-                for (int j = 0; j < 16; ++j) s[b][j] = 0.0f;
+                for (int j = 0; j < 4; ++j) s[b][j] = 4 * b + j < see ? s[b][j] : -INFINITY;
+        }
 #pragma unroll
-                for (int i = 0; i < C; ++i) {
-                    f16x8 lo, hi;
-                    codes_to_half(kr[b][i], lo, hi);
-                    s[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lo, qf[2 * i], s[b], 0, 0, 0);
-                    s[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(hi, qf[2 * i + 1], s[b], 0, 0, 0);
-                }
-            }
-            float top = -INFINITY;
-            const bool cut = k0 + kTileKeys > length - tile.count;          // some row may not see all of it
+        for (int b = 0; b < 4; ++b)
 #pragma unroll
-            for (int b = 0; b < 2; ++b)
-#pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const f32x4 sk = *(const f32x4*)&lds_step[wave][0][32 * half + 16 * b + 4 * g], lv = *(const f32x4*)&lds_step[wave][1][32 * half + 16 * b + 4 * g];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        float y = fmaf(s[b][4 * g + j] * q_back, sk[j], lv[j]);
-                        if (cut) y = k0 + 32 * half + 16 * b + 4 * g + j < see ? y : -INFINITY;
-                        s[b][4 * g + j] = y;
-                        top = fmaxf(top, y);
-                    }
-                }
+            for (int j = 0; j < 4; ++j) top = fmaxf(top, s[b][j]);
+        if (__ballot(top > M + kSlack)) {
             top = fmaxf(top, __shfl_xor(top, 32, 64));
-            const float m_new = fmaxf(M, top), m_use = m_new == -INFINITY ? 0.0f : m_new;
-            const float shrink = __builtin_amdgcn_exp2f(M - m_use);
-            L = wild ? times_exp2(L, M - m_use) : L * shrink;
+            top = fmaxf(top, __shfl_xor(top, 16, 64));
+            const float m_new = fmaxf(M, top), d = M - (m_new == -INFINITY ? 0.0f : m_new);
+            const float shrink = __builtin_amdgcn_exp2f(d);
+            L = times_exp2(L, d);
             M = m_new;
 #pragma unroll
-            for (int i = 0; i < C; ++i)
+            for (int i = 0; i < DT; ++i) acc[i] = acc[i] * shrink;
+        }
+        const float m_use = M == -INFINITY ? 0.0f : M;
+        if (wild) {
 #pragma unroll
-                for (int j = 0; j < 16; ++j) acc[i][j] *= shrink;
-            if (wild) {
+            for (int b = 0; b < 4; ++b)
 #pragma unroll
-                for (int b = 0; b < 2; ++b)
+                for (int j = 0; j < 4; ++j) L += sum_term(s[b][j], m_use, lds_step[wave][2][16 * quarter + 4 * b + j]);
+        }
+        f16x8 w[2];
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) L += sum_term(s[b][j], m_use, lds_step[wave][2][32 * half + 16 * b + j]);
-            }
+        for (int b = 0; b < 4; ++b) {
+            const f32x4 iv = *(const f32x4*)&lds_step[wave][2][16 * quarter + 4 * b];
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                f16x8 w[2];
-#pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const f32x4 iv = *(const f32x4*)&lds_step[wave][2][32 * half + 16 * b + 4 * g];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const float e = __builtin_amdgcn_exp2f(s[b][4 * g + j] - m_use);
-                        if (!wild) L = fmaf(e, iv[j], L);
-                        w[g >> 1][4 * (g & 1) + j] = (_Float16)e;
-                    }
-                }
-#pragma unroll
-                for (int i = 0; i < C; ++i) {
-                    f16x8 lo, hi;
-                    codes_to_half(vr[b][i], lo, hi);
-                    acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lo, w[0], acc[i], 0, 0, 0);
-                    acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(hi, w[1], acc[i], 0, 0, 0);
-                }
+            for (int j = 0; j < 4; ++j) {
+                const float e = __builtin_amdgcn_exp2f(s[b][j] - m_use);
+                if (!wild) L = fmaf(e, iv[j], L);
+                w[b >> 1][4 * (b & 1) + j] = (_Float16)e;
             }
         }
+        asm volatile("" : "+v"(L));                             // (the sum is formed here: kept for later, its terms would fill the registers)
+#pragma unroll
+        for (int i = 0; i < DT; ++i) {
+            f16x8 lo, hi;
+            codes_to_half(vr[i], lo, hi);
+            acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo, w[0], acc[i], 0, 0, 0);
+            acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi, w[1], acc[i], 0, 0, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        fetch_values(nxt.have, row_of_tile, row_of_key, place);
+        cur = nxt;
     }
     L += __shfl_xor(L, 32, 64);
+    L += __shfl_xor(L, 16, 64);
 
     // join the wavefronts
-    if (half == 0) { lds_m[wave][n] = M; lds_l[wave][n] = L; }
+    if (quarter == 0) { lds_m[wave][n] = M; lds_l[wave][n] = L; }
     __syncthreads();
     float m_all = lds_m[0][n];
 #pragma unroll
@@ -374,14 +468,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves) k_attend_rows(AttendArgs a)
     {
         const float f = __builtin_amdgcn_exp2f(M - (m_all == -INFINITY ? 0.0f : m_all));
 #pragma unroll
-        for (int i = 0; i < C; ++i)
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                f32x4 o;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) o[j] = acc[i][4 * g + j] * f;
-                *(f32x4*)&lds_acc[wave][n][32 * i + 8 * g + 4 * half] = o;
-            }
+        for (int i = 0; i < DT; ++i) *(f32x4*)&lds_acc[wave][n][16 * i + 4 * quarter] = acc[i] * f;
     }
     __syncthreads();
     constexpr int Q = D / 4;
@@ -413,44 +500,58 @@ __global__ void __launch_bounds__(64 * kAttendWaves) k_attend_rows(AttendArgs a)
     }
 }
 
-// Joins the splits of each row: a block per row, D / 4 threads for the row's values and as many splits side by side as the block has room for.
+// Joins the splits of each row.  D / 4 threads hold a row's values; `sides` such groups share a row's splits (a power of two, as many as there are splits
+// while the block has room), each with a running reference of its own, and the block's other groups take other rows.
 template <typename T, int D>
-__global__ void __launch_bounds__(256) k_attend_join(AttendArgs a) {
-    constexpr int Q = D / 4, SIDE = 256 / Q;
-    __shared__ __align__(16) f32x4 lds_o[SIDE][Q];
-    __shared__ float lds_l[SIDE], lds_m[4];
+__global__ void __launch_bounds__(256) k_attend_join(AttendArgs a, int sides) {
+    constexpr int Q = D / 4, GROUPS = 256 / Q;
+    __shared__ __align__(16) f32x4 lds_o[GROUPS][Q];
+    __shared__ float lds_l[GROUPS], lds_m[GROUPS];
     const int heads = a.st.heads * a.group;
-    const int64_t all = a.tokens * heads, row = blockIdx.x, t = row / heads;
-    if (a.q_start && (t < a.q_start[0] || t >= a.q_start[a.sequences])) return;      // no sequence's: nothing was computed
-    float m = -INFINITY;
-    for (int s = threadIdx.x; s < a.splits; s += 256) m = fmaxf(m, a.part_m[(int64_t)s * all + row]);
-    m = wave_max_f32(m);
-    if ((threadIdx.x & 63) == 0) lds_m[threadIdx.x >> 6] = m;
-    __syncthreads();
-    m = fmaxf(fmaxf(lds_m[0], lds_m[1]), fmaxf(lds_m[2], lds_m[3]));
-    const float m_use = m == -INFINITY ? 0.0f : m;
-    const int side = threadIdx.x / Q, d = threadIdx.x - side * Q;
-    if (side < SIDE) {
-        float l = 0.0f;
-        f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 4
-        for (int s = side; s < a.splits; s += SIDE) {
-            const int64_t at = (int64_t)s * all + row;
-            const float dm = a.part_m[at] - m_use;
-            l += times_exp2(a.part_l[at], dm);
-            o += *(const f32x4*)&a.part_acc[at * D + 4 * d] * __builtin_amdgcn_exp2f(dm);
+    const int group = threadIdx.x / Q, d = threadIdx.x - group * Q;
+    const int side = group & (sides - 1), rows = GROUPS / sides;
+    const int64_t all = a.tokens * heads, row = (int64_t)blockIdx.x * rows + group / sides, t = row / heads;
+    bool live = group < rows * sides && row < all;
+    if (live && a.q_start) live = t >= a.q_start[0] && t < a.q_start[a.sequences];      // no sequence's: nothing was computed
+    float m = -INFINITY, l = 0.0f;
+    f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (live) {
+        for (int s0 = side; s0 < a.splits; s0 += 4 * sides) {
+            float ms[4], ls[4];
+            f32x4 os[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {                     // (four at a time are requested together)
+                const int s = s0 + i * sides;
+                const int64_t at = (int64_t)min(s, a.splits - 1) * all + row;
+                ms[i] = a.part_m[at];
+                ls[i] = a.part_l[at];
+                os[i] = *(const f32x4*)&a.part_acc[at * D + 4 * d];
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (s0 + i * sides >= a.splits) break;
+                const float m_new = fmaxf(m, ms[i]), m_use = m_new == -INFINITY ? 0.0f : m_new;
+                l = times_exp2(l, m - m_use) + times_exp2(ls[i], ms[i] - m_use);
+                o = o * __builtin_amdgcn_exp2f(m - m_use) + os[i] * __builtin_amdgcn_exp2f(ms[i] - m_use);
+                m = m_new;
+            }
         }
-        lds_o[side][d] = o;
-        if (d == 0) lds_l[side] = l;
+    }
+    if (group < GROUPS) {
+        lds_o[group][d] = o;
+        if (d == 0) { lds_m[group] = m; lds_l[group] = l; }
     }
     __syncthreads();
-    if (threadIdx.x >= Q) return;
-    float l = 0.0f;
-    f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-    for (int i = 0; i < SIDE; ++i) {
-        l += lds_l[i];
-        o += lds_o[i][d];
+    if (!live || side) return;
+    float m_all = m;
+    for (int i = 1; i < sides; ++i) m_all = fmaxf(m_all, lds_m[group + i]);
+    const float m_use = m_all == -INFINITY ? 0.0f : m_all;
+    l = times_exp2(l, m - m_use);
+    o = o * __builtin_amdgcn_exp2f(m - m_use);
+    for (int i = 1; i < sides; ++i) {
+        const float dm = lds_m[group + i] - m_use;
+        l += times_exp2(lds_l[group + i], dm);
+        o += lds_o[group + i][d] * __builtin_amdgcn_exp2f(dm);
     }
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
     store4<T>(a.out, t * a.out_token + (row - t * heads) * a.out_head + 4 * d, a.out_wide, o * inv);

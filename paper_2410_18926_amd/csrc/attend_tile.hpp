@@ -4,52 +4,6 @@
 
 namespace lorann {
 
-// A tile of 64 keys: keys k .. k + 63 of a table of `length` keys.  All values are the same in every thread of a block.
-struct KeyTile {
-    const int32_t* pages;
-    int k, length;
-    float bias;
-    bool have;
-};
-
-// The key tiles of one split, in order: units of tables (attend.hpp), 64 keys at a time.
-struct KeyTiles {
-    int r, sub, left, k_end;
-    KeyTile t;
-
-    __device__ __forceinline__ void start(const AttendArgs& a, int split) {
-        const int u = split * a.per_split;
-        left = min(a.found * a.units, u + a.per_split) - u;
-        r = u / a.units;
-        sub = u - r * a.units - 1;
-        k_end = 0;
-        t = KeyTile{nullptr, 0, 0, 0.0f, true};
-    }
-    // Moves on to the next tile (t.have: there is one).  `behind`: tokens of the sequence after the last one that any row of the block sees (causal only).
-    __device__ __forceinline__ void next(const AttendArgs& a, int s, int behind) {
-        if (!t.have) return;
-        t.k += kTileKeys;
-        if (__builtin_expect(t.k < k_end, 1)) return;
-        while (t.k >= k_end) {
-            if (--left < 0) { t.have = false; return; }
-            if (++sub == a.units) { sub = 0; ++r; }
-            int64_t table = s;
-            t.bias = 0.0f;
-            if (a.ids) {
-                table = a.ids[(int64_t)s * a.found + r];
-                t.k = k_end = 0;
-                if ((uint64_t)table >= (uint64_t)a.passages) continue;
-                if (a.scores) t.bias = a.weight * a.scores[(int64_t)s * a.found + r];
-                if (t.bias == -INFINITY) continue;
-            }
-            t.pages = a.tables + table * a.width;
-            t.length = min(max(a.lengths[table], 0), a.width << a.st.shift);
-            t.k = sub * a.unit;
-            k_end = min(a.ids ? t.length : t.length - behind, t.k + a.unit);
-        }
-    }
-};
-
 __device__ __forceinline__ int pick4(const i32x4 v, int i) { return i & 2 ? (i & 1 ? v[3] : v[2]) : (i & 1 ? v[1] : v[0]); }
 
 // f(0) .. f(N - 1) with the number as a constant of its type (array elements picked by it stay in registers).
@@ -65,10 +19,6 @@ __device__ __forceinline__ void unrolled(F&& f) {
 // binary16 in LDS, in the order of the matrix operands (next tile's codes are in flight and are converted into the other buffer while this one
 // is used; one barrier per tile).  As in k_attend_rows the scores come out transposed, a lane holds scores of one row, and the weights
 // are the second product's operand as they stand.
-// The reference M of the weights is raised only when a score passes it by more than kSlack (weights stay below 2^kSlack, which binary16 holds with the same relative
-// rounding), so the answer's registers are rarely rescaled.
-constexpr float kSlack = 6.0f;
-
 template <typename T, int D, int NW, int RT, bool WHOLE>
 __global__ void __launch_bounds__(64 * NW, RT == 1 ? 2 : 1) k_attend_tile(AttendArgs a) {
     constexpr int C = D / 32, ROWS = NW * RT * 32, THREADS = 64 * NW;

@@ -75,7 +75,7 @@ struct Plan {
     int64_t workspace;
 };
 
-constexpr int64_t kBlocksWanted = 2048;         // eight blocks a CU: what keeps the memory system busy with ragged lengths
+constexpr int64_t kBlocksWanted = 1024;         // four blocks a CU: what keeps the memory system busy with ragged lengths
 constexpr int64_t kTileBlocksWanted = 512;
 #ifndef TILED_FROM
 #define TILED_FROM 64
@@ -157,13 +157,17 @@ int attend(const lorann_states* st, const lorann_questions* qs, const int64_t* i
     a.out_wide = aligned(qs->out, 8) && qs->out_token % 4 == 0 && qs->out_head % 4 == 0;
     const dim3 grid((unsigned)p.tiles, (unsigned)st->heads, (unsigned)p.splits), block(64 * kAttendWaves);
     const dim3 tile_grid((unsigned)(p.tiles * st->heads), (unsigned)p.splits);
-    const dim3 join((unsigned)rows);
+    const int join_groups = 256 / (st->dim / 4);
+    int sides = 1;
+    while (sides < p.splits && 2 * sides <= join_groups) sides *= 2;
+    const dim3 join((unsigned)ceil_div(rows, join_groups / sides));
 #define LAUNCH(T_, D_)                                                                              \
     do {                                                                                            \
         if (p.tiled && a.st.shift >= 6) hipLaunchKernelGGL((k_attend_tile<T_, D_, kTileWaves, 1, true>), tile_grid, dim3(64 * kTileWaves), 0, stream, a); \
         else if (p.tiled) hipLaunchKernelGGL((k_attend_tile<T_, D_, kTileWaves, 1, false>), tile_grid, dim3(64 * kTileWaves), 0, stream, a); \
-        else hipLaunchKernelGGL((k_attend_rows<T_, D_>), grid, block, 0, stream, a);                \
-        if (p.splits > 1) hipLaunchKernelGGL((k_attend_join<T_, D_>), join, dim3(256), 0, stream, a); \
+        else if (a.st.shift >= 6) hipLaunchKernelGGL((k_attend_rows<T_, D_, true>), grid, block, 0, stream, a); \
+        else hipLaunchKernelGGL((k_attend_rows<T_, D_, false>), grid, block, 0, stream, a);         \
+        if (p.splits > 1) hipLaunchKernelGGL((k_attend_join<T_, D_>), join, dim3(256), 0, stream, a, sides); \
     } while (0)
 #define LAUNCH_DIM(D_) do { if (qs->type == LORANN_F16) LAUNCH(_Float16, D_); else LAUNCH(__bf16, D_); } while (0)
     switch (st->dim) {

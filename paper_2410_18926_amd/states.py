@@ -55,12 +55,19 @@ def _raise(code: int):
 
 
 def _array(t, dtype, shape, what):
-    """A contiguous GPU tensor of this type and shape (None in the shape: any)."""
-    if t.dtype != dtype or t.dim() != len(shape) or any(n is not None and n != m for n, m in zip(shape, t.shape)):
-        raise ValueError(f"{what} must be a {dtype} tensor of shape {tuple('*' if n is None else n for n in shape)}, got {t.dtype} {tuple(t.shape)}")
+    """The address of a contiguous tensor of this type and shape."""
+    if t.dtype is not dtype or t.shape != shape:
+        raise ValueError(f"{what} must be a {dtype} tensor of shape {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
     if not t.is_contiguous():
         raise ValueError(f"{what} must be contiguous (no copy is made)")
     return t.data_ptr()
+
+
+def _strides(x, what):
+    token, head, value = x.stride()
+    if value != 1 and x.shape[2] > 1:
+        raise ValueError(f"{what}: the values of a row must be consecutive")
+    return token, head
 
 
 class States:
@@ -71,10 +78,11 @@ class States:
     The tensors stay the caller's; slot = page * page_size + place in the page."""
 
     def __init__(self, k_codes, v_codes, k_scales, v_scales):
-        self.pages, self.heads, self.page_size, self.dim = k_codes.shape
-        self.device = k_codes.device
         self.k_codes, self.v_codes, self.k_scales, self.v_scales = k_codes, v_codes, k_scales, v_scales
-        n, h, p, d = k_codes.shape
+        self.device = k_codes.device
+        if k_codes.dim() != 4:
+            raise ValueError(f"k_codes must be [pages, heads, page_size, dim], got {tuple(k_codes.shape)}")
+        self.pages, self.heads, self.page_size, self.dim = n, h, p, d = k_codes.shape
         self._st = CStates(_array(k_codes, torch.int8, (n, h, p, d), "k_codes"), _array(v_codes, torch.int8, (n, h, d, p), "v_codes"),
                            _array(k_scales, torch.float32, (n, h, p), "k_scales"), _array(v_scales, torch.float32, (n, h, p), "v_scales"), n, h, p, d)
 
@@ -86,19 +94,13 @@ class States:
                    z(pages, heads, page_size, t=torch.float32), z(pages, heads, page_size, t=torch.float32))
 
     def _rows(self, x, tokens, what):
-        if x.dim() != 3 or x.shape[0] != tokens or x.shape[1] != self.heads or x.shape[2] != self.dim:
+        if x.shape != (tokens, self.heads, self.dim):
             raise ValueError(f"{what} must be [{tokens}, {self.heads}, {self.dim}], got {tuple(x.shape)}")
-        return self._strided(x, what)
-
-    @staticmethod
-    def _strided(x, what):
-        s = x.stride()
-        if s[2] != 1 and x.shape[2] > 1:
-            raise ValueError(f"{what}: the values of a row must be consecutive")
-        return s[0], s[1]
+        return _strides(x, what)
 
     def _stream(self):
-        return torch.cuda.current_stream().cuda_stream if self.device.type == "cuda" else None
+        """torch's current stream (its handle alone: the stream object takes longer than a launch)."""
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()) if self.device.type == "cuda" else None
 
     def write(self, k, v, slots):
         """Quantise keys and values [tokens, heads, dim] (float32, float16 or bfloat16; any distances between tokens and heads) into their slots
@@ -134,11 +136,11 @@ class States:
         if q.dim() != 3 or q.shape[2] != self.dim:
             raise ValueError(f"q must be [tokens, heads, {self.dim}], got {tuple(q.shape)}")
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
         elif out.shape != q.shape or out.dtype != q.dtype:
             raise ValueError(f"out must be {tuple(q.shape)} {q.dtype}, got {tuple(out.shape)} {out.dtype}")
-        qt, qh = self._strided(q, "q")
-        ot, oh = self._strided(out, "out")
+        qt, qh = _strides(q, "q")
+        ot, oh = _strides(out, "out")
         start = None if q_start is None else _array(q_start, torch.int32, (sequences + 1,), "q_start")
         return CQuestions(q.data_ptr(), out.data_ptr(), _TYPE.get(q.dtype, -1), q.shape[1], q.shape[0], sequences, qt, qh, ot, oh, start,
                           self.dim ** -0.5 if scale is None else scale), out
