@@ -57,6 +57,11 @@ Store view(const lorann_states* st) {
 
 int element_size(int32_t type) { return type == LORANN_F32 ? 4 : type == LORANN_F16 || type == LORANN_BF16 ? 2 : 0; }
 
+TokenRows rows_of(void* p, int64_t token, int64_t head, int32_t type) {
+    const int per = 16 / element_size(type);
+    return TokenRows{p, token, head, aligned(p, 16) && token % per == 0 && head % per == 0};
+}
+
 int check_tokens(const lorann_states* st, int32_t type, int64_t tokens) {
     if (!element_size(type)) return fail(LORANN_E_INVAL, "unknown element type %d", type);
     if (tokens < 0) return fail(LORANN_E_INVAL, "%lld tokens", (long long)tokens);
@@ -194,8 +199,8 @@ int lorann_states_write(const lorann_states* st, const void* k, const void* v, i
     if ((rc = check_store(st))) return rc;
     if ((rc = check_device(k, "k")) || (rc = check_device(v, "v")) || (rc = check_device(slots, "slots"))) return rc;
     if (!aligned(k, element_size(type)) || !aligned(v, element_size(type))) return fail(LORANN_E_INVAL, "k or v is not aligned to its type");
-    const dim3 grid((unsigned)ceil_div(tokens * st->heads, 16), 2);
-    const TokenRows kr{const_cast<void*>(k), k_token, k_head}, vr{const_cast<void*>(v), v_token, v_head};
+    const dim3 grid((unsigned)ceil_div(tokens, kBlockTokens), (unsigned)st->heads, 2);
+    const TokenRows kr = rows_of(const_cast<void*>(k), k_token, k_head, type), vr = rows_of(const_cast<void*>(v), v_token, v_head, type);
     hipStream_t s = (hipStream_t)hip_stream;
     if (type == LORANN_F32) hipLaunchKernelGGL((k_states_write<float>), grid, dim3(256), 0, s, view(st), kr, vr, slots, tokens, st->dim);
     else if (type == LORANN_F16) hipLaunchKernelGGL((k_states_write<_Float16>), grid, dim3(256), 0, s, view(st), kr, vr, slots, tokens, st->dim);
@@ -213,8 +218,8 @@ int lorann_states_read(const lorann_states* st, const int64_t* slots, int64_t to
     if ((rc = check_device(slots, "slots"))) return rc;
     if ((k && (rc = check_device(k, "k"))) || (v && (rc = check_device(v, "v")))) return rc;
     if (!aligned(k, element_size(type)) || !aligned(v, element_size(type))) return fail(LORANN_E_INVAL, "k or v is not aligned to its type");
-    const dim3 grid((unsigned)ceil_div(tokens * st->heads, 16), 2);
-    const TokenRows kr{k, k_token, k_head}, vr{v, v_token, v_head};
+    const dim3 grid((unsigned)ceil_div(tokens, kBlockTokens), (unsigned)st->heads, 2);
+    const TokenRows kr = rows_of(k, k_token, k_head, type), vr = rows_of(v, v_token, v_head, type);
     hipStream_t s = (hipStream_t)hip_stream;
     if (type == LORANN_F32) hipLaunchKernelGGL((k_states_read<float>), grid, dim3(256), 0, s, view(st), slots, tokens, kr, vr, st->dim);
     else if (type == LORANN_F16) hipLaunchKernelGGL((k_states_read<_Float16>), grid, dim3(256), 0, s, view(st), slots, tokens, kr, vr, st->dim);
