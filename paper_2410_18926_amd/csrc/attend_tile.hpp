@@ -28,7 +28,7 @@ __global__ void __launch_bounds__(64 * NW, RT == 1 ? 2 : 1) k_attend_tile(Attend
     __shared__ __align__(16) _Float16 lds_k[2][kTileKeys * KS];
     __shared__ __align__(16) _Float16 lds_v[2][D * VS];
     __shared__ __align__(16) float lds_step[3][3][kTileKeys];
-    __shared__ int lds_flag[NW], lds_wild[3][NW];
+    __shared__ int lds_flag[NW], lds_wild[3];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = lane & 31, half = lane >> 5;
@@ -112,64 +112,79 @@ __global__ void __launch_bounds__(64 * NW, RT == 1 ? 2 : 1) k_attend_tile(Attend
             for (int j = 0; j < 16; ++j) acc[t][i][j] = 0.0f;
     }
 
-    // Pages of a tile, requested one tile before they are used.  Pages of 64 tokens and more (WHOLE) hold a tile in one piece; smaller ones are looked up
-    // for each 16-key group.  A page number outside the store becomes page 0, its keys get no weight.
-    // (Vector loads, all lanes the same: scalar loads would have to return before the next wait for LDS does.)
+    // Loading: the thread's pieces of the keys (a key, 16 of its values) and of the values (a component, 16 keys), and in one of three wavefronts in turn
+    // the steps of a key per lane.  Page numbers are requested one tile before they are used: pages of 64 tokens and more (WHOLE) hold a tile in one
+    // piece, smaller ones are looked up for each piece.  A page number outside the store becomes page 0, its keys get no weight.
+    // (Vector loads, all lanes the same where the page is: scalar loads would have to return before the next wait for LDS does.)
     int lane_zero;
     asm volatile("v_mov_b32 %0, 0" : "=v"(lane_zero));
-    i32x4 pg = {0, 0, 0, 0};
+    int pg[WHOLE ? 1 : PER], pg_step = 0;                       // WHOLE: the tile's page; else the pages of the thread's keys and of the lane's key
+    int pv[WHOLE ? 1 : PER];                                    // ... and of the thread's values, of the tile before (WHOLE: as page * heads + head)
+    auto page_at = [&](const KeyTile& kt, int key) { return kt.pages[min(kt.k + key, kt.length - 1) >> a.st.shift]; };
     auto find_pages = [&](const KeyTile& kt) {
         if (!kt.have) return;
-        pg[0] = kt.pages[(kt.k >> a.st.shift) + lane_zero];
-        if constexpr (WHOLE) return;
+        if constexpr (WHOLE) pg[0] = kt.pages[(kt.k >> a.st.shift) + lane_zero];
+        else {
 #pragma unroll
-        for (int i = 1; i < 4; ++i) pg[i] = kt.pages[(min(kt.k + 16 * i, kt.length - 1) >> a.st.shift) + lane_zero];
+            for (int i = 0; i < PER; ++i) pg[i] = page_at(kt, (tid + i * THREADS) / (D / 16) % kTileKeys);
+            pg_step = page_at(kt, lane);
+        }
     };
-    // Loading: the thread's pieces of the keys (a key, 16 of its values) and of the values (a component, 16 keys), and one key's steps.
-    // The values are requested one tile after the keys: they are used later.
+    auto row_of = [&](int page) { return ((uint32_t)page < (uint64_t)a.st.pages ? page : 0) * a.st.heads + head; };
     i32x4 ck[PER], cv[PER];
     float rks = 0.0f, rvs = 0.0f;
     bool rhave = false;
-    const int skey = tid % kTileKeys;                           // (several threads form the same key's steps: all wavefronts do the same work)
-    const int page_bytes = D << a.st.shift;
-    struct Place { i32x4 row; int off; bool have; };            // page * heads + head of each group; place in the page
-    auto place = [&](const KeyTile& kt) {
-        Place pl;
-        pl.have = kt.have;
-        pl.off = kt.k & (P - 1);                                // (a tile starts at a multiple of 64: within a page, or at a page's start)
+    const uint32_t page_bytes = (uint32_t)D << a.st.shift;
+    int off_v = 0;                                              // place in the page of the tile whose values are requested next
+    bool have_v = false;
+    // requests the keys of a tile, its steps in wavefront `by`, and notes where its values are
+    auto fetch_keys = [&](const KeyTile& kt, int by) {
+        have_v = kt.have;
+        if (!kt.have) return;
+        const int off = kt.k & (P - 1);                         // (a tile starts at a multiple of 64: within a page, or at a page's start)
+        off_v = off;
+        if constexpr (WHOLE) {
+            const int page = __builtin_amdgcn_readfirstlane(pg[0]);
+            pv[0] = row_of(page);
+            const int8_t* base = a.st.kc + (uint64_t)(uint32_t)pv[0] * page_bytes + (uint32_t)(off * D);
 #pragma unroll
-        for (int i = 0; i < (WHOLE ? 1 : 4); ++i) pg[i] = __builtin_amdgcn_readfirstlane(pg[i]);
+            for (int i = 0; i < PER; ++i) {
+                const int p = tid + i * THREADS;
+                if (PIECES % THREADS && p >= PIECES) break;
+                ck[i] = *(const i32x4*)(base + (uint32_t)(16 * p));
+            }
+            if (wave == by) {
+                rhave = kt.k + lane < kt.length && (uint32_t)page < (uint64_t)a.st.pages;
+                const uint64_t at = ((uint64_t)(uint32_t)pv[0] << a.st.shift) + (uint32_t)off;
+                rks = (a.st.ks + at)[lane];
+                rvs = (a.st.vs + at)[lane];
+            }
+        } else {
 #pragma unroll
-        for (int i = 0; i < (WHOLE ? 1 : 4); ++i) pl.row[i] = ((uint32_t)pg[i] < (uint64_t)a.st.pages ? pg[i] : 0) * a.st.heads + head;
-        return pl;
-    };
-    auto fetch_keys = [&](const Place& pl, const KeyTile& kt) {
-        if (!pl.have) return;
-        const int8_t* base = a.st.kc + (uint64_t)(uint32_t)pl.row[0] * (uint32_t)page_bytes + (uint32_t)(pl.off * D);
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const int p = tid + i * THREADS;
-            if (PIECES % THREADS && p >= PIECES) break;
-            const int key = p / (D / 16), part = p % (D / 16);
-            if constexpr (WHOLE) ck[i] = *(const i32x4*)(base + (uint32_t)(key * D + 16 * part));
-            else ck[i] = *(const i32x4*)(a.st.kc + (uint64_t)(uint32_t)pick4(pl.row, key >> 4) * (uint32_t)page_bytes + (uint32_t)((key & (P - 1)) * D + 16 * part));
+            for (int i = 0; i < PER; ++i) {
+                const int p = tid + i * THREADS;
+                if (PIECES % THREADS && p >= PIECES) break;
+                const int key = p / (D / 16), part = p % (D / 16);
+                ck[i] = *(const i32x4*)(a.st.kc + (uint64_t)(uint32_t)row_of(pg[i]) * page_bytes + (uint32_t)((key & (P - 1)) * D + 16 * part));
+                pv[i] = page_at(kt, 16 * (p % 4));
+            }
+            if (wave == by) {
+                rhave = kt.k + lane < kt.length && (uint32_t)pg_step < (uint64_t)a.st.pages;
+                const uint64_t at = ((uint64_t)(uint32_t)row_of(pg_step) << a.st.shift) + (uint32_t)(lane & (P - 1));
+                rks = a.st.ks[at];
+                rvs = a.st.vs[at];
+            }
         }
-        const int p = WHOLE ? pg[0] : pick4(pg, skey >> 4);
-        rhave = kt.k + skey < kt.length && (uint32_t)p < (uint64_t)a.st.pages;
-        const uint64_t at = ((uint64_t)(uint32_t)(WHOLE ? pl.row[0] : pick4(pl.row, skey >> 4)) << a.st.shift) + (uint32_t)(WHOLE ? pl.off + skey : skey & (P - 1));
-        rks = a.st.ks[at];
-        rvs = a.st.vs[at];
     };
-    auto fetch_values = [&](const Place& pl) {
-        if (!pl.have) return;
-        const int8_t* base = a.st.vc + (uint64_t)(uint32_t)pl.row[0] * (uint32_t)page_bytes + (uint32_t)pl.off;
+    auto fetch_values = [&]() {
+        if (!have_v) return;
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const int p = tid + i * THREADS;
             if (PIECES % THREADS && p >= PIECES) break;
             const int comp = p / 4, grp = p % 4;
-            if constexpr (WHOLE) cv[i] = *(const i32x4*)(base + (uint32_t)((comp << a.st.shift) + 16 * grp));
-            else cv[i] = *(const i32x4*)(a.st.vc + (uint64_t)(uint32_t)pick4(pl.row, grp) * (uint32_t)page_bytes + (uint32_t)((comp << a.st.shift) + ((16 * grp) & (P - 1))));
+            if constexpr (WHOLE) cv[i] = *(const i32x4*)(a.st.vc + (uint64_t)(uint32_t)pv[0] * page_bytes + (uint32_t)off_v + (uint32_t)((comp << a.st.shift) + 16 * grp));
+            else cv[i] = *(const i32x4*)(a.st.vc + (uint64_t)(uint32_t)row_of(pv[i]) * page_bytes + (uint32_t)((comp << a.st.shift) + ((16 * grp) & (P - 1))));
         }
     };
     auto put = [&](_Float16* to, const i32x4 codes) {
@@ -191,13 +206,16 @@ __global__ void __launch_bounds__(64 * NW, RT == 1 ? 2 : 1) k_attend_tile(Attend
         if (PIECES % THREADS && p >= PIECES) return;
         put(&lds_v[kb][p / 4 * VS + 16 * (p % 4)], cv[i]);
     };
-    auto stage_steps = [&](int vb, const KeyTile& kt) {
+    auto stage_steps = [&](int vb, const KeyTile& kt) {         // (by the wavefront that requested them: tiles go round)
+        if (wave != vb) return;
         const KeySteps ks = key_steps(rks, rvs, c, kt.bias, rhave);
-        lds_step[vb][0][skey] = ks.product;
-        lds_step[vb][1][skey] = ks.add;
-        lds_step[vb][2][skey] = ks.inverse;
-        lds_wild[vb][wave] = __ballot(ks.wild) != 0;
+        lds_step[vb][0][lane] = ks.product;
+        lds_step[vb][1][lane] = ks.add;
+        lds_step[vb][2][lane] = ks.inverse;
+        const int w = __ballot(ks.wild) != 0;
+        if (lane == 0) lds_wild[vb] = w;
     };
+
     const int last_row = min(rows, tile.row0 + ROWS) - 1;
     const int behind = tile.count - 1 - last_row / a.group;
     const int first_behind = tile.count - 1 - tile.row0 / a.group;
@@ -312,50 +330,38 @@ __global__ void __launch_bounds__(64 * NW, RT == 1 ? 2 : 1) k_attend_tile(Attend
 
     // Pipeline, for tile t in turn: the first product of t + 1 runs beside the exponentials of t; the second product of t beside the conversion of the keys
     // of t + 2 and the values of t + 1 into LDS and the scores of t + 1; then the codes of the tiles after those are requested.
+    static_assert(NW >= 3, "three wavefronts form the steps in turn");
     KeyTiles it;
     KeyTile d0, d1, d2;
-    Place pk, pv;
     it.start(a, split);
     it.next(a, tile.s, behind);
     d0 = it.t;
     find_pages(d0);
-    pk = place(d0);
-    fetch_keys(pk, d0);
-    fetch_values(pk);
+    fetch_keys(d0, 0);
+    fetch_values();
 #pragma unroll
     for (int i = 0; i < PER; ++i) { stage_keys(0, i); stage_values(0, i); }
     stage_steps(0, d0);
     it.next(a, tile.s, behind);
     d1 = it.t;
     find_pages(d1);
-    pk = place(d1);
-    fetch_keys(pk, d1);
-    fetch_values(pk);
+    fetch_keys(d1, 1);
+    fetch_values();
 #pragma unroll
     for (int i = 0; i < PER; ++i) stage_keys(1, i);
     stage_steps(1, d1);
     it.next(a, tile.s, behind);
     d2 = it.t;
     find_pages(d2);
-    pk = place(d2);
-    fetch_keys(pk, d2);
-    pv = pk;
+    fetch_keys(d2, 2);
     it.next(a, tile.s, behind);
     find_pages(it.t);
     __syncthreads();
-    auto wild_at = [&](int vb) {
-        int any = 0;
-#pragma unroll
-        for (int w = 0; w < NW; ++w) any |= lds_wild[vb][w];
-        return any;
-    };
     int kb = 0, vb = 0;                  // buffers of tile t: keys and values, steps
     // requests the keys of t + 3 and the values of t + 2 and moves on
     auto advance = [&]() {
-        fetch_values(pv);
-        pk = place(it.t);
-        fetch_keys(pk, it.t);
-        pv = pk;
+        fetch_values();
+        fetch_keys(it.t, vb);
         d0 = d1;
         d1 = d2;
         d2 = it.t;
@@ -372,7 +378,7 @@ __global__ void __launch_bounds__(64 * NW, RT == 1 ? 2 : 1) k_attend_tile(Attend
 #pragma unroll
         for (int t = 0; t < RT; ++t) top[t] = top_of(y[t]);
         raise(top);
-        int wild_now = wild_at(0);
+        int wild_now = lds_wild[0];
         __syncthreads();
         while (d0.have && !__builtin_amdgcn_readfirstlane(wild_now)) {
             const int v1 = vb == 2 ? 0 : vb + 1, v2 = v1 == 2 ? 0 : v1 + 1;
@@ -426,7 +432,7 @@ __global__ void __launch_bounds__(64 * NW, RT == 1 ? 2 : 1) k_attend_tile(Attend
                     __builtin_amdgcn_sched_barrier(0);
                 });
             }
-            wild_now = wild_at(v1);
+            wild_now = lds_wild[v1];
             {
                 // (pieces and steps of a tile that is not there are converted all the same, into a buffer that nothing reads)
                 constexpr int STEPS = 4 * C, AHEAD = 2, FIRST = STEPS / 2;
@@ -449,7 +455,6 @@ __global__ void __launch_bounds__(64 * NW, RT == 1 ? 2 : 1) k_attend_tile(Attend
                 unrolled<0, STEPS>([&](auto xc) {
                     constexpr int x = decltype(xc)::value, bj = x / C, i = x % C;
                     read_v(std::integral_constant<int, x + AHEAD>{});
-                    if constexpr (x == 0) stage_steps(v2, d2);
                     if constexpr (x == FIRST - 1) read_step(std::integral_constant<int, 0>{});
 #pragma unroll
                     for (int t = 0; t < RT; ++t) acc[t][i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v[x % (AHEAD + 1)], w[t][bj >> 1][bj & 1], acc[t][i], 0, 0, 0);
@@ -477,6 +482,7 @@ __global__ void __launch_bounds__(64 * NW, RT == 1 ? 2 : 1) k_attend_tile(Attend
                     __builtin_amdgcn_sched_barrier(0);
                 });
             }
+            stage_steps(v2, d2);
             if (hide(d1, s)) {
 #pragma unroll
                 for (int t = 0; t < RT; ++t) top[t] = top_of(s[t]);
@@ -494,7 +500,7 @@ __global__ void __launch_bounds__(64 * NW, RT == 1 ? 2 : 1) k_attend_tile(Attend
     bool wild = false;
     while (d0.have) {
         const int v1 = vb == 2 ? 0 : vb + 1, v2 = v1 == 2 ? 0 : v1 + 1;
-        wild = wild || __builtin_amdgcn_readfirstlane(wild_at(vb));
+        wild = wild || __builtin_amdgcn_readfirstlane(lds_wild[vb]);
         f32x16 s[RT][2];
         f16x8 w[RT][2][2];
         scores(kb, s);

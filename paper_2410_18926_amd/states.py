@@ -28,6 +28,7 @@ class CQuestions(C.Structure):
                 ("q_token", C.c_int64), ("q_head", C.c_int64), ("out_token", C.c_int64), ("out_head", C.c_int64), ("q_start", C.c_void_p), ("scale", C.c_float)]
 
 
+_raw_stream, _current_device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
 _lib = None
 
 
@@ -79,12 +80,17 @@ class States:
 
     def __init__(self, k_codes, v_codes, k_scales, v_scales):
         self.k_codes, self.v_codes, self.k_scales, self.v_scales = k_codes, v_codes, k_scales, v_scales
-        self.device = k_codes.device
         if k_codes.dim() != 4:
             raise ValueError(f"k_codes must be [pages, heads, page_size, dim], got {tuple(k_codes.shape)}")
         self.pages, self.heads, self.page_size, self.dim = n, h, p, d = k_codes.shape
-        self._st = CStates(_array(k_codes, torch.int8, (n, h, p, d), "k_codes"), _array(v_codes, torch.int8, (n, h, d, p), "v_codes"),
-                           _array(k_scales, torch.float32, (n, h, p), "k_scales"), _array(v_scales, torch.float32, (n, h, p), "v_scales"), n, h, p, d)
+        self._on_gpu = k_codes.is_cuda
+        steps = (n, h, p)
+        self._st = CStates(_array(k_codes, torch.int8, k_codes.shape, "k_codes"), _array(v_codes, torch.int8, (n, h, d, p), "v_codes"),
+                           _array(k_scales, torch.float32, steps, "k_scales"), _array(v_scales, torch.float32, steps, "v_scales"), n, h, p, d)
+
+    @property
+    def device(self):
+        return self.k_codes.device
 
     @classmethod
     def empty(cls, pages: int, heads: int, page_size: int, dim: int, device="cuda") -> "States":
@@ -100,7 +106,7 @@ class States:
 
     def _stream(self):
         """torch's current stream (its handle alone: the stream object takes longer than a launch)."""
-        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()) if self.device.type == "cuda" else None
+        return _raw_stream(_current_device()) if self._on_gpu else None
 
     def write(self, k, v, slots):
         """Quantise keys and values [tokens, heads, dim] (float32, float16 or bfloat16; any distances between tokens and heads) into their slots
@@ -119,8 +125,8 @@ class States:
         to (any distances between tokens and heads)."""
         n = slots.shape[0]
         if out is None:
-            k = torch.empty((n, self.heads, self.dim), dtype=dtype, device=self.device)
-            v = torch.empty((n, self.heads, self.dim), dtype=dtype, device=self.device)
+            k = torch.empty((n, self.heads, self.dim), dtype=dtype, device=self.k_codes.device)
+            v = torch.empty_like(k)
         else:
             k, v = out
         kt, kh = self._rows(k, n, "out[0]")
@@ -133,27 +139,28 @@ class States:
         return k, v
 
     def _questions(self, q, q_start, sequences, scale, out):
-        if q.dim() != 3 or q.shape[2] != self.dim:
+        tokens, heads, dim = q.shape
+        if dim != self.dim:
             raise ValueError(f"q must be [tokens, heads, {self.dim}], got {tuple(q.shape)}")
         if out is None:
             out = torch.empty_like(q, memory_format=torch.contiguous_format)
-        elif out.shape != q.shape or out.dtype != q.dtype:
+        elif out.shape != q.shape or out.dtype is not q.dtype:
             raise ValueError(f"out must be {tuple(q.shape)} {q.dtype}, got {tuple(out.shape)} {out.dtype}")
         qt, qh = _strides(q, "q")
         ot, oh = _strides(out, "out")
-        start = None if q_start is None else _array(q_start, torch.int32, (sequences + 1,), "q_start")
-        return CQuestions(q.data_ptr(), out.data_ptr(), _TYPE.get(q.dtype, -1), q.shape[1], q.shape[0], sequences, qt, qh, ot, oh, start,
-                          self.dim ** -0.5 if scale is None else scale), out
+        return CQuestions(q.data_ptr(), out.data_ptr(), _TYPE.get(q.dtype, -1), heads, tokens, sequences, qt, qh, ot, oh,
+                          None if q_start is None else _array(q_start, torch.int32, (sequences + 1,), "q_start"), dim ** -0.5 if scale is None else scale), out
 
     def _workspace(self, qs, found, width, workspace):
+        if workspace is not None:
+            return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
         need = lib().lorann_attend_workspace(self._st, qs, found, width)
         if need < 0:
             _raise(need)
-        if workspace is None:
-            if not need:
-                return None, 0, None
-            workspace = torch.empty(need, dtype=torch.uint8, device=self.device)
-        return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
+        if not need:
+            return None, 0, None
+        workspace = torch.empty(need, dtype=torch.uint8, device=self.k_codes.device)
+        return workspace.data_ptr(), need, workspace
 
     def workspace_bytes(self, q, sequences: int, width: int, found: int = 0, ragged: bool = False) -> int:
         """Bytes of `workspace` that a call with these queries and sizes needs (found = 0: attend_chunk; ragged: with q_start)."""
