@@ -180,6 +180,12 @@ __device__ __forceinline__ float times_exp2(float x, float d) {
     return x * h * h;
 }
 
+// A 32-bit offset that is widened where it is used (scalar base + vector offset in one instruction) instead of being kept as 64 bits.
+__device__ __forceinline__ uint32_t here(uint32_t x) {
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
 // LDS is served in a wavefront's order; this keeps the compiler from moving accesses that other lanes depend on.
 __device__ __forceinline__ void wave_lds_order() {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -296,25 +302,38 @@ __global__ void __launch_bounds__(64 * kAttendWaves, 2) k_attend_rows(AttendArgs
         const uint64_t at = ((uint64_t)(uint32_t)(WHOLE ? row_of_tile : row_of_key) << a.st.shift) + (uint32_t)((place + lane) & (P - 1));
         rks = a.st.ks[at];
         rvs = a.st.vs[at];
+        if constexpr (WHOLE) {
+            const int8_t* base = a.st.kc + (uint64_t)(uint32_t)row_of_tile * page_bytes + (uint32_t)(place * D);
 #pragma unroll
-        for (int b = 0; b < 4; ++b) {
-            const int key = my_key + 4 * b;
-            const int8_t* kp;
-            if constexpr (WHOLE) kp = a.st.kc + (uint64_t)(uint32_t)row_of_tile * page_bytes + (uint32_t)(place * D) + (uint32_t)(key * D);
-            else kp = a.st.kc + (uint64_t)(uint32_t)__shfl(row_of_key, key, 64) * page_bytes + (uint32_t)((key & (P - 1)) * D);
+            for (int b = 0; b < 4; ++b) {
+                const int key = my_key + 4 * b;
 #pragma unroll
-            for (int i = 0; i < C; ++i) kr[b][i] = *(const i32x4*)(kp + (uint32_t)(64 * i + 16 * quarter));
-            if constexpr (ODD) ko[b] = *(const uint2*)(kp + (uint32_t)(64 * C + 8 * quarter));
+                for (int i = 0; i < C; ++i) kr[b][i] = *(const i32x4*)(base + here(key * D + 64 * i + 16 * quarter));
+                if constexpr (ODD) ko[b] = *(const uint2*)(base + here(key * D + 64 * C + 8 * quarter));
+            }
+        } else {
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+                const int key = my_key + 4 * b;
+                const int8_t* kp = a.st.kc + (uint64_t)(uint32_t)__shfl(row_of_key, key, 64) * page_bytes + (uint32_t)((key & (P - 1)) * D);
+#pragma unroll
+                for (int i = 0; i < C; ++i) kr[b][i] = *(const i32x4*)(kp + (uint32_t)(64 * i + 16 * quarter));
+                if constexpr (ODD) ko[b] = *(const uint2*)(kp + (uint32_t)(64 * C + 8 * quarter));
+            }
         }
     };
     auto fetch_values = [&](bool have, int row_tile, int row_key, int at) {
         if (!have) return;
         const int key = 16 * quarter;
-        const int8_t* vp;
-        if constexpr (WHOLE) vp = a.st.vc + (uint64_t)(uint32_t)row_tile * page_bytes + (uint32_t)at + (uint32_t)((n << a.st.shift) + key);
-        else vp = a.st.vc + (uint64_t)(uint32_t)__shfl(row_key, key, 64) * page_bytes + (uint32_t)((n << a.st.shift) + (key & (P - 1)));
+        if constexpr (WHOLE) {
+            const int8_t* base = a.st.vc + (uint64_t)(uint32_t)row_tile * page_bytes + (uint32_t)at;
 #pragma unroll
-        for (int i = 0; i < DT; ++i) vr[i] = *(const i32x4*)(vp + ((uint32_t)(16 * i) << a.st.shift));
+            for (int i = 0; i < DT; ++i) vr[i] = *(const i32x4*)(base + here(((n + 16 * i) << a.st.shift) + key));
+        } else {
+            const int8_t* vp = a.st.vc + (uint64_t)(uint32_t)__shfl(row_key, key, 64) * page_bytes + (uint32_t)((n << a.st.shift) + (key & (P - 1)));
+#pragma unroll
+            for (int i = 0; i < DT; ++i) vr[i] = *(const i32x4*)(vp + ((uint32_t)(16 * i) << a.st.shift));
+        }
     };
     it.skip(a, tile.s, behind, 1 + wave);
     KeyTile cur = it.t;

@@ -116,14 +116,12 @@ __global__ void __launch_bounds__(64 * NW, RT == 1 ? 2 : 1) k_attend_tile(Attend
     // the steps of a key per lane.  Page numbers are requested one tile before they are used: pages of 64 tokens and more (WHOLE) hold a tile in one
     // piece, smaller ones are looked up for each piece.  A page number outside the store becomes page 0, its keys get no weight.
     // (Vector loads, all lanes the same where the page is: scalar loads would have to return before the next wait for LDS does.)
-    int lane_zero;
-    asm volatile("v_mov_b32 %0, 0" : "=v"(lane_zero));
     int pg[WHOLE ? 1 : PER], pg_step = 0;                       // WHOLE: the tile's page; else the pages of the thread's keys and of the lane's key
     int pv[WHOLE ? 1 : PER];                                    // ... and of the thread's values, of the tile before (WHOLE: as page * heads + head)
     auto page_at = [&](const KeyTile& kt, int key) { return kt.pages[min(kt.k + key, kt.length - 1) >> a.st.shift]; };
     auto find_pages = [&](const KeyTile& kt) {
         if (!kt.have) return;
-        if constexpr (WHOLE) pg[0] = kt.pages[(kt.k >> a.st.shift) + lane_zero];
+        if constexpr (WHOLE) pg[0] = *(const int32_t*)((const char*)(kt.pages + (kt.k >> a.st.shift)) + here(0));
         else {
 #pragma unroll
             for (int i = 0; i < PER; ++i) pg[i] = page_at(kt, (tid + i * THREADS) / (D / 16) % kTileKeys);
@@ -151,13 +149,13 @@ __global__ void __launch_bounds__(64 * NW, RT == 1 ? 2 : 1) k_attend_tile(Attend
             for (int i = 0; i < PER; ++i) {
                 const int p = tid + i * THREADS;
                 if (PIECES % THREADS && p >= PIECES) break;
-                ck[i] = *(const i32x4*)(base + (uint32_t)(16 * p));
+                ck[i] = *(const i32x4*)(base + here(16 * p));
             }
             if (wave == by) {
                 rhave = kt.k + lane < kt.length && (uint32_t)page < (uint64_t)a.st.pages;
                 const uint64_t at = ((uint64_t)(uint32_t)pv[0] << a.st.shift) + (uint32_t)off;
-                rks = (a.st.ks + at)[lane];
-                rvs = (a.st.vs + at)[lane];
+                rks = *(const float*)((const char*)(a.st.ks + at) + here(4 * lane));
+                rvs = *(const float*)((const char*)(a.st.vs + at) + here(4 * lane));
             }
         } else {
 #pragma unroll
@@ -183,7 +181,7 @@ __global__ void __launch_bounds__(64 * NW, RT == 1 ? 2 : 1) k_attend_tile(Attend
             const int p = tid + i * THREADS;
             if (PIECES % THREADS && p >= PIECES) break;
             const int comp = p / 4, grp = p % 4;
-            if constexpr (WHOLE) cv[i] = *(const i32x4*)(a.st.vc + (uint64_t)(uint32_t)pv[0] * page_bytes + (uint32_t)off_v + (uint32_t)((comp << a.st.shift) + 16 * grp));
+            if constexpr (WHOLE) cv[i] = *(const i32x4*)(a.st.vc + (uint64_t)(uint32_t)pv[0] * page_bytes + (uint32_t)off_v + here((comp << a.st.shift) + 16 * grp));
             else cv[i] = *(const i32x4*)(a.st.vc + (uint64_t)(uint32_t)row_of(pv[i]) * page_bytes + (uint32_t)((comp << a.st.shift) + ((16 * grp) & (P - 1))));
         }
     };
