@@ -200,18 +200,32 @@ struct KeyTile {
     bool have;
 };
 
-// The key tiles of one split, in order: units of tables (attend.hpp), 64 keys at a time.
+// The key tiles of one split, in order: units of tables (AttendArgs), 64 keys at a time.
 struct KeyTiles {
     int r, sub, left, k_end;
+    int r0, info;              // passages r0 .. r0 + 20: lanes 3 i, 3 i + 1, 3 i + 2 hold the number (-1: none), the length and the bias of passage r0 + i
     KeyTile t;
 
-    __device__ __forceinline__ void start(const AttendArgs& a, int split) {
+    __device__ __forceinline__ void start(const AttendArgs& a, int s, int split) {
         const int u = split * a.per_split;
         left = min(a.found * a.units, u + a.per_split) - u;
         r = u / a.units;
         sub = u - r * a.units - 1;
         k_end = 0;
         t = KeyTile{nullptr, 0, 0, 0.0f, true};
+        r0 = r;
+        info = 0;
+        if (a.ids && left > 0) look_up(a, s);
+    }
+    // Everything about the next 21 passages at once: one by one, each would wait for its number and then for its length.
+    __device__ __forceinline__ void look_up(const AttendArgs& a, int s) {
+        const int lane = threadIdx.x & 63, p = lane / 3, field = lane - 3 * p;
+        const int64_t at = (int64_t)s * a.found + min(r0 + p, a.found - 1);
+        const int64_t id = a.ids[at];
+        const float bias = a.scores ? a.weight * a.scores[at] : 0.0f;
+        const bool ok = (uint64_t)id < (uint64_t)a.passages && bias != -INFINITY;
+        const int length = min(max(a.lengths[ok ? id : 0], 0), a.width << a.st.shift);
+        info = field == 0 ? (ok ? (int)id : -1) : field == 1 ? length : __float_as_int(bias);
     }
     // Moves on by `n` tiles.
     __device__ __forceinline__ void skip(const AttendArgs& a, int s, int behind, int n) {
@@ -227,17 +241,19 @@ struct KeyTiles {
         while (t.k >= k_end) {
             if (--left < 0) { t.have = false; return; }
             if (++sub == a.units) { sub = 0; ++r; }
-            int64_t table = s;
-            t.bias = 0.0f;
+            int table = s;
             if (a.ids) {
-                table = a.ids[(int64_t)s * a.found + r];
+                if (r - r0 >= 21) { r0 = r; look_up(a, s); }
+                const int i = 3 * (r - r0);
+                table = __builtin_amdgcn_readlane(info, i);
                 t.k = k_end = 0;
-                if ((uint64_t)table >= (uint64_t)a.passages) continue;
-                if (a.scores) t.bias = a.weight * a.scores[(int64_t)s * a.found + r];
-                if (t.bias == -INFINITY) continue;
+                if (table < 0) continue;
+                t.length = __builtin_amdgcn_readlane(info, i + 1);
+                t.bias = __int_as_float(__builtin_amdgcn_readlane(info, i + 2));
+            } else {
+                t.length = min(max(a.lengths[table], 0), a.width << a.st.shift);
             }
-            t.pages = a.tables + table * a.width;
-            t.length = min(max(a.lengths[table], 0), a.width << a.st.shift);
+            t.pages = a.tables + (int64_t)table * a.width;
             t.k = sub * a.unit;
             k_end = min(a.ids ? t.length : t.length - behind, t.k + a.unit);
         }
@@ -278,7 +294,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, 2) k_attend_rows(AttendArgs
 
     // the wavefront's tiles: every fourth of the block's
     KeyTiles it;
-    it.start(a, split);
+    it.start(a, tile.s, split);
     int page = 0;                                               // lane = key of a tile: its page
     auto find_page = [&](const KeyTile& kt) {
         if (kt.have) page = kt.pages[min(kt.k + lane, kt.length - 1) >> a.st.shift];

@@ -331,7 +331,7 @@ __global__ void __launch_bounds__(64 * NW, RT == 1 ? 2 : 1) k_attend_tile(Attend
     static_assert(NW >= 3, "three wavefronts form the steps in turn");
     KeyTiles it;
     KeyTile d0, d1, d2;
-    it.start(a, split);
+    it.start(a, tile.s, split);
     it.next(a, tile.s, behind);
     d0 = it.t;
     find_pages(d0);

@@ -71,20 +71,16 @@ int check_tokens(const lorann_states* st, int32_t type, int64_t tokens) {
 
 // ---- attention ----
 
-constexpr int kTileWaves = 4, kTileRows = kTileWaves * 32;      // block of k_attend_tile
-
 struct Plan {
-    bool tiled;                      // k_attend_tile, else k_attend_rows
+    int32_t waves;                   // wavefronts of a block of k_attend_tile (32 rows each); 0: k_attend_rows
     int64_t tiles;                   // row tiles over all sequences, at most
     int32_t unit, units, splits, per_split;
     int64_t workspace;
 };
 
 constexpr int64_t kBlocksWanted = 1024;         // four blocks a CU: what keeps the memory system busy with ragged lengths
-constexpr int64_t kTileBlocksWanted = 512;
-#ifndef TILED_FROM
-#define TILED_FROM 64
-#endif
+constexpr int64_t kTileBlocksWanted = 512;      // two blocks of k_attend_tile a CU
+constexpr int64_t kTileFromRows = 32;           // rows per sequence and head (tokens x group) from which k_attend_tile is taken
 constexpr int64_t kKeysPerBlock = 64 * kAttendWaves;
 
 int check_questions(const lorann_states* st, const lorann_questions* qs, int32_t found, int32_t width) {
@@ -105,12 +101,12 @@ Plan plan_of(const lorann_states* st, const lorann_questions* qs, int32_t found,
     Plan p{};
     const int64_t group = qs->heads / st->heads;
     const int64_t sequences = std::max<int64_t>(qs->sequences, 1), mean_rows = qs->tokens * group / sequences;
-    p.tiled = mean_rows > TILED_FROM;
-    const int64_t rows_block = p.tiled ? kTileRows : kRows;
-    p.tiles = qs->q_start ? qs->tokens * group / rows_block + sequences : sequences * ceil_div(mean_rows, rows_block);
+    auto tiles_of = [&](int64_t rows) { return qs->q_start ? qs->tokens * group / rows + sequences : sequences * ceil_div(mean_rows, rows); };
+    p.waves = mean_rows <= kTileFromRows ? 0 : tiles_of(256) * st->heads >= 512 && mean_rows >= 1024 && st->dim > 64 ? 8 : 4;
+    p.tiles = tiles_of(p.waves ? 32 * p.waves : kRows);
     const int64_t table_keys = std::max<int64_t>((int64_t)width * st->page_size, 1), tables = std::max(found, 1), keys = tables * table_keys;
     const int64_t blocks = std::max<int64_t>(p.tiles * st->heads, 1);
-    const int64_t want = std::max<int64_t>(1, std::min((p.tiled ? kTileBlocksWanted : kBlocksWanted) / blocks, ceil_div(keys, kKeysPerBlock)));
+    const int64_t want = std::max<int64_t>(1, std::min((p.waves ? kTileBlocksWanted : kBlocksWanted) / blocks, ceil_div(keys, kKeysPerBlock)));
     if (want <= tables) {              // whole tables per split
         p.unit = (int32_t)(ceil_div(table_keys, kTileKeys) * kTileKeys);
         p.units = 1;
@@ -166,10 +162,15 @@ int attend(const lorann_states* st, const lorann_questions* qs, const int64_t* i
     int sides = 1;
     while (sides < p.splits && 2 * sides <= join_groups) sides *= 2;
     const dim3 join((unsigned)ceil_div(rows, join_groups / sides));
+#define LAUNCH_TILE(T_, D_, NW_)                                                                    \
+    do {                                                                                            \
+        if (a.st.shift >= 6) hipLaunchKernelGGL((k_attend_tile<T_, D_, NW_, 1, true>), tile_grid, dim3(64 * NW_), 0, stream, a); \
+        else hipLaunchKernelGGL((k_attend_tile<T_, D_, NW_, 1, false>), tile_grid, dim3(64 * NW_), 0, stream, a); \
+    } while (0)
 #define LAUNCH(T_, D_)                                                                              \
     do {                                                                                            \
-        if (p.tiled && a.st.shift >= 6) hipLaunchKernelGGL((k_attend_tile<T_, D_, kTileWaves, 1, true>), tile_grid, dim3(64 * kTileWaves), 0, stream, a); \
-        else if (p.tiled) hipLaunchKernelGGL((k_attend_tile<T_, D_, kTileWaves, 1, false>), tile_grid, dim3(64 * kTileWaves), 0, stream, a); \
+        if (p.waves == 8) LAUNCH_TILE(T_, D_, 8);                                                   \
+        else if (p.waves) LAUNCH_TILE(T_, D_, 4);                                                   \
         else if (a.st.shift >= 6) hipLaunchKernelGGL((k_attend_rows<T_, D_, true>), grid, block, 0, stream, a); \
         else hipLaunchKernelGGL((k_attend_rows<T_, D_, false>), grid, block, 0, stream, a);         \
         if (p.splits > 1) hipLaunchKernelGGL((k_attend_join<T_, D_>), join, dim3(256), 0, stream, a, sides); \
@@ -183,6 +184,7 @@ int attend(const lorann_states* st, const lorann_questions* qs, const int64_t* i
     }
 #undef LAUNCH_DIM
 #undef LAUNCH
+#undef LAUNCH_TILE
     HIP_TRY(hipGetLastError());
     return LORANN_OK;
 }
@@ -248,6 +250,7 @@ int lorann_attend_passages(const lorann_states* st, const lorann_questions* qs, 
     int rc;
     if ((rc = check_sizes(st)) || (rc = check_questions(st, qs, found, width))) return rc;
     if (passages < 0) return fail(LORANN_E_INVAL, "%lld passages", (long long)passages);
+    if (passages > 0x7fffffff) return fail(LORANN_E_UNSUPPORTED, "%lld passages are more than 32 bits count", (long long)passages);
     if (!(std::fabs(score_weight) <= 1.0e38f)) return fail(LORANN_E_INVAL, "the weight of the scores is not finite");
     if (found < 1) return fail(LORANN_E_INVAL, "%d passages per sequence", found);
     if (qs->tokens > 0 && qs->sequences > 0) {
