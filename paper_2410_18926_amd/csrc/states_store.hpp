@@ -143,11 +143,55 @@ __device__ __forceinline__ uint32_t any_word(const uint8_t* p) {
     return __builtin_amdgcn_alignbyte(w[1], w[0], a);
 }
 
-// One rounded division per value would be most of the kernel's time: rint(127 x / top) is formed as rint(q) with q = 127 x * (1 / top), and the quotient is
-// divided only where q lies within 2^-10 of a half, where an error of q (below 2^-15: three roundings of 2^-24 relative, |q| <= 127) could decide.
-__device__ __forceinline__ float code_of(float x, float top, float inverse) {
-    const float p = x * 127.0f, q = p * inverse, r = rintf(q);
-    return fabsf(fabsf(q - r) - 0.5f) < 0x1p-10f ? rintf(p / top) : r;
+// The largest of 16 lanes (a row of the wavefront) in each of them.
+__device__ __forceinline__ uint32_t row_max_u32(uint32_t v) {
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x128, 0xf, 0xf, true));      // rotated by 8, 4, 2, 1 lanes
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x124, 0xf, 0xf, true));
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x122, 0xf, 0xf, true));
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x121, 0xf, 0xf, true));
+    return v;
+}
+
+// Four rows of 16 lanes hold four tokens t .. t + 3, lane l of a row the bytes 8 l .. 8 l + 7 of its token in `lo`, `hi`.  Afterwards `lo`, `hi` hold the four
+// tokens' bytes of components turned_component(lane) and the next one; turn_back undoes it.
+__device__ __forceinline__ void turn(uint32_t& lo, uint32_t& hi) {
+    const auto a = __builtin_amdgcn_permlane32_swap(lo, hi, false, false);     // lower half: bytes 0-3 of tokens r, r + 2; upper half: bytes 4-7
+    const uint32_t x = __builtin_amdgcn_perm(a[1], a[0], 0x05010400u), y = __builtin_amdgcn_perm(a[1], a[0], 0x07030602u);
+    const auto b = __builtin_amdgcn_permlane16_swap(x, y, false, false);       // even rows: the first two components, of tokens 0, 2 and 1, 3; odd rows: the others
+    lo = __builtin_amdgcn_perm(b[1], b[0], 0x05010400u);
+    hi = __builtin_amdgcn_perm(b[1], b[0], 0x07030602u);
+}
+__device__ __forceinline__ void turn_back(uint32_t& lo, uint32_t& hi) {
+    const uint32_t x = __builtin_amdgcn_perm(hi, lo, 0x06040200u), y = __builtin_amdgcn_perm(hi, lo, 0x07050301u);
+    const auto b = __builtin_amdgcn_permlane16_swap(x, y, false, false);
+    const uint32_t p = __builtin_amdgcn_perm(b[1], b[0], 0x06040200u), q = __builtin_amdgcn_perm(b[1], b[0], 0x07050301u);
+    const auto a = __builtin_amdgcn_permlane32_swap(p, q, false, false);
+    lo = a[0];
+    hi = a[1];
+}
+__device__ __forceinline__ int turned_component(int lane) { return (lane & 15) * 8 + (lane >> 5) * 4 + (lane >> 4 & 1) * 2; }
+
+// Eight codes of a row whose largest magnitude is `top` (finite, not tiny).  The definition divides: rint(127 x / top).  Here q = x * (127 / top), rounded by
+// adding 1.5 * 2^23, whose low byte then is the code; where a q lies within 2^-14 of a half, the eight are divided (one wavefront in twenty).  Before rounding, q and the
+// definition's quotient are each off by at most two roundings of 2^-24 relative of at most 127: 2^-15 in all.
+__device__ __forceinline__ uint2 codes_of(const float (&x)[8], float top) {
+    const float scale = 127.0f / top;
+    float t[8], worst = 0.0f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const float q = x[j] * scale;
+        t[j] = q + 12582912.0f;
+        worst = fmaxf(worst, fabsf(q - (t[j] - 12582912.0f)));
+    }
+    if (worst > 0.5f - 0x1p-14f) {
+        const float keep = top > kHugeRow ? kHugeDown : 1.0f, low = top * keep;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) t[j] = rintf(x[j] * keep * 127.0f / low) + 12582912.0f;
+    }
+    uint32_t c[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) c[j] = __builtin_amdgcn_perm(__float_as_uint(t[2 * j + 1]), __float_as_uint(t[2 * j]), 0x0c0c0400u);
+    return uint2{c[0] | c[1] << 16, c[2] | c[3] << 16};
 }
 
 template <typename T>
@@ -157,50 +201,58 @@ __global__ void __launch_bounds__(256) k_states_write(Store st, TokenRows k, Tok
     const int64_t token0 = (int64_t)blockIdx.x * kBlockTokens;
     const int head = blockIdx.y;
     const bool values = blockIdx.z;
-    load_slots(bs, st, slots, token0, tokens, values);
     const TokenRows in = values ? v : k;
     const int lane = threadIdx.x & 15, d = lane * 8, P = 1 << st.shift;
-    // a group of 16 lanes per row, 16 rows at a time: all rows are requested before the first is used
+    const int last = (int)min(tokens - 1 - token0, (int64_t)kBlockTokens - 1);
+    // a group of 16 lanes per row, 16 rows at a time: all rows are requested first, without regard to their slots
     float f[4][8];
-    const T* x = (const T*)in.p + token0 * in.token + head * in.head;
+    {
+        const T* x = (const T*)in.p + token0 * in.token + head * in.head + (d < dim ? d : 0);
+        const int t = threadIdx.x >> 4;
+        if (last >= 16) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int t = i * 16 + (threadIdx.x >> 4);
-        if (d < dim && bs.slot[t] >= 0) Eight<T>::load(x + t * in.token + d, in.wide, f[i]);
-        else {
+            for (int i = 0; i < 4; ++i) Eight<T>::load(x + min(i * 16 + t, last) * in.token, in.wide, f[i]);
+        } else {                                               // (a few tokens: one row a group)
+            Eight<T>::load(x + min(t, last) * in.token, in.wide, f[0]);
+#pragma unroll
+            for (int i = 1; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) f[i][j] = 0.0f;
+        }
+    }
+    load_slots(bs, st, slots, token0, tokens, values);
+    if (d >= dim) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int j = 0; j < 8; ++j) f[i][j] = 0.0f;
-        }
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
+        if (i > 0 && last < 16) break;
         const int t = i * 16 + (threadIdx.x >> 4);
-        float top = 0.0f;
-        bool bad = false;
+        uint32_t most = 0;                                     // bits of the largest magnitude: infinities and NaN are above every number
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            bad |= !(fabsf(f[i][j]) <= 3.4028235e38f);
-            top = fmaxf(top, fabsf(f[i][j]));
-        }
-        if (bad) top = INFINITY;                               // (the maximum of the row, unless a value of it is no number: then infinity)
-#pragma unroll
-        for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 16));
-        bad = top == INFINITY;
-        const bool zero = bad || top < kTinyRow;
-        const float keep = top > kHugeRow ? kHugeDown : 1.0f, low = top * keep, inverse = zero ? 0.0f : 1.0f / low;
-        union { int8_t c[8]; uint2 u; } code;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) code.c[j] = zero ? (int8_t)0 : (int8_t)code_of(f[i][j] * keep, low, inverse);
+        for (int j = 0; j < 8; ++j) most = max(most, __float_as_uint(f[i][j]) & 0x7fffffffu);
+        most = row_max_u32(most);
+        const float top = __uint_as_float(most);
+        const bool bad = most >= 0x7f800000u, zero = bad || top < kTinyRow;
+        uint2 code = codes_of(f[i], zero ? 1.0f : top);
+        if (zero) code = uint2{0, 0};
         const int64_t slot = bs.slot[t];
-        if (slot < 0) continue;
-        const int64_t base = st.row(slot >> st.shift, head);
-        const int off = (int)(slot & (P - 1));
-        if (lane == 0) (values ? st.vs : st.ks)[base + off] = bad ? __int_as_float(0x7fc00000) : zero ? 0.0f : top / 127.0f;
-        if (d >= dim) continue;
-        if (!values) *(uint2*)(st.kc + (base + off) * dim + d) = code.u;
-        else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) lds[(d + j) * kTokenStride + t] = (uint8_t)code.c[j];
+        if (slot >= 0) {
+            const int64_t base = st.row(slot >> st.shift, head);
+            const int off = (int)(slot & (P - 1));
+            if (lane == 0) (values ? st.vs : st.ks)[base + off] = bad ? __int_as_float(0x7fc00000) : zero ? 0.0f : top / 127.0f;
+            if (!values && d < dim) *(uint2*)(st.kc + (base + off) * dim + d) = code;
+        }
+        if (values) {
+            turn(code.x, code.y);
+            const int comp = turned_component(threadIdx.x & 63), t0 = i * 16 + (threadIdx.x >> 6) * 4;
+            if (comp < dim) {
+                *(uint32_t*)&lds[comp * kTokenStride + t0] = code.x;
+                *(uint32_t*)&lds[(comp + 1) * kTokenStride + t0] = code.y;
+            }
         }
     }
     if (!values) return;
@@ -267,30 +319,31 @@ __global__ void __launch_bounds__(256) k_states_read(Store st, const int64_t* __
         }
         __syncthreads();
     }
-    if (d >= dim) return;
     T* x = (T*)to.p + token0 * to.token + head * to.head;
+    const int last = (int)min(tokens - 1 - token0, (int64_t)kBlockTokens - 1);
     uint2 code[4];
     float step[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
+        if (i * 16 > last) break;
         const int t = i * 16 + (threadIdx.x >> 4);
         const int64_t slot = bs.slot[t];
         const int64_t base = slot < 0 ? 0 : st.row(slot >> st.shift, head);
         const int off = slot < 0 ? 0 : (int)(slot & (P - 1));
         step[i] = (values ? st.vs : st.ks)[base + off];         // (of some token where there is none)
         code[i] = uint2{0, 0};
-        if (!values) code[i] = *(const uint2*)(st.kc + (base + off) * dim + d);
+        if (values) {
+            const int comp = turned_component(threadIdx.x & 63), t0 = i * 16 + (threadIdx.x >> 6) * 4;
+            if (comp < dim) code[i] = uint2{*(const uint32_t*)&lds[comp * kTokenStride + t0], *(const uint32_t*)&lds[(comp + 1) * kTokenStride + t0]};
+            turn_back(code[i].x, code[i].y);
+        } else if (d < dim) code[i] = *(const uint2*)(st.kc + (base + off) * dim + d);
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int t = i * 16 + (threadIdx.x >> 4);
-        if (token0 + t >= tokens) break;
+        if (d >= dim || t > last) break;
         union { int8_t c[8]; uint2 u; } c;
         c.u = code[i];
-        if (values) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) c.c[j] = (int8_t)lds[(d + j) * kTokenStride + t];
-        }
         float f[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
