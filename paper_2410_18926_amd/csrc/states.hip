@@ -65,7 +65,7 @@ TokenRows rows_of(void* p, int64_t token, int64_t head, int32_t type) {
 int check_tokens(const lorann_states* st, int32_t type, int64_t tokens) {
     if (!element_size(type)) return fail(LORANN_E_INVAL, "unknown element type %d", type);
     if (tokens < 0) return fail(LORANN_E_INVAL, "%lld tokens", (long long)tokens);
-    if (tokens > 0x7fffffffLL / st->heads) return fail(LORANN_E_UNSUPPORTED, "%lld tokens of %d heads in one call", (long long)tokens, st->heads);
+    if (tokens > 0x7fffffffLL / st->heads || tokens >= 1 << 30) return fail(LORANN_E_UNSUPPORTED, "%lld tokens of %d heads in one call", (long long)tokens, st->heads);
     return LORANN_OK;
 }
 
@@ -134,6 +134,8 @@ int attend(const lorann_states* st, const lorann_questions* qs, const int64_t* i
     if (qs->q_start && (rc = check_device(qs->q_start, "q_start"))) return rc;
     if (width > 0 && (!ids || passages > 0) && (!ids || found > 0) && ((rc = check_device(tables, "tables")) || (rc = check_device(lengths, "lengths")))) return rc;
     const Plan p = plan_of(st, qs, found, width);
+    if ((p.waves ? p.tiles * st->heads * 64 * p.waves : p.tiles * 64 * kAttendWaves) > 0xffffffffLL)       // threads of a grid's first dimension
+        return fail(LORANN_E_UNSUPPORTED, "%lld tokens of %lld sequences are more than one launch holds", (long long)qs->tokens, (long long)qs->sequences);
     if (p.workspace) {
         if (!workspace || workspace_bytes < p.workspace) return fail(LORANN_E_INVAL, "the workspace holds %lld bytes, %lld are needed", (long long)(workspace ? workspace_bytes : 0), (long long)p.workspace);
         if (!aligned(workspace, 16)) return fail(LORANN_E_INVAL, "the workspace is not 16-byte aligned");

@@ -83,7 +83,7 @@ class States:
         if k_codes.dim() != 4:
             raise ValueError(f"k_codes must be [pages, heads, page_size, dim], got {tuple(k_codes.shape)}")
         self.pages, self.heads, self.page_size, self.dim = n, h, p, d = k_codes.shape
-        self._on_gpu = k_codes.is_cuda
+        self._gpu = k_codes.device.index if k_codes.is_cuda else None
         steps = (n, h, p)
         self._st = CStates(_array(k_codes, torch.int8, k_codes.shape, "k_codes"), _array(v_codes, torch.int8, (n, h, d, p), "v_codes"),
                            _array(k_scales, torch.float32, steps, "k_scales"), _array(v_scales, torch.float32, steps, "v_scales"), n, h, p, d)
@@ -106,7 +106,11 @@ class States:
 
     def _stream(self):
         """torch's current stream (its handle alone: the stream object takes longer than a launch)."""
-        return _raw_stream(_current_device()) if self._on_gpu else None
+        if self._gpu is None:
+            return None            # (host memory: the library refuses it)
+        if self._gpu != _current_device():
+            raise ValueError(f"the store is on cuda:{self._gpu}, the current device is cuda:{_current_device()}")
+        return _raw_stream(self._gpu)
 
     def write(self, k, v, slots):
         """Quantise keys and values [tokens, heads, dim] (float32, float16 or bfloat16; any distances between tokens and heads) into their slots

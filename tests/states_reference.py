@@ -116,6 +116,33 @@ def passages(st, q, ids, tables, lengths, q_start, scores, weight, scale):
     return out.reshape(q.shape), tol.reshape(q.shape)
 
 
+def chunk_on_gpu(st, q, tables, lengths, q_start, scale):
+    """chunk() for sizes that are too many for one row at a time: the same in float64 on the GPU, a sequence and query head at a time.  Tensors."""
+    H, G, D, P = st.heads, q.shape[1] // st.heads, st.dim, st.page_size
+    out, tol = torch.zeros(q.shape, dtype=torch.float64, device=q.device), torch.zeros(q.shape, dtype=torch.float64, device=q.device)
+    for s in range(tables.shape[0]):
+        lo, hi, n = int(q_start[s]), int(q_start[s + 1]), int(lengths[s])
+        t = torch.arange(n, device=q.device)
+        page, off = tables[s].long()[t // P], t % P
+        seen = t[None, :] <= (n - (hi - lo) + torch.arange(hi - lo, device=q.device))[:, None]
+        for h in range(H):
+            ks, vs = st.k_scales[page, h, off].double(), st.v_scales[page, h, off].double()
+            vc = st.v_codes[page, h, :, off].double()
+            k, v = st.k_codes[page, h, off].double() * ks[:, None], vc * vs[:, None]
+            for g in range(G):
+                x = q[lo:hi, h * G + g].double()
+                z = (scale * (x @ k.T)).masked_fill(~seen, float("-inf"))
+                p = torch.softmax(z, 1)
+                o, a = p @ v, p @ v.abs()
+                y = z / np.log(2) + torch.log2(vs)
+                w = torch.exp2(y - y.max(1, keepdim=True).values)
+                e = (D + 8) * 2.0 ** -24 * abs(scale) * (x.abs() @ k.abs().T).max(1, keepdim=True).values + 2.0 ** -21 * (y.masked_fill(~seen, 0).abs().max(1, keepdim=True).values + 8)
+                sub = 2.0 ** -25 * (seen.double() @ vc.abs()) / (w / vs).sum(1, keepdim=True)
+                out[lo:hi, h * G + g] = o
+                tol[lo:hi, h * G + g] = U_OUT[q.dtype] * o.abs() + (2.0 ** -11 + 2 * e + 2 * n * 2.0 ** -24) * a + sub + 1e-30
+    return out, tol
+
+
 def assert_close(got, want, tol, what=""):
     got = got.detach().cpu().double().numpy()
     assert got.shape == want.shape, what

@@ -195,6 +195,39 @@ def test_chunk(S, new, lengths, heads, group, dim, page, dtype):
     assert torch.equal(got, again), "two runs differ"
 
 
+MORE_CHUNKS = [
+    # rows enough for shared tiles at every width, pages smaller and larger than a tile
+    ([40, 60], [40, 333], 2, 2, 32, 16, F16),
+    ([70], [500], 1, 3, 32, 128, BF16),
+    ([50, 20], [300, 700], 2, 3, 96, 128, BF16),
+    ([45], [129], 3, 2, 96, 64, F16),
+    ([90], [4000], 1, 1, 64, 32, BF16),
+    ([33, 0, 64], [33, 50, 4097], 1, 4, 128, 256, F16),
+]
+
+
+@pytest.mark.parametrize("new,lengths,heads,group,dim,page,dtype", MORE_CHUNKS)
+def test_chunk_in_shared_tiles(S, new, lengths, heads, group, dim, page, dtype):
+    test_chunk(S, new, lengths, heads, group, dim, page, dtype)
+
+
+@pytest.mark.parametrize("sequences,new,context,heads,group,dim,page", [(4, 600, 300, 8, 8, 128, 64), (4, 513, 100, 16, 4, 96, 32), (3, 700, 777, 8, 4, 64, 64)])
+def test_large_chunks(S, sequences, new, context, heads, group, dim, page):
+    """Rows enough to fill the GPU with the largest blocks."""
+    g = gen(21)
+    lengths = [new + context + 17 * i for i in range(sequences)]
+    pages = sum(-(-n // page) for n in lengths) + 1
+    st = filled(S, pages, heads, page, dim, seed=22, spread=0.3)
+    tables = dev(make_tables(g, lengths, pages, page, junk=False))
+    q = (1.5 * randn(g, sequences * new, heads * group, dim)).to(BF16)
+    want, tol = R.chunk_on_gpu(st, q, tables, lengths, [i * new for i in range(sequences + 1)], dim ** -0.5)
+    got = st.attend_chunk(q, tables, dev(lengths))
+    off = (got.double() - want).abs() - tol
+    assert not (off > 0).any() and not torch.isnan(got).any(), float(off.max())
+    start = dev([i * new for i in range(sequences + 1)])
+    assert torch.equal(got, st.attend_chunk(q, tables, dev(lengths), q_start=start)), "two runs differ"
+
+
 def test_many_short_sequences(S):
     """More sequences than a wavefront counts at a time, some without queries."""
     g = gen(3)
@@ -243,6 +276,23 @@ def test_passages(S, new, found, stock, heads, group, dim, page, dtype, weighted
     if len(set(new)) == 1:
         R.assert_close(st.attend_passages(q, dev(ids, torch.int64), dev(tables), dev(stock), **args), want, tol, "the same number each")
     assert torch.equal(got, st.attend_passages(q, dev(ids, torch.int64), dev(tables), dev(stock), q_start=dev(start), **args)), "two runs differ"
+
+
+MORE_PASSAGES = [
+    # more passages than are looked up at a time (found, and numbers outside among them)
+    ([1, 1], 50, [30, 64, 5, 100, 0, 17] * 3, 2, 4, 64, 16, BF16, True),
+    ([40], 64, [9, 70, 33, 0, 128] * 4, 1, 2, 128, 64, F16, True),
+    ([17, 30], 43, [20, 16, 64, 40] * 5, 2, 3, 32, 16, BF16, False),
+    ([1], 22, [300, 65], 1, 16, 96, 32, BF16, True),
+    # one long passage for one token: cut, and joined
+    ([1], 1, [3000], 2, 4, 128, 64, BF16, False),
+    ([60], 2, [2500, 900], 1, 2, 64, 128, BF16, True),
+]
+
+
+@pytest.mark.parametrize("new,found,stock,heads,group,dim,page,dtype,weighted", MORE_PASSAGES)
+def test_many_and_long_passages(S, new, found, stock, heads, group, dim, page, dtype, weighted):
+    test_passages(S, new, found, stock, heads, group, dim, page, dtype, weighted)
 
 
 @pytest.mark.parametrize("new", [1, 40])

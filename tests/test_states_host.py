@@ -106,6 +106,8 @@ def test_other_refusals(S):
     refused(-4, "passages", L.lorann_attend_passages(st, qs, 16, 5000, None, 1.0, 16, 1, 16, 1, None, 0, None))
     refused(-1, "passages", L.lorann_attend_passages(st, qs, 16, 1, None, 1.0, 16, 1, 16, -1, None, 0, None))
     refused(-1, "weight", L.lorann_attend_passages(st, qs, 16, 1, None, float("nan"), 16, 1, 16, 1, None, 0, None))
+    refused(-4, "tokens", L.lorann_states_write(store(S, heads=1), 16, 16, 0, 2 ** 30, 1, 1, 1, 1, 16, None))
+    refused(-4, "passages", L.lorann_attend_passages(st, qs, 16, 1, None, 1.0, 16, 1, 16, 2 ** 31, None, 0, None))
     # host memory where device memory is asked for
     host = torch.zeros(64, dtype=torch.float32)
     at = host.data_ptr() + (-host.data_ptr()) % 16
