@@ -35,9 +35,18 @@ struct AttendArgs {
     float weight;                      // score_weight * log2 e
     int32_t unit, units;               // a table's keys are taken in `units` units of `unit` keys
     int32_t splits, per_split;         // units (over all passages of the sequence) per split
-    float *part_acc, *part_m, *part_l; // [splits][tokens * query heads][dim], and [splits][tokens * query heads] (splits > 1)
+    float *part_acc, *part_m, *part_l; // [splits][tokens * query heads][dim] (not written where part_l is 0), and [splits][tokens * query heads] (splits > 1)
     bool q_wide, out_wide;             // rows are aligned to 16 / 8 bytes
 };
+
+// Which head, split and row tile a block has.  Consecutive blocks, which go to different dies (each with an L2 and a share of the memory bandwidth of its own), are the heads
+// and then the splits of one row tile: one long sequence among short ones is read by all of them.  (With the row tiles consecutive, a token after 131072 keys
+// beside 63 after 1000 took 808 us, all of it on one die; 156 us so.)
+struct BlockWork { int head, split, tile; };
+__device__ __forceinline__ BlockWork block_work(const AttendArgs& a) {
+    const int rest = blockIdx.x / a.st.heads, tile = rest / a.splits;
+    return BlockWork{(int)blockIdx.x - rest * a.st.heads, rest - tile * a.splits, tile};
+}
 
 // Which tile of query rows a block has.
 struct RowTile {
@@ -281,9 +290,10 @@ __global__ void __launch_bounds__(64 * kAttendWaves, 2) k_attend_rows(AttendArgs
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = lane & 15, quarter = lane >> 4;
-    const int head = blockIdx.y, split = blockIdx.z;
+    const BlockWork work = block_work(a);
+    const int head = work.head, split = work.split;
     RowTile tile;
-    if (!find_tile<kRows>(a, blockIdx.x, tile)) return;
+    if (!find_tile<kRows>(a, work.tile, tile)) return;
     const int rows = tile.count * a.group;
     const int row = tile.row0 + n;
     const bool live = row < rows;
@@ -529,7 +539,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, 2) k_attend_rows(AttendArgs
             store4<T>(a.out, (int64_t)t * a.out_token + (int64_t)hq * a.out_head + d, a.out_wide, o * inv);
         } else {
             const int64_t at = ((int64_t)split * a.tokens + t) * heads + hq;
-            *(f32x4*)&a.part_acc[at * D + d] = o;
+            if (l != 0.0f) *(f32x4*)&a.part_acc[at * D + d] = o;       // (l = 0: no key was seen, and nothing is read there)
             if (d == 0) { a.part_m[at] = m; a.part_l[at] = l; }
         }
     }
@@ -567,7 +577,8 @@ __global__ void __launch_bounds__(256) k_attend_join(AttendArgs a, int sides) {
                 if (s0 + i * sides >= a.splits) break;
                 const float m_new = fmaxf(m, ms[i]), m_use = m_new == -INFINITY ? 0.0f : m_new;
                 l = times_exp2(l, m - m_use) + times_exp2(ls[i], ms[i] - m_use);
-                o = o * __builtin_amdgcn_exp2f(m - m_use) + os[i] * __builtin_amdgcn_exp2f(ms[i] - m_use);
+                o = o * __builtin_amdgcn_exp2f(m - m_use);
+                if (ls[i] != 0.0f) o += os[i] * __builtin_amdgcn_exp2f(ms[i] - m_use);
                 m = m_new;
             }
         }

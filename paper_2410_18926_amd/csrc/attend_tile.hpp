@@ -32,9 +32,10 @@ __global__ void __launch_bounds__(64 * NW, RT == 1 ? 2 : 1) k_attend_tile(Attend
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = lane & 31, half = lane >> 5;
-    const int head = blockIdx.x % a.st.heads, split = blockIdx.y;
+    const BlockWork work = block_work(a);
+    const int head = work.head, split = work.split;
     RowTile tile;
-    if (!find_tile<ROWS>(a, blockIdx.x / a.st.heads, tile)) return;
+    if (!find_tile<ROWS>(a, work.tile, tile)) return;
     const int rows = tile.count * a.group;
     const int P = 1 << a.st.shift;
 
@@ -536,11 +537,13 @@ __global__ void __launch_bounds__(64 * NW, RT == 1 ? 2 : 1) k_attend_tile(Attend
                 }
         } else {
             const int64_t at = ((int64_t)split * a.tokens + at_tok) * heads + qh;
+            if (l != 0.0f) {
 #pragma unroll
-            for (int i = 0; i < C; ++i)
+                for (int i = 0; i < C; ++i)
 #pragma unroll
-                for (int g = 0; g < 4; ++g)
-                    *(f32x4*)&a.part_acc[at * D + 32 * i + 8 * g + 4 * half] = f32x4{acc[t][i][4 * g], acc[t][i][4 * g + 1], acc[t][i][4 * g + 2], acc[t][i][4 * g + 3]};
+                    for (int g = 0; g < 4; ++g)
+                        *(f32x4*)&a.part_acc[at * D + 32 * i + 8 * g + 4 * half] = f32x4{acc[t][i][4 * g], acc[t][i][4 * g + 1], acc[t][i][4 * g + 2], acc[t][i][4 * g + 3]};
+            }
             if (half == 0) { a.part_m[at] = M[t]; a.part_l[at] = l; }
         }
     }

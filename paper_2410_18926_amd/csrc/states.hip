@@ -78,8 +78,11 @@ struct Plan {
     int64_t workspace;
 };
 
-constexpr int64_t kBlocksWanted = 1024;         // four blocks a CU: what keeps the memory system busy with ragged lengths
-constexpr int64_t kTileBlocksWanted = 512;      // two blocks of k_attend_tile a CU
+// Splitting.  Two blocks of either kernel fit a CU: 512 fill the GPU, more only add to what is joined (a token after 131071 keys: 53 us with 512, 59 with
+// 1024, 68 with 1536).  The host does not know the lengths, only the tables' width: where that is long, a block still gets at most so many keys, so that one
+// long sequence among short ones does not run on a few CUs alone.
+constexpr int64_t kBlocksWanted = 512;
+constexpr int64_t kMostKeys = 16384, kMostTileKeys = 32768, kMostPartRows = 1 << 17;      // (and no more than that many rows of partial answers)
 constexpr int64_t kTileFromRows = 32;           // rows per sequence and head (tokens x group) from which k_attend_tile is taken
 constexpr int64_t kKeysPerBlock = 64 * kAttendWaves;
 
@@ -105,8 +108,8 @@ Plan plan_of(const lorann_states* st, const lorann_questions* qs, int32_t found,
     p.waves = mean_rows <= kTileFromRows ? 0 : tiles_of(256) * st->heads >= 512 && mean_rows >= 1024 && st->dim > 64 ? 8 : 4;
     p.tiles = tiles_of(p.waves ? 32 * p.waves : kRows);
     const int64_t table_keys = std::max<int64_t>((int64_t)width * st->page_size, 1), tables = std::max(found, 1), keys = tables * table_keys;
-    const int64_t blocks = std::max<int64_t>(p.tiles * st->heads, 1);
-    const int64_t want = std::max<int64_t>(1, std::min((p.waves ? kTileBlocksWanted : kBlocksWanted) / blocks, ceil_div(keys, kKeysPerBlock)));
+    const int64_t blocks = std::max<int64_t>(p.tiles * st->heads, 1), rows = std::max<int64_t>(qs->tokens * qs->heads, 1);
+    const int64_t want = std::max(std::max<int64_t>(1, std::min(kBlocksWanted / blocks, ceil_div(keys, kKeysPerBlock))), std::min(ceil_div(keys, p.waves ? kMostTileKeys : kMostKeys), kMostPartRows / rows));
     if (want <= tables) {              // whole tables per split
         p.unit = (int32_t)(ceil_div(table_keys, kTileKeys) * kTileKeys);
         p.units = 1;
@@ -118,7 +121,6 @@ Plan plan_of(const lorann_states* st, const lorann_questions* qs, int32_t found,
         p.per_split = 1;
         p.splits = (int32_t)(tables * p.units);
     }
-    const int64_t rows = qs->tokens * qs->heads;
     p.workspace = p.splits > 1 ? (int64_t)p.splits * rows * (st->dim + 2) * 4 : 0;
     return p;
 }
@@ -134,7 +136,8 @@ int attend(const lorann_states* st, const lorann_questions* qs, const int64_t* i
     if (qs->q_start && (rc = check_device(qs->q_start, "q_start"))) return rc;
     if (width > 0 && (!ids || passages > 0) && (!ids || found > 0) && ((rc = check_device(tables, "tables")) || (rc = check_device(lengths, "lengths")))) return rc;
     const Plan p = plan_of(st, qs, found, width);
-    if ((p.waves ? p.tiles * st->heads * 64 * p.waves : p.tiles * 64 * kAttendWaves) > 0xffffffffLL)       // threads of a grid's first dimension
+    const int64_t blocks = p.tiles * st->heads * p.splits;
+    if (p.tiles > 0x7fffffff || blocks > 0xffffffffLL / (64 * std::max(p.waves, kAttendWaves)))       // (threads of a grid)
         return fail(LORANN_E_UNSUPPORTED, "%lld tokens of %lld sequences are more than one launch holds", (long long)qs->tokens, (long long)qs->sequences);
     if (p.workspace) {
         if (!workspace || workspace_bytes < p.workspace) return fail(LORANN_E_INVAL, "the workspace holds %lld bytes, %lld are needed", (long long)(workspace ? workspace_bytes : 0), (long long)p.workspace);
@@ -158,16 +161,15 @@ int attend(const lorann_states* st, const lorann_questions* qs, const int64_t* i
     a.part_l = a.part_m + (int64_t)p.splits * rows;
     a.q_wide = aligned(qs->q, 16) && qs->q_token % 8 == 0 && qs->q_head % 8 == 0;
     a.out_wide = aligned(qs->out, 8) && qs->out_token % 4 == 0 && qs->out_head % 4 == 0;
-    const dim3 grid((unsigned)p.tiles, (unsigned)st->heads, (unsigned)p.splits), block(64 * kAttendWaves);
-    const dim3 tile_grid((unsigned)(p.tiles * st->heads), (unsigned)p.splits);
+    const dim3 grid((unsigned)blocks), block(64 * (p.waves ? p.waves : kAttendWaves));
     const int join_groups = 256 / (st->dim / 4);
     int sides = 1;
     while (sides < p.splits && 2 * sides <= join_groups) sides *= 2;
     const dim3 join((unsigned)ceil_div(rows, join_groups / sides));
 #define LAUNCH_TILE(T_, D_, NW_)                                                                    \
     do {                                                                                            \
-        if (a.st.shift >= 6) hipLaunchKernelGGL((k_attend_tile<T_, D_, NW_, 1, true>), tile_grid, dim3(64 * NW_), 0, stream, a); \
-        else hipLaunchKernelGGL((k_attend_tile<T_, D_, NW_, 1, false>), tile_grid, dim3(64 * NW_), 0, stream, a); \
+        if (a.st.shift >= 6) hipLaunchKernelGGL((k_attend_tile<T_, D_, NW_, 1, true>), grid, block, 0, stream, a); \
+        else hipLaunchKernelGGL((k_attend_tile<T_, D_, NW_, 1, false>), grid, block, 0, stream, a); \
     } while (0)
 #define LAUNCH(T_, D_)                                                                              \
     do {                                                                                            \
