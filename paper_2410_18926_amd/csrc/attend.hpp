@@ -302,10 +302,18 @@ __global__ void __launch_bounds__(64 * kAttendWaves, 2) k_attend_rows(AttendArgs
     const int behind = tile.count - 1 - (min(rows, tile.row0 + kRows) - 1) / a.group, first_behind = tile.count - 1 - tile.row0 / a.group;
     const int P = 1 << a.st.shift;
 
+    // What does not depend on lengths is requested first: the queries, and (chunk: one unit of the sequence's own table) the pages of the wavefront's first tile.
+    const int qh = head * a.group + (live ? row - tok * a.group : 0);
+    const int64_t q_at = (int64_t)(tile.first + tok) * a.q_token + (int64_t)qh * a.q_head;
+    i32x4 raw[S32];
+#pragma unroll
+    for (int i = 0; i < S32; ++i) raw[i] = load8_raw(a.q, q_at + (i < 2 * C ? 64 * (i >> 1) + 16 * quarter + 8 * (i & 1) : 64 * C + 8 * quarter), a.q_wide);
+    int page = 0;                                               // lane = key of a tile: its page
+    const bool ahead = !a.ids && a.width > 0;
+    if (ahead) page = a.tables[(int64_t)tile.s * a.width + min((split * a.unit + wave * kTileKeys + lane) >> a.st.shift, a.width - 1)];
     // the wavefront's tiles: every fourth of the block's
     KeyTiles it;
     it.start(a, tile.s, split);
-    int page = 0;                                               // lane = key of a tile: its page
     auto find_page = [&](const KeyTile& kt) {
         if (kt.have) page = kt.pages[min(kt.k + lane, kt.length - 1) >> a.st.shift];
     };
@@ -363,7 +371,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, 2) k_attend_rows(AttendArgs
     };
     it.skip(a, tile.s, behind, 1 + wave);
     KeyTile cur = it.t;
-    find_page(cur);
+    if (!ahead) find_page(cur);
     fetch_keys(cur);
     const int first_row_tile = row_of_tile, first_row_key = row_of_key, first_place = place;
     it.skip(a, tile.s, behind, kAttendWaves);
@@ -374,12 +382,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, 2) k_attend_rows(AttendArgs
     f16x8 qf[S32];
     float q_back;
     {
-        const int qh = head * a.group + (live ? row - tok * a.group : 0);
-        const int64_t at = (int64_t)(tile.first + tok) * a.q_token + (int64_t)qh * a.q_head;
-        i32x4 raw[S32];
         float top = 0.0f;
-#pragma unroll
-        for (int i = 0; i < S32; ++i) raw[i] = load8_raw(a.q, at + (i < 2 * C ? 64 * (i >> 1) + 16 * quarter + 8 * (i & 1) : 64 * C + 8 * quarter), a.q_wide);
 #pragma unroll
         for (int i = 0; i < S32; ++i) {
             if (!live) raw[i] = i32x4{0, 0, 0, 0};

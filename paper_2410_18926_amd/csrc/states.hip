@@ -118,7 +118,7 @@ Plan plan_of(const lorann_states* st, const lorann_questions* qs, int32_t found,
     } else {                           // tables cut
         p.unit = (int32_t)(ceil_div(ceil_div(table_keys, ceil_div(want, tables)), kKeysPerBlock) * kKeysPerBlock);
         p.units = (int32_t)ceil_div(table_keys, p.unit);
-        p.per_split = 1;
+        p.per_split = 1;               // (k_attend_rows counts on one unit per split where a sequence has one table)
         p.splits = (int32_t)(tables * p.units);
     }
     p.workspace = p.splits > 1 ? (int64_t)p.splits * rows * (st->dim + 2) * 4 : 0;

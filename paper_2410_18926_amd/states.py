@@ -85,8 +85,13 @@ class States:
         self.pages, self.heads, self.page_size, self.dim = n, h, p, d = k_codes.shape
         self._gpu = k_codes.device.index if k_codes.is_cuda else None
         steps = (n, h, p)
-        self._st = CStates(_array(k_codes, torch.int8, k_codes.shape, "k_codes"), _array(v_codes, torch.int8, (n, h, d, p), "v_codes"),
-                           _array(k_scales, torch.float32, steps, "k_scales"), _array(v_scales, torch.float32, steps, "v_scales"), n, h, p, d)
+        if not (k_codes.dtype is torch.int8 and v_codes.dtype is torch.int8 and k_scales.dtype is torch.float32 and v_scales.dtype is torch.float32
+                and v_codes.shape == (n, h, d, p) and k_scales.shape == steps and v_scales.shape == steps
+                and k_codes.is_contiguous() and v_codes.is_contiguous() and k_scales.is_contiguous() and v_scales.is_contiguous()):
+            for t, dtype, shape, what in ((k_codes, torch.int8, (n, h, p, d), "k_codes"), (v_codes, torch.int8, (n, h, d, p), "v_codes"),
+                                          (k_scales, torch.float32, steps, "k_scales"), (v_scales, torch.float32, steps, "v_scales")):
+                _array(t, dtype, shape, what)          # (says which)
+        self._st = CStates(k_codes.data_ptr(), v_codes.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(), n, h, p, d)
 
     @property
     def device(self):
