@@ -15,13 +15,13 @@ __device__ __forceinline__ void unrolled(F&& f) {
     }
 }
 
-// A block has NW * RT * 32 query rows of one head; a wavefront RT * 32 of them.  The block's threads convert each tile of 64 keys and values once to
+// A block has NW * 32 query rows of one head; a wavefront 32 of them.  The block's threads convert each tile of 64 keys and values once to
 // binary16 in LDS, in the order of the matrix operands (next tile's codes are in flight and are converted into the other buffer while this one
 // is used; one barrier per tile).  As in k_attend_rows the scores come out transposed, a lane holds scores of one row, and the weights
 // are the second product's operand as they stand.
-template <typename T, int D, int NW, int RT, bool WHOLE>
-__global__ void __launch_bounds__(64 * NW, RT == 1 ? 2 : 1) k_attend_tile(AttendArgs a) {
-    constexpr int C = D / 32, ROWS = NW * RT * 32, THREADS = 64 * NW;
+template <typename T, int D, int NW, bool WHOLE>
+__global__ void __launch_bounds__(64 * NW, 2) k_attend_tile(AttendArgs a) {
+    constexpr int C = D / 32, ROWS = NW * 32, THREADS = 64 * NW;
     constexpr int KS = D + 8, VS = kTileKeys + 8;               // row strides in LDS (16 bytes of padding: rows start in other banks)
     constexpr int PIECES = kTileKeys * D / 16;                  // 16-code pieces of the keys, and of the values
     constexpr int PER = (PIECES + THREADS - 1) / THREADS;
@@ -40,40 +40,37 @@ __global__ void __launch_bounds__(64 * NW, RT == 1 ? 2 : 1) k_attend_tile(Attend
     const int P = 1 << a.st.shift;
 
     // queries
-    int tok[RT], see_after[RT];
-    f16x8 qf[RT][2 * C];
-    float row_up[RT];                                           // of rows whose power of two is not the block's
+    int tok, see_after;
+    f16x8 qf[2 * C];
+    float row_up;                                               // of rows whose power of two is not the block's
     int e_block;
     bool mixed;
     {
-        i32x4 raw[RT][2 * C];
-        int e_row[RT];
+        i32x4 raw[2 * C];
+        int e_row;
         int e_max = -1000, e_min = 1000;
+        const int row = tile.row0 + wave * 32 + n;
+        const bool live = row < rows;
+        tok = live ? row / a.group : 0;
+        see_after = tile.count - 1 - tok;
+        const int qh = head * a.group + (live ? row - tok * a.group : 0);
+        const int64_t at = (int64_t)(tile.first + tok) * a.q_token + (int64_t)qh * a.q_head;
+        float top = 0.0f;
 #pragma unroll
-        for (int t = 0; t < RT; ++t) {
-            const int row = tile.row0 + (wave * RT + t) * 32 + n;
-            const bool live = row < rows;
-            tok[t] = live ? row / a.group : 0;
-            see_after[t] = tile.count - 1 - tok[t];
-            const int qh = head * a.group + (live ? row - tok[t] * a.group : 0);
-            const int64_t at = (int64_t)(tile.first + tok[t]) * a.q_token + (int64_t)qh * a.q_head;
-            float top = 0.0f;
+        for (int i = 0; i < 2 * C; ++i) {
+            float f[8];
+            raw[i] = load8_raw(a.q, at + 16 * i + 8 * half, a.q_wide);
+            if (!live) raw[i] = i32x4{0, 0, 0, 0};
+            widen8<T>(raw[i], f);
 #pragma unroll
-            for (int i = 0; i < 2 * C; ++i) {
-                float f[8];
-                raw[t][i] = load8_raw(a.q, at + 16 * i + 8 * half, a.q_wide);
-                if (!live) raw[t][i] = i32x4{0, 0, 0, 0};
-                widen8<T>(raw[t][i], f);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float m = fabsf(f[j]);
-                    if (m <= 3.4028235e38f) top = fmaxf(top, m);
-                }
+            for (int j = 0; j < 8; ++j) {
+                const float m = fabsf(f[j]);
+                if (m <= 3.4028235e38f) top = fmaxf(top, m);
             }
-            top = fmaxf(top, __shfl_xor(top, 32, 64));
-            e_row[t] = top < kTinyRow ? -1000 : (int)((__float_as_uint(top) >> 23) & 255) - 127;
-            if (e_row[t] > -1000) { e_max = max(e_max, e_row[t]); e_min = min(e_min, e_row[t]); }
         }
+        top = fmaxf(top, __shfl_xor(top, 32, 64));
+        e_row = top < kTinyRow ? -1000 : (int)((__float_as_uint(top) >> 23) & 255) - 127;
+        if (e_row > -1000) { e_max = max(e_max, e_row); e_min = min(e_min, e_row); }
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) { e_max = max(e_max, __shfl_xor(e_max, o, 64)); e_min = min(e_min, __shfl_xor(e_min, o, 64)); }
         if (lane == 0) lds_flag[wave] = (e_max + 1000) << 12 | (e_min + 1000);
@@ -85,33 +82,25 @@ __global__ void __launch_bounds__(64 * NW, RT == 1 ? 2 : 1) k_attend_tile(Attend
         e_min = __builtin_amdgcn_readfirstlane(e_min);
         e_block = e_max > -1000 ? e_max : 14;
         mixed = e_max - e_min > 12 && e_max > -1000;
+        const int e = mixed && e_row > -1000 ? e_row : e_block;
+        const float up = ldexpf(1.0f, 14 - e);
+        row_up = ldexpf(1.0f, e - e_block);
 #pragma unroll
-        for (int t = 0; t < RT; ++t) {
-            const int e = mixed && e_row[t] > -1000 ? e_row[t] : e_block;
-            const float up = ldexpf(1.0f, 14 - e);
-            row_up[t] = ldexpf(1.0f, e - e_block);
+        for (int i = 0; i < 2 * C; ++i) {
+            float f[8];
+            widen8<T>(raw[i], f);
 #pragma unroll
-            for (int i = 0; i < 2 * C; ++i) {
-                float f[8];
-                widen8<T>(raw[t][i], f);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) qf[t][i][j] = (_Float16)(f[j] * up);
-            }
+            for (int j = 0; j < 8; ++j) qf[i][j] = (_Float16)(f[j] * up);
         }
     }
     const float c = ldexpf(a.c, e_block - 14);
 
-    f32x16 acc[RT][C];
-    float M[RT], L[RT];
+    f32x16 acc[C];
+    float M = -INFINITY, L = 0.0f;
 #pragma unroll
-    for (int t = 0; t < RT; ++t) {
-        M[t] = -INFINITY;
-        L[t] = 0.0f;
+    for (int i = 0; i < C; ++i)
 #pragma unroll
-        for (int i = 0; i < C; ++i)
-#pragma unroll
-            for (int j = 0; j < 16; ++j) acc[t][i][j] = 0.0f;
-    }
+        for (int j = 0; j < 16; ++j) acc[i][j] = 0.0f;
 
     // Loading: the thread's pieces of the keys (a key, 16 of its values) and of the values (a component, 16 keys), and in one of three wavefronts in turn
     // the steps of a key per lane.  Page numbers are requested one tile before they are used: pages of 64 tokens and more (WHOLE) hold a tile in one
@@ -220,37 +209,31 @@ __global__ void __launch_bounds__(64 * NW, RT == 1 ? 2 : 1) k_attend_tile(Attend
     const int first_behind = tile.count - 1 - tile.row0 / a.group;
 
     // first product of a tile
-    auto scores = [&](int kb, f32x16 (&s)[RT][2]) {
+    auto scores = [&](int kb, f32x16 (&s)[2]) {
 #pragma unroll
-        for (int t = 0; t < RT; ++t)
+        for (int b = 0; b < 2; ++b)
 #pragma unroll
-            for (int b = 0; b < 2; ++b)
-#pragma unroll
-                for (int j = 0; j < 16; ++j) s[t][b][j] = 0.0f;
+            for (int j = 0; j < 16; ++j) s[b][j] = 0.0f;
 #pragma unroll
         for (int i = 0; i < 2 * C; ++i)
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
                 const f16x8 k = *(const f16x8*)&lds_k[kb][(32 * b + n) * KS + 16 * i + 8 * half];
-#pragma unroll
-                for (int t = 0; t < RT; ++t) s[t][b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, qf[t][i], s[t][b], 0, 0, 0);
+                s[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, qf[i], s[b], 0, 0, 0);
             }
     };
     // what a row does not see becomes -inf
-    auto hide = [&](const KeyTile& kt, f32x16 (&s)[RT][2]) -> bool {
+    auto hide = [&](const KeyTile& kt, f32x16 (&s)[2]) -> bool {
         if (a.ids || kt.k + kTileKeys <= kt.length - first_behind) return false;
+        const int see = kt.length - see_after - kt.k - 32 * half;
 #pragma unroll
-        for (int t = 0; t < RT; ++t) {
-            const int see = kt.length - see_after[t] - kt.k - 32 * half;
+        for (int b = 0; b < 2; ++b)
 #pragma unroll
-            for (int b = 0; b < 2; ++b)
-#pragma unroll
-                for (int j = 0; j < 16; ++j) s[t][b][j] = 16 * b + j < see ? s[t][b][j] : -INFINITY;
-        }
+            for (int j = 0; j < 16; ++j) s[b][j] = 16 * b + j < see ? s[b][j] : -INFINITY;
         return true;
     };
     // y of a tile from its products; what a row does not see is -inf
-    auto logits = [&](int vb, const KeyTile& kt, f32x16 (&s)[RT][2], bool mixed_now) {
+    auto logits = [&](int vb, const KeyTile& kt, f32x16 (&s)[2], bool mixed_now) {
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
@@ -258,12 +241,10 @@ __global__ void __launch_bounds__(64 * NW, RT == 1 ? 2 : 1) k_attend_tile(Attend
                 const int at = 32 * half + 16 * b + 4 * g;
                 const f32x4 sk = *(const f32x4*)&lds_step[vb][0][at], lv = *(const f32x4*)&lds_step[vb][1][at];
 #pragma unroll
-                for (int t = 0; t < RT; ++t)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const float x = mixed_now ? s[t][b][4 * g + j] * row_up[t] : s[t][b][4 * g + j];
-                        s[t][b][4 * g + j] = fmaf(x, sk[j], lv[j]);
-                    }
+                for (int j = 0; j < 4; ++j) {
+                    const float x = mixed_now ? s[b][4 * g + j] * row_up : s[b][4 * g + j];
+                    s[b][4 * g + j] = fmaf(x, sk[j], lv[j]);
+                }
             }
         hide(kt, s);
     };
@@ -276,45 +257,37 @@ __global__ void __launch_bounds__(64 * NW, RT == 1 ? 2 : 1) k_attend_tile(Attend
         return top;
     };
     // raises M where a row's largest score passes it by more than kSlack
-    auto raise = [&](const float (&tops)[RT]) {
+    auto raise = [&](float top) {
+        if (__ballot(top > M + kSlack)) {
+            top = fmaxf(top, __shfl_xor(top, 32, 64));
+            const float m_new = fmaxf(M, top), d = M - (m_new == -INFINITY ? 0.0f : m_new);
+            const float shrink = __builtin_amdgcn_exp2f(d);
+            L = times_exp2(L, d);
+            M = m_new;
 #pragma unroll
-        for (int t = 0; t < RT; ++t) {
-            float top = tops[t];
-            if (__ballot(top > M[t] + kSlack)) {
-                top = fmaxf(top, __shfl_xor(top, 32, 64));
-                const float m_new = fmaxf(M[t], top), d = M[t] - (m_new == -INFINITY ? 0.0f : m_new);
-                const float shrink = __builtin_amdgcn_exp2f(d);
-                L[t] = times_exp2(L[t], d);
-                M[t] = m_new;
+            for (int i = 0; i < C; ++i)
 #pragma unroll
-                for (int i = 0; i < C; ++i)
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) acc[t][i][j] *= shrink;
-            }
+                for (int j = 0; j < 16; ++j) acc[i][j] *= shrink;
         }
     };
     // the weights of a tile and their sum
-    auto weights = [&](int vb, const f32x16 (&y)[RT][2], f16x8 (&w)[RT][2][2], bool wild_now) {
-        float m_use[RT];
-#pragma unroll
-        for (int t = 0; t < RT; ++t) m_use[t] = M[t] == -INFINITY ? 0.0f : M[t];
+    auto weights = [&](int vb, const f32x16 (&y)[2], f16x8 (&w)[2][2], bool wild_now) {
+        const float m_use = M == -INFINITY ? 0.0f : M;
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
                 const f32x4 iv = *(const f32x4*)&lds_step[vb][2][32 * half + 16 * b + 4 * g];
 #pragma unroll
-                for (int t = 0; t < RT; ++t)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const float e = __builtin_amdgcn_exp2f(y[t][b][4 * g + j] - m_use[t]);
-                        L[t] = wild_now ? L[t] + sum_term(y[t][b][4 * g + j], m_use[t], iv[j]) : fmaf(e, iv[j], L[t]);
-                        w[t][b][g >> 1][4 * (g & 1) + j] = (_Float16)e;
-                    }
+                for (int j = 0; j < 4; ++j) {
+                    const float e = __builtin_amdgcn_exp2f(y[b][4 * g + j] - m_use);
+                    L = wild_now ? L + sum_term(y[b][4 * g + j], m_use, iv[j]) : fmaf(e, iv[j], L);
+                    w[b][g >> 1][4 * (g & 1) + j] = (_Float16)e;
+                }
             }
     };
     // second product
-    auto gather = [&](int kb, const f16x8 (&w)[RT][2][2]) {
+    auto gather = [&](int kb, const f16x8 (&w)[2][2]) {
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
@@ -322,8 +295,7 @@ __global__ void __launch_bounds__(64 * NW, RT == 1 ? 2 : 1) k_attend_tile(Attend
 #pragma unroll
                 for (int i = 0; i < C; ++i) {
                     const f16x8 v = *(const f16x8*)&lds_v[kb][(32 * i + n) * VS + 32 * half + 16 * b + 8 * j];
-#pragma unroll
-                    for (int t = 0; t < RT; ++t) acc[t][i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, w[t][b][j], acc[t][i], 0, 0, 0);
+                    acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, w[b][j], acc[i], 0, 0, 0);
                 }
     };
 
@@ -370,23 +342,19 @@ __global__ void __launch_bounds__(64 * NW, RT == 1 ? 2 : 1) k_attend_tile(Attend
         vb = vb == 2 ? 0 : vb + 1;
     };
     if (!mixed && d0.have) {
-        f32x16 y[RT][2];
+        f32x16 y[2];
         scores(0, y);
         logits(0, d0, y, false);
-        float top[RT];
-#pragma unroll
-        for (int t = 0; t < RT; ++t) top[t] = top_of(y[t]);
+        float top = top_of(y);
         raise(top);
         int wild_now = lds_wild[0];
         __syncthreads();
         while (d0.have && !__builtin_amdgcn_readfirstlane(wild_now)) {
             const int v1 = vb == 2 ? 0 : vb + 1, v2 = v1 == 2 ? 0 : v1 + 1;
-            f32x16 s[RT][2];
-            f16x8 w[RT][2][2];
+            f32x16 s[2];
+            f16x8 w[2][2];
             {
-                float m_use[RT];
-#pragma unroll
-                for (int t = 0; t < RT; ++t) m_use[t] = M[t] == -INFINITY ? 0.0f : M[t];
+                const float m_use = M == -INFINITY ? 0.0f : M;
                 __builtin_amdgcn_sched_barrier(0);
                 // operands are read from LDS two steps ahead of the products that use them
                 constexpr int STEPS = 4 * C;
@@ -408,26 +376,20 @@ __global__ void __launch_bounds__(64 * NW, RT == 1 ? 2 : 1) k_attend_tile(Attend
                     read_k(std::integral_constant<int, x + 2>{});
                     if constexpr (i == 0) {
 #pragma unroll
-                        for (int t = 0; t < RT; ++t)
-#pragma unroll
-                            for (int j = 0; j < 16; ++j) s[t][b][j] = 0.0f;
+                        for (int j = 0; j < 16; ++j) s[b][j] = 0.0f;
                     }
-#pragma unroll
-                    for (int t = 0; t < RT; ++t) s[t][b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k[x % 3], qf[t][i], s[t][b], 0, 0, 0);
+                    s[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k[x % 3], qf[i], s[b], 0, 0, 0);
                     unrolled<8 * i / (2 * C), 8 * (i + 1) / (2 * C)>([&](auto pc) {      // pairs of scores
                         constexpr int pr = decltype(pc)::value, g = 4 * b + pr / 2;
                         if constexpr (pr % 2 == 0) read_iv(std::integral_constant<int, g + 1>{});
 #pragma unroll
-                        for (int t = 0; t < RT; ++t)
-#pragma unroll
-                            for (int j = 2 * pr; j < 2 * pr + 2; ++j) {
-                                const float e = __builtin_amdgcn_exp2f(y[t][b][j] - m_use[t]);
-                                L[t] = fmaf(e, iv[g % 2][j % 4], L[t]);
-                                w[t][b][j / 8][j % 8] = (_Float16)e;
-                            }
+                        for (int j = 2 * pr; j < 2 * pr + 2; ++j) {
+                            const float e = __builtin_amdgcn_exp2f(y[b][j] - m_use);
+                            L = fmaf(e, iv[g % 2][j % 4], L);
+                            w[b][j / 8][j % 8] = (_Float16)e;
+                        }
                     });
-#pragma unroll
-                    for (int t = 0; t < RT; ++t) asm volatile("" : "+v"(L[t]));       // (the sum is formed here, not where it is next used)
+                    asm volatile("" : "+v"(L));       // (the sum is formed here, not where it is next used)
                     __builtin_amdgcn_sched_barrier(0);
                 });
             }
@@ -435,8 +397,7 @@ __global__ void __launch_bounds__(64 * NW, RT == 1 ? 2 : 1) k_attend_tile(Attend
             {
                 // (pieces and steps of a tile that is not there are converted all the same, into a buffer that nothing reads)
                 constexpr int STEPS = 4 * C, AHEAD = 2, FIRST = STEPS / 2;
-#pragma unroll
-                for (int t = 0; t < RT; ++t) top[t] = -INFINITY;
+                top = -INFINITY;
                 f16x8 v[AHEAD + 1];
                 f32x4 sk[2], lv[2];
                 auto read_v = [&](auto xc) {
@@ -455,8 +416,7 @@ __global__ void __launch_bounds__(64 * NW, RT == 1 ? 2 : 1) k_attend_tile(Attend
                     constexpr int x = decltype(xc)::value, bj = x / C, i = x % C;
                     read_v(std::integral_constant<int, x + AHEAD>{});
                     if constexpr (x == FIRST - 1) read_step(std::integral_constant<int, 0>{});
-#pragma unroll
-                    for (int t = 0; t < RT; ++t) acc[t][i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v[x % (AHEAD + 1)], w[t][bj >> 1][bj & 1], acc[t][i], 0, 0, 0);
+                    acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v[x % (AHEAD + 1)], w[bj >> 1][bj & 1], acc[i], 0, 0, 0);
                     // beside the products: first the conversions, then the scores of the next tile
                     if constexpr (x < FIRST) {
                         unrolled<2 * PER * x / FIRST, 2 * PER * (x + 1) / FIRST>([&](auto uc) {
@@ -468,14 +428,11 @@ __global__ void __launch_bounds__(64 * NW, RT == 1 ? 2 : 1) k_attend_tile(Attend
                             constexpr int z = decltype(bg)::value, b = z >> 2, g = z & 3;
                             read_step(std::integral_constant<int, z + 1>{});
 #pragma unroll
-                            for (int t = 0; t < RT; ++t)
-#pragma unroll
-                                for (int j = 0; j < 4; ++j) {
-                                    s[t][b][4 * g + j] = fmaf(s[t][b][4 * g + j], sk[z % 2][j], lv[z % 2][j]);
-                                    top[t] = fmaxf(top[t], s[t][b][4 * g + j]);
-                                }
-#pragma unroll
-                            for (int t = 0; t < RT; ++t) asm volatile("" : "+v"(top[t]));
+                            for (int j = 0; j < 4; ++j) {
+                                s[b][4 * g + j] = fmaf(s[b][4 * g + j], sk[z % 2][j], lv[z % 2][j]);
+                                top = fmaxf(top, s[b][4 * g + j]);
+                            }
+                            asm volatile("" : "+v"(top));
                         });
                     }
                     __builtin_amdgcn_sched_barrier(0);
@@ -483,15 +440,12 @@ __global__ void __launch_bounds__(64 * NW, RT == 1 ? 2 : 1) k_attend_tile(Attend
             }
             stage_steps(v2, d2);
             if (hide(d1, s)) {
-#pragma unroll
-                for (int t = 0; t < RT; ++t) top[t] = top_of(s[t]);
+                top = top_of(s);
             }
             advance();
             if (d0.have) raise(top);
 #pragma unroll
-            for (int t = 0; t < RT; ++t)
-#pragma unroll
-                for (int b = 0; b < 2; ++b) y[t][b] = s[t][b];
+            for (int b = 0; b < 2; ++b) y[b] = s[b];
             __syncthreads();
         }
     }
@@ -500,13 +454,11 @@ __global__ void __launch_bounds__(64 * NW, RT == 1 ? 2 : 1) k_attend_tile(Attend
     while (d0.have) {
         const int v1 = vb == 2 ? 0 : vb + 1, v2 = v1 == 2 ? 0 : v1 + 1;
         wild = wild || __builtin_amdgcn_readfirstlane(lds_wild[vb]);
-        f32x16 s[RT][2];
-        f16x8 w[RT][2][2];
+        f32x16 s[2];
+        f16x8 w[2][2];
         scores(kb, s);
         logits(vb, d0, s, true);
-        float top[RT];
-#pragma unroll
-        for (int t = 0; t < RT; ++t) top[t] = top_of(s[t]);
+        float top = top_of(s);
         raise(top);
         weights(vb, s, w, wild);
         gather(kb, w);
@@ -519,33 +471,30 @@ __global__ void __launch_bounds__(64 * NW, RT == 1 ? 2 : 1) k_attend_tile(Attend
     }
 
     const int heads = a.st.heads * a.group;
+    const float l = L + __shfl_xor(L, 32, 64);
+    const int row = tile.row0 + wave * 32 + n;
+    if (row >= rows) return;
+    const int64_t at_tok = tile.first + tok;
+    const int qh = head * a.group + row - tok * a.group;
+    if (a.splits == 1) {
+        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
 #pragma unroll
-    for (int t = 0; t < RT; ++t) {
-        const float l = L[t] + __shfl_xor(L[t], 32, 64);
-        const int row = tile.row0 + (wave * RT + t) * 32 + n;
-        if (row >= rows) continue;
-        const int64_t at_tok = tile.first + tok[t];
-        const int qh = head * a.group + row - tok[t] * a.group;
-        if (a.splits == 1) {
-            const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+        for (int i = 0; i < C; ++i)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const f32x4 o = {acc[i][4 * g] * inv, acc[i][4 * g + 1] * inv, acc[i][4 * g + 2] * inv, acc[i][4 * g + 3] * inv};
+                store4<T>(a.out, at_tok * a.out_token + (int64_t)qh * a.out_head + 32 * i + 8 * g + 4 * half, a.out_wide, o);
+            }
+    } else {
+        const int64_t at = ((int64_t)split * a.tokens + at_tok) * heads + qh;
+        if (l != 0.0f) {
 #pragma unroll
             for (int i = 0; i < C; ++i)
 #pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const f32x4 o = {acc[t][i][4 * g] * inv, acc[t][i][4 * g + 1] * inv, acc[t][i][4 * g + 2] * inv, acc[t][i][4 * g + 3] * inv};
-                    store4<T>(a.out, at_tok * a.out_token + (int64_t)qh * a.out_head + 32 * i + 8 * g + 4 * half, a.out_wide, o);
-                }
-        } else {
-            const int64_t at = ((int64_t)split * a.tokens + at_tok) * heads + qh;
-            if (l != 0.0f) {
-#pragma unroll
-                for (int i = 0; i < C; ++i)
-#pragma unroll
-                    for (int g = 0; g < 4; ++g)
-                        *(f32x4*)&a.part_acc[at * D + 32 * i + 8 * g + 4 * half] = f32x4{acc[t][i][4 * g], acc[t][i][4 * g + 1], acc[t][i][4 * g + 2], acc[t][i][4 * g + 3]};
-            }
-            if (half == 0) { a.part_m[at] = M[t]; a.part_l[at] = l; }
+                for (int g = 0; g < 4; ++g)
+                    *(f32x4*)&a.part_acc[at * D + 32 * i + 8 * g + 4 * half] = f32x4{acc[i][4 * g], acc[i][4 * g + 1], acc[i][4 * g + 2], acc[i][4 * g + 3]};
         }
+        if (half == 0) { a.part_m[at] = M; a.part_l[at] = l; }
     }
 }
 

@@ -84,6 +84,7 @@ struct Plan {
 constexpr int64_t kBlocksWanted = 512;
 constexpr int64_t kMostKeys = 16384, kMostTileKeys = 32768, kMostPartRows = 1 << 17;      // (and no more than that many rows of partial answers)
 constexpr int64_t kTileFromRows = 32;           // rows per sequence and head (tokens x group) from which k_attend_tile is taken
+constexpr int kDimForFour = 64;                 // up to this dimension its blocks have 4 wavefronts, whatever the rows
 constexpr int64_t kKeysPerBlock = 64 * kAttendWaves;
 
 int check_questions(const lorann_states* st, const lorann_questions* qs, int32_t found, int32_t width) {
@@ -105,7 +106,7 @@ Plan plan_of(const lorann_states* st, const lorann_questions* qs, int32_t found,
     const int64_t group = qs->heads / st->heads;
     const int64_t sequences = std::max<int64_t>(qs->sequences, 1), mean_rows = qs->tokens * group / sequences;
     auto tiles_of = [&](int64_t rows) { return qs->q_start ? qs->tokens * group / rows + sequences : sequences * ceil_div(mean_rows, rows); };
-    p.waves = mean_rows <= kTileFromRows ? 0 : tiles_of(256) * st->heads >= 512 && mean_rows >= 1024 && st->dim > 64 ? 8 : 4;
+    p.waves = mean_rows <= kTileFromRows ? 0 : tiles_of(256) * st->heads >= 512 && mean_rows >= 1024 && st->dim > kDimForFour ? 8 : 4;
     p.tiles = tiles_of(p.waves ? 32 * p.waves : kRows);
     const int64_t table_keys = std::max<int64_t>((int64_t)width * st->page_size, 1), tables = std::max(found, 1), keys = tables * table_keys;
     const int64_t blocks = std::max<int64_t>(p.tiles * st->heads, 1), rows = std::max<int64_t>(qs->tokens * qs->heads, 1);
@@ -123,6 +124,31 @@ Plan plan_of(const lorann_states* st, const lorann_questions* qs, int32_t found,
     }
     p.workspace = p.splits > 1 ? (int64_t)p.splits * rows * (st->dim + 2) * 4 : 0;
     return p;
+}
+
+// `grid`, `block`: of the first kernel.
+template <typename T, int D>
+void launch_attend(const Plan& p, const AttendArgs& a, dim3 grid, dim3 block, hipStream_t stream) {
+    const bool whole = a.st.shift >= 6;          // pages of 64 tokens and more: a tile of keys lies in one
+    if (p.waves == 8) {
+        if constexpr (D > kDimForFour) {
+            if (whole) hipLaunchKernelGGL((k_attend_tile<T, D, 8, true>), grid, block, 0, stream, a);
+            else hipLaunchKernelGGL((k_attend_tile<T, D, 8, false>), grid, block, 0, stream, a);
+        }
+    } else if (p.waves) {
+        if (whole) hipLaunchKernelGGL((k_attend_tile<T, D, 4, true>), grid, block, 0, stream, a);
+        else hipLaunchKernelGGL((k_attend_tile<T, D, 4, false>), grid, block, 0, stream, a);
+    } else {
+        if (whole) hipLaunchKernelGGL((k_attend_rows<T, D, true>), grid, block, 0, stream, a);
+        else hipLaunchKernelGGL((k_attend_rows<T, D, false>), grid, block, 0, stream, a);
+    }
+    if (p.splits > 1) {
+        constexpr int groups = 256 / (D / 4);
+        int sides = 1;
+        while (sides < p.splits && 2 * sides <= groups) sides *= 2;
+        const int64_t rows = a.tokens * a.st.heads * a.group;
+        hipLaunchKernelGGL((k_attend_join<T, D>), dim3((unsigned)ceil_div(rows, groups / sides)), dim3(256), 0, stream, a, sides);
+    }
 }
 
 int attend(const lorann_states* st, const lorann_questions* qs, const int64_t* ids, int32_t found, const float* scores, float score_weight,
@@ -162,24 +188,7 @@ int attend(const lorann_states* st, const lorann_questions* qs, const int64_t* i
     a.q_wide = aligned(qs->q, 16) && qs->q_token % 8 == 0 && qs->q_head % 8 == 0;
     a.out_wide = aligned(qs->out, 8) && qs->out_token % 4 == 0 && qs->out_head % 4 == 0;
     const dim3 grid((unsigned)blocks), block(64 * (p.waves ? p.waves : kAttendWaves));
-    const int join_groups = 256 / (st->dim / 4);
-    int sides = 1;
-    while (sides < p.splits && 2 * sides <= join_groups) sides *= 2;
-    const dim3 join((unsigned)ceil_div(rows, join_groups / sides));
-#define LAUNCH_TILE(T_, D_, NW_)                                                                    \
-    do {                                                                                            \
-        if (a.st.shift >= 6) hipLaunchKernelGGL((k_attend_tile<T_, D_, NW_, 1, true>), grid, block, 0, stream, a); \
-        else hipLaunchKernelGGL((k_attend_tile<T_, D_, NW_, 1, false>), grid, block, 0, stream, a); \
-    } while (0)
-#define LAUNCH(T_, D_)                                                                              \
-    do {                                                                                            \
-        if (p.waves == 8) LAUNCH_TILE(T_, D_, 8);                                                   \
-        else if (p.waves) LAUNCH_TILE(T_, D_, 4);                                                   \
-        else if (a.st.shift >= 6) hipLaunchKernelGGL((k_attend_rows<T_, D_, true>), grid, block, 0, stream, a); \
-        else hipLaunchKernelGGL((k_attend_rows<T_, D_, false>), grid, block, 0, stream, a);         \
-        if (p.splits > 1) hipLaunchKernelGGL((k_attend_join<T_, D_>), join, dim3(256), 0, stream, a, sides); \
-    } while (0)
-#define LAUNCH_DIM(D_) do { if (qs->type == LORANN_F16) LAUNCH(_Float16, D_); else LAUNCH(__bf16, D_); } while (0)
+#define LAUNCH_DIM(D_) do { if (qs->type == LORANN_F16) launch_attend<_Float16, D_>(p, a, grid, block, stream); else launch_attend<__bf16, D_>(p, a, grid, block, stream); } while (0)
     switch (st->dim) {
         case 32: LAUNCH_DIM(32); break;
         case 64: LAUNCH_DIM(64); break;
@@ -187,8 +196,6 @@ int attend(const lorann_states* st, const lorann_questions* qs, const int64_t* i
         default: LAUNCH_DIM(128); break;
     }
 #undef LAUNCH_DIM
-#undef LAUNCH
-#undef LAUNCH_TILE
     HIP_TRY(hipGetLastError());
     return LORANN_OK;
 }
