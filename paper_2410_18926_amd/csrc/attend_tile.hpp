@@ -35,7 +35,7 @@ __global__ void __launch_bounds__(64 * NW, 2) k_attend_tile(AttendArgs a) {
     const BlockWork work = block_work(a);
     const int head = work.head, split = work.split;
     RowTile tile;
-    if (!find_tile<ROWS>(a, work.tile, tile)) return;
+    if (!find_tile<ROWS, true>(a, work.tile, tile)) return;
     const int rows = tile.count * a.group;
     const int P = 1 << a.st.shift;
 
