@@ -3,10 +3,11 @@
 // For query q and key j with codes K_j, V_j and steps sk_j, sv_j, in units of log2:
 //   x_j = <q, K_j> (scale sk_j log2 e) + bias;   y_j = x_j + log2 sv_j;   M = max_j y_j (running);
 //   w_j = 2^(y_j - M);   out = (sum_j w_j V_j) / (sum_j w_j / sv_j).
-// The steps of the values are folded into the exponent, so the operand w of the second product lies in [0, 1] whatever the steps are and the codes stay
-// integers: both products are binary16 matrix products whose codes are exact, and the only rounding before the answer's is w's to 11 bits
-// (2^-12 relative per weight; the answer's own rounding to bfloat16 is 2^-9).  Queries become binary16 with a power of two per row, which
-// loses nothing of their 8 or 11 bits down to 2^-28 of the row's largest.
+// The steps of the values are folded into the exponent, so the operand w of the second product lies in [0, 2^kSlack] whatever the steps are and the codes
+// stay integers: both products are binary16 matrix products whose codes are exact (products of binary16 numbers added in float), and the only rounding before
+// the answer's is w's to 11 bits (2^-12 relative per weight; the answer's own rounding to bfloat16 is 2^-9).  Queries become binary16 with a power of two
+// per row, which loses nothing of their 8 or 11 bits down to 2^-28 of the row's largest.  Scores, M, the sum and the answer are floats throughout.
+// (bfloat16 products instead would round the weights to 8 bits, at the same rate.)
 #pragma once
 #include "states_store.hpp"
 
@@ -284,7 +285,10 @@ struct KeyTiles {
 // rounding), so the answer's registers are rarely rescaled.
 constexpr float kSlack = 6.0f;
 
-// Few query rows: bound by reading the states.  A block has up to 16 rows of one head and a range of keys; its wavefronts take tiles of 64 keys in turn,
+// Few query rows: bound by reading the states, 2 D + 8 bytes per key and head for up to 16 rows.  Measured: 64 tokens of 32 heads over 1638 to 8192 keys (8 heads of
+// 128, 705 MB) 140 us, 5.0 TB/s; one token of 64 heads over 131072 keys (8 heads of 128, 277 MB, 512 splits) 44 us + 4.5 us for the join; one token
+// over 4001 keys 8.4 + 3.1 us, of which the memory would take 2: two rounds of dependent loads (length and page, then codes) and two launches.
+// A block has up to 16 rows of one head and a range of keys; its wavefronts take tiles of 64 keys in turn,
 // codes straight from memory into registers in the order of the matrix operands (no LDS: the order of the contracted axis is free), and
 // their sums are joined in LDS at the end.  The first product is formed transposed (keys x rows), so a lane holds 16 scores of ONE row: statistics are
 // in-lane but for exchanges between the four quarters of the wavefront, and the weights are the second product's operand as they stand.
@@ -559,7 +563,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, 2) k_attend_rows(AttendArgs
     }
 }
 
-// Joins the splits of each row.  D / 4 threads hold a row's values; `sides` such groups share a row's splits (a power of two, as many as there are splits
+// Joins the splits of each row: out = (sum_s 2^(M_s - M) acc_s) / (sum_s 2^(M_s - M) l_s).  Bound by latency for one token (3 us with 16 to 512 splits).  D / 4 threads hold a row's values; `sides` such groups share a row's splits (a power of two, as many as there are splits
 // while the block has room), each with a running reference of its own, and the block's other groups take other rows.
 template <typename T, int D>
 __global__ void __launch_bounds__(256) k_attend_join(AttendArgs a, int sides) {

@@ -83,8 +83,14 @@ struct Plan {
 // long sequence among short ones does not run on a few CUs alone.
 constexpr int64_t kBlocksWanted = 512;
 constexpr int64_t kMostKeys = 16384, kMostTileKeys = 32768, kMostPartRows = 1 << 17;      // (and no more than that many rows of partial answers)
-constexpr int64_t kTileFromRows = 32;           // rows per sequence and head (tokens x group) from which k_attend_tile is taken
-constexpr int kDimForFour = 64;                 // up to this dimension its blocks have 4 wavefronts, whatever the rows
+// Rows per sequence and head (tokens x group) up to which k_attend_rows is taken, which reads the states once for every 16 rows.  32 sequences of 4096 keys, 8 heads
+// of 128, us of k_attend_rows / k_attend_tile: 16 rows 53 / 118, 32 rows 67 / 109, 48 rows 95 / 108, 64 rows 115 / 107, 128 rows 210 / 121.
+constexpr int64_t kMostFewRows = 48;
+// Blocks of k_attend_tile have 4 wavefronts, or 8 where they still fill the GPU and little of them is empty: then the codes are converted for 256 rows at once.
+// us of 4 / 8 wavefronts: 4096 tokens of 32 heads over 32768 keys 2550 / 2430, 16 x 256 tokens over 4352 keys 355 / 345; 8 heads of 96, 4096 tokens over 12288
+// keys 780 / 730; but one with 256 blocks, 2048 tokens over 16384 keys, 633 / 648; and up to a dimension of 64 either is faster by up to 4 %.
+constexpr int64_t kManyBlocks = 512, kManyRows = 1024;
+constexpr int kDimForFour = 64;
 constexpr int64_t kKeysPerBlock = 64 * kAttendWaves;
 
 int check_questions(const lorann_states* st, const lorann_questions* qs, int32_t found, int32_t width) {
@@ -106,7 +112,7 @@ Plan plan_of(const lorann_states* st, const lorann_questions* qs, int32_t found,
     const int64_t group = qs->heads / st->heads;
     const int64_t sequences = std::max<int64_t>(qs->sequences, 1), mean_rows = qs->tokens * group / sequences;
     auto tiles_of = [&](int64_t rows) { return qs->q_start ? qs->tokens * group / rows + sequences : sequences * ceil_div(mean_rows, rows); };
-    p.waves = mean_rows <= kTileFromRows ? 0 : tiles_of(256) * st->heads >= 512 && mean_rows >= 1024 && st->dim > kDimForFour ? 8 : 4;
+    p.waves = mean_rows <= kMostFewRows ? 0 : tiles_of(256) * st->heads >= kManyBlocks && mean_rows >= kManyRows && st->dim > kDimForFour ? 8 : 4;
     p.tiles = tiles_of(p.waves ? 32 * p.waves : kRows);
     const int64_t table_keys = std::max<int64_t>((int64_t)width * st->page_size, 1), tables = std::max(found, 1), keys = tables * table_keys;
     const int64_t blocks = std::max<int64_t>(p.tiles * st->heads, 1), rows = std::max<int64_t>(qs->tokens * qs->heads, 1);

@@ -245,6 +245,27 @@ def test_many_short_sequences(S):
     R.assert_close(st.attend_chunk(q, dev(tables), dev(lengths), q_start=dev(start)), want, tol)
 
 
+@pytest.mark.parametrize("n", [2, 63, 64, 65])
+@pytest.mark.parametrize("same", [False, True])
+def test_sequences_of_uneven_lengths(S, n, same):
+    """Rows enough for shared tiles of as many sequences as a wavefront has lanes, and one more: lengths in no order, several alike, some 0, some without queries."""
+    g = gen(n)
+    rng = np.random.default_rng(n)
+    page, group = 16, 4
+    new = np.full(n, 33) if same else rng.choice([0, 1, 20, 33, 70], n)
+    if not same:
+        new[:2] = 70
+    lengths = rng.choice([0, 5, 33, 90, 90, 200], n)
+    lengths[1] = 200
+    pages = int(sum(-(-l // page) for l in lengths)) + 1
+    st = filled(S, pages, 1, page, 32)
+    tables = make_tables(g, list(lengths), pages, page)
+    q = randn(g, int(new.sum()), group, 32).to(BF16)
+    start = np.concatenate([[0], np.cumsum(new)])
+    want, tol = R.chunk(st, q, tables, lengths, start, 0.2)
+    R.assert_close(st.attend_chunk(q, dev(tables), dev(lengths), scale=0.2, q_start=None if same else dev(start)), want, tol)
+
+
 PASSAGES = [
     # new tokens, found, stock lengths, heads, group, dim, page, type, weighted
     ([1], 1, [1], 1, 1, 32, 16, BF16, False),
