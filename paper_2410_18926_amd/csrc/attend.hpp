@@ -95,9 +95,9 @@ __device__ __forceinline__ bool find_tile(const AttendArgs& a, int x, RowTile& t
                 if (lane >= o) upto += w;
             }
         }
-        const unsigned long long here = __ballot(x - base >= upto - n && x - base < upto);
-        if (here) {
-            const int src = __ffsll((long long)here) - 1;
+        const unsigned long long mine = __ballot(x - base >= upto - n && x - base < upto);
+        if (mine) {
+            const int src = __ffsll((long long)mine) - 1;
             t.s = s0 + src;
             t.first = __builtin_amdgcn_readlane(first, src);         // (scalar, so that everything that follows from them is)
             t.count = __builtin_amdgcn_readlane(count, src);
