@@ -50,9 +50,9 @@ def build_sanitized() -> pathlib.Path:
     loading, workspace planning; device code is compiled as usual).  Load it with LORANN_LIB=<path> and clang's
     sanitizer runtime first in the process (sanitizer_runtime())."""
     hipcc = shutil.which("hipcc") or "/opt/rocm/bin/hipcc"
-    flags = [f for f in FLAGS if f != "-O3"] + ["-O1", "-g", "-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=undefined",
-                                                 "-Xarch_host", "-fno-sanitize-recover=all", "-Xarch_host", "-fno-omit-frame-pointer"]
-    _compile_and_link(hipcc, flags, SAN_LIB, link=[f for f in flags if "sanitize" in f or f == "-Xarch_host"])
+    checks = ["-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=undefined"]
+    flags = [f for f in FLAGS if f != "-O3"] + ["-O1", "-g", *checks, "-Xarch_host", "-fno-sanitize-recover=all", "-Xarch_host", "-fno-omit-frame-pointer"]
+    _compile_and_link(hipcc, flags, SAN_LIB, link=checks)
     return SAN_LIB
 
 
