@@ -100,8 +100,8 @@ typedef struct lorann_questions {
  *             Entries beyond a sequence's length are not used.  The keys of an entry outside [0, pages) are left out.
  *   lengths   [sequences] int32: tokens of the sequence in the store, the new ones included; taken within [0, width * page_size]
  * A query without a key (length 0, or more queries than tokens) answers with zeros.  A key whose states hold a NaN makes the answers of
- * those queries NaN that see it, and no others.  Products are exact sums of 8-bit codes and 16-bit queries in float; softmax statistics and
- * sums are float, the weights of the second product are rounded to 11 bits, the answer once to its type.
+ * those queries NaN that see it, and no others.  Products of 8-bit codes and 16-bit queries are exact, their sums float, as are the softmax statistics
+ * and sums; the weights of the second product are rounded to 11 bits (those below 2^-23 of the largest to a multiple of 2^-33 of it), the answer once to its type.
  *   workspace      lorann_attend_workspace() bytes of device memory, 16-byte aligned (NULL if that is 0); calls that may overlap need one each
  */
 int lorann_attend_chunk(const lorann_states *st, const lorann_questions *qs, const int32_t *tables, int32_t width, const int32_t *lengths,

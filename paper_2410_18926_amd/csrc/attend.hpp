@@ -5,9 +5,11 @@
 //   w_j = 2^(y_j - M);   out = (sum_j w_j V_j) / (sum_j w_j / sv_j).
 // The steps of the values are folded into the exponent, so the operand w of the second product lies in [0, 2^kSlack] whatever the steps are and the codes
 // stay integers: both products are binary16 matrix products whose codes are exact (products of binary16 numbers added in float), and the only rounding before
-// the answer's is w's to 11 bits (2^-12 relative per weight; the answer's own rounding to bfloat16 is 2^-9).  Queries become binary16 with a power of two
-// per row, which loses nothing of their 8 or 11 bits down to 2^-28 of the row's largest.  Scores, M, the sum and the answer are floats throughout.
-// (bfloat16 products instead would round the weights to 8 bits, at the same rate.)
+// the answer's is w's to 11 bits (at most 2^-11 relative per weight; the answer's own rounding to bfloat16 is at most 2^-8).  The operand is 2^kLift w, which fills
+// binary16's range to its top: weights keep their 11 bits down to 2^-23 of 2^M, and below that are off by at most 2^-34 of 2^M.  Queries become binary16
+// with a power of two per row (k_attend_tile: per block while its rows lie within 2^12 of each other), which loses nothing of their 8 or 11 bits down to 2^-28 (2^-16) of
+// the row's largest and 2^-39 (2^-27) of that below.  Scores, M, the sum and the answer are floats throughout.  (bfloat16 products instead would round the
+// weights to 8 bits, at the same rate.)
 #pragma once
 #include "states_store.hpp"
 
@@ -36,7 +38,7 @@ struct AttendArgs {
     float weight;                      // score_weight * log2 e
     int32_t unit, units;               // a table's keys are taken in `units` units of `unit` keys
     int32_t splits, per_split;         // units (over all passages of the sequence) per split
-    float *part_acc, *part_m, *part_l; // [splits][tokens * query heads][dim] (not written where part_l is 0), and [splits][tokens * query heads] (splits > 1)
+    float *part_acc, *part_m, *part_l; // [splits][tokens * query heads][dim] (2^kLift sum w V; not written where part_l is 0), and [splits][tokens * query heads] (splits > 1)
     bool q_wide, out_wide;             // rows are aligned to 16 / 8 bytes
 };
 
@@ -175,9 +177,14 @@ __device__ __forceinline__ void row_power(float top, float& to_half, float& back
 //   - A key that is not there has add = -inf: its weight is 0 in every row.
 //   - A step of 0 stands beside codes of 0, so any step may be taken in its place: 1.
 //   - A NaN step of the values acts through add alone: rows that do not see the key multiply `inverse` by 0.
-// While all steps of the values are within 2^+-45 ("tame"), a weight w of 2^-24 of the row's largest is still a normal float and w * inverse
+// While all steps of the values are within 2^+-45 ("tame"), a weight w of 2^-24 of the row's largest is still a normal float and (2^kLift w) * inverse
 // is the sum's term.  Beyond that the terms are computed by an exponential of their own (sum_term).
 constexpr float kTameLog2 = 45.0f;
+// The reference M of the weights is raised only when a score passes it by more than kSlack, so the answer's registers are rarely rescaled.  Weights stay below
+// 2^kSlack, and the operands 2^kLift w below 2^15, the last power of two but one that binary16 holds.  (Without the lift, weights below 2^-14 would lose bits and those
+// below 2^-25 become 0 in the numerator alone: an answer of one key 20 to 26 octaves above 2^19 others was up to 1.8 % off.)
+constexpr float kSlack = 6.0f, kLift = 9.0f;
+constexpr float kUnlift = 1.0f / 512;          // 2^-kLift
 struct KeySteps { float product, add, inverse; bool wild; };
 __device__ __forceinline__ KeySteps key_steps(float ks, float vs, float c, float bias, bool have) {
     vs = vs == 0.0f ? 1.0f : vs < 0x1p-120f ? 0x1p-120f : vs;
@@ -185,12 +192,15 @@ __device__ __forceinline__ KeySteps key_steps(float ks, float vs, float c, float
     KeySteps k;
     k.product = have ? ks * c : 0.0f;
     k.add = have ? lg + bias : -INFINITY;
-    k.inverse = have && vs == vs ? __builtin_amdgcn_rcpf(vs) : 1.0f;       // (1 ulp)
+    k.inverse = (have && vs == vs ? __builtin_amdgcn_rcpf(vs) : 1.0f) * kUnlift;       // (1 ulp)
     k.wild = have && fabsf(lg) > kTameLog2;
     return k;
 }
 
-// The sum's term of a key in units of 2^M, where steps span more than a float's exponent.
+// The reference of the operands: 2^(y - lifted(M)) = 2^kLift w.
+__device__ __forceinline__ float lifted(float m) { return m == -INFINITY ? 0.0f : m - kLift; }
+
+// The sum's term of a key in units of 2^M, where steps span more than a float's exponent.  m: the lifted reference.
 __device__ __forceinline__ float sum_term(float y, float m, float inverse) {
     return y == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(y - m + __log2f(inverse));
 }
@@ -280,10 +290,6 @@ struct KeyTiles {
         }
     }
 };
-
-// The reference M of the weights is raised only when a score passes it by more than kSlack (weights stay below 2^kSlack, which binary16 holds with the same relative
-// rounding), so the answer's registers are rarely rescaled.
-constexpr float kSlack = 6.0f;
 
 // Few query rows: bound by reading the states, 2 D + 8 bytes per key and head for up to 16 rows.  Measured: 64 tokens of 32 heads over 1638 to 8192 keys (8 heads of
 // 128, 705 MB) 140 us, 5.0 TB/s; one token of 64 heads over 131072 keys (8 heads of 128, 277 MB, 512 splits) 44 us + 4.5 us for the join; one token
@@ -489,12 +495,13 @@ __global__ void __launch_bounds__(64 * kAttendWaves, 2) k_attend_rows(AttendArgs
 #pragma unroll
             for (int i = 0; i < DT; ++i) acc[i] = acc[i] * shrink;
         }
-        const float m_use = M == -INFINITY ? 0.0f : M;
+        const float m_use = lifted(M);
+        float l = 0.0f;                                         // the tile's part of the sum: terms far below the sum so far would each be rounded away
         if (wild) {
 #pragma unroll
             for (int b = 0; b < 4; ++b)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) L += sum_term(s[b][j], m_use, lds_step[wave][2][16 * quarter + 4 * b + j]);
+                for (int j = 0; j < 4; ++j) l += sum_term(s[b][j], m_use, lds_step[wave][2][16 * quarter + 4 * b + j]);
         }
         f16x8 w[2];
 #pragma unroll
@@ -503,10 +510,11 @@ __global__ void __launch_bounds__(64 * kAttendWaves, 2) k_attend_rows(AttendArgs
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const float e = __builtin_amdgcn_exp2f(s[b][j] - m_use);
-                if (!wild) L = fmaf(e, iv[j], L);
+                if (!wild) l = fmaf(e, iv[j], l);
                 w[b >> 1][4 * (b & 1) + j] = (_Float16)e;
             }
         }
+        L += l;
         asm volatile("" : "+v"(L));                             // (the sum is formed here: kept for later, its terms would fill the registers)
 #pragma unroll
         for (int i = 0; i < DT; ++i) {
@@ -553,7 +561,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, 2) k_attend_rows(AttendArgs
         }
         const int t = tile.first + grow / a.group, hq = head * a.group + grow % a.group;
         if (a.splits == 1) {
-            const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+            const float inv = l == 0.0f ? 0.0f : kUnlift / l;
             store4<T>(a.out, (int64_t)t * a.out_token + (int64_t)hq * a.out_head + d, a.out_wide, o * inv);
         } else {
             const int64_t at = ((int64_t)split * a.tokens + t) * heads + hq;
@@ -563,7 +571,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, 2) k_attend_rows(AttendArgs
     }
 }
 
-// Joins the splits of each row: out = (sum_s 2^(M_s - M) acc_s) / (sum_s 2^(M_s - M) l_s).  Bound by latency for one token (3 us with 16 to 512 splits).  D / 4 threads hold a row's values; `sides` such groups share a row's splits (a power of two, as many as there are splits
+// Joins the splits of each row: out = (sum_s 2^(M_s - M) acc_s) / (sum_s 2^(M_s - M) l_s), acc lifted.  Bound by latency for one token (3 us with 16 to 512 splits).  D / 4 threads hold a row's values; `sides` such groups share a row's splits (a power of two, as many as there are splits
 // while the block has room), each with a running reference of its own, and the block's other groups take other rows.
 template <typename T, int D>
 __global__ void __launch_bounds__(256) k_attend_join(AttendArgs a, int sides) {
@@ -617,7 +625,7 @@ __global__ void __launch_bounds__(256) k_attend_join(AttendArgs a, int sides) {
         l += times_exp2(lds_l[group + i], dm);
         o += lds_o[group + i][d] * __builtin_amdgcn_exp2f(dm);
     }
-    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    const float inv = l == 0.0f ? 0.0f : kUnlift / l;
     store4<T>(a.out, t * a.out_token + (row - t * heads) * a.out_head + 4 * d, a.out_wide, o * inv);
 }
 

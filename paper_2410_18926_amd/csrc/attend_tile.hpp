@@ -280,7 +280,8 @@ __global__ void __launch_bounds__(64 * NW, 2) k_attend_tile(AttendArgs a) {
     };
     // the weights of a tile and their sum
     auto weights = [&](int vb, const f32x16 (&y)[2], f16x8 (&w)[2][2], bool wild_now) {
-        const float m_use = M == -INFINITY ? 0.0f : M;
+        const float m_use = lifted(M);
+        float l = 0.0f;                  // the tile's part of the sum: terms far below the sum so far would each be rounded away
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
@@ -289,10 +290,11 @@ __global__ void __launch_bounds__(64 * NW, 2) k_attend_tile(AttendArgs a) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const float e = __builtin_amdgcn_exp2f(y[b][4 * g + j] - m_use);
-                    L = wild_now ? L + sum_term(y[b][4 * g + j], m_use, iv[j]) : fmaf(e, iv[j], L);
+                    l = wild_now ? l + sum_term(y[b][4 * g + j], m_use, iv[j]) : fmaf(e, iv[j], l);
                     w[b][g >> 1][4 * (g & 1) + j] = (_Float16)e;
                 }
             }
+        L += l;
     };
     // second product
     auto gather = [&](int kb, const f16x8 (&w)[2][2]) {
@@ -362,7 +364,8 @@ __global__ void __launch_bounds__(64 * NW, 2) k_attend_tile(AttendArgs a) {
             f32x16 s[2];
             f16x8 w[2][2];
             {
-                const float m_use = M == -INFINITY ? 0.0f : M;
+                const float m_use = lifted(M);
+                float l = 0.0f;          // (as in weights)
                 __builtin_amdgcn_sched_barrier(0);
                 // operands are read from LDS two steps ahead of the products that use them
                 constexpr int STEPS = 4 * C;
@@ -393,13 +396,14 @@ __global__ void __launch_bounds__(64 * NW, 2) k_attend_tile(AttendArgs a) {
 #pragma unroll
                         for (int j = 2 * pr; j < 2 * pr + 2; ++j) {
                             const float e = __builtin_amdgcn_exp2f(y[b][j] - m_use);
-                            L = fmaf(e, iv[g % 2][j % 4], L);
+                            l = fmaf(e, iv[g % 2][j % 4], l);
                             w[b][j / 8][j % 8] = (_Float16)e;
                         }
                     });
-                    asm volatile("" : "+v"(L));       // (the sum is formed here, not where it is next used)
+                    asm volatile("" : "+v"(l));       // (the sum is formed here, not where it is next used)
                     __builtin_amdgcn_sched_barrier(0);
                 });
+                L += l;
             }
             wild_now = lds_wild[v1];
             {
@@ -485,7 +489,7 @@ __global__ void __launch_bounds__(64 * NW, 2) k_attend_tile(AttendArgs a) {
     const int64_t at_tok = tile.first + tok;
     const int qh = head * a.group + row - tok * a.group;
     if (a.splits == 1) {
-        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+        const float inv = l == 0.0f ? 0.0f : kUnlift / l;
 #pragma unroll
         for (int i = 0; i < C; ++i)
 #pragma unroll
