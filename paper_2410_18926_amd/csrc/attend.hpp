@@ -175,11 +175,13 @@ __device__ __forceinline__ void row_power(float top, float& to_half, float& back
 
 // What a key's steps become: y = product * <q, K> + add, and the sum's term w * inverse.
 //   - A key that is not there has add = -inf: its weight is 0 in every row.
-//   - A step of 0 stands beside codes of 0, so any step may be taken in its place: 1.
+//   - A step of 0 stands beside codes of 0: any step may be taken in its place.  The key counts in the sum and adds nothing to the numerator, so the step
+//     is one, kNoStep, with which its y hardly ever raises M (the weights of the other keys would be rounded where binary16 has few bits or none: with a step of
+//     1, one zero row with a logit of 10 among values of 0.01 put answers off by 20 times their rounding and more).  Keys of step s keep their 11 bits up to a logit of log2(s) + 107 octaves below its.
 //   - A NaN step of the values acts through add alone: rows that do not see the key multiply `inverse` by 0.
-// While all steps of the values are within 2^+-45 ("tame"), a weight w of 2^-24 of the row's largest is still a normal float and (2^kLift w) * inverse
-// is the sum's term.  Beyond that the terms are computed by an exponential of their own (sum_term).
-constexpr float kTameLog2 = 45.0f;
+// While all steps of the values are within 2^-45 .. 2^10 ("tame") or 0, the operand 2^kLift w of a key whose share of the sum is 2^-40 of the largest is still a normal
+// float, whatever the two keys' steps are, and operand * inverse is the sum's term.  Beyond that the terms are computed by an exponential of their own (sum_term).
+constexpr float kTameLow = 0x1p-45f, kTameHigh = 0x1p10f, kNoStep = 0x1p-84f;
 // The reference M of the weights is raised only when a score passes it by more than kSlack, so the answer's registers are rarely rescaled.  Weights stay below
 // 2^kSlack, and the operands 2^kLift w below 2^15, the last power of two but one that binary16 holds.  (Without the lift, weights below 2^-14 would lose bits and those
 // below 2^-25 become 0 in the numerator alone: an answer of one key 20 to 26 octaves above 2^19 others was up to 1.8 % off.)
@@ -187,13 +189,14 @@ constexpr float kSlack = 6.0f, kLift = 9.0f;
 constexpr float kUnlift = 1.0f / 512;          // 2^-kLift
 struct KeySteps { float product, add, inverse; bool wild; };
 __device__ __forceinline__ KeySteps key_steps(float ks, float vs, float c, float bias, bool have) {
-    vs = vs == 0.0f ? 1.0f : vs < 0x1p-120f ? 0x1p-120f : vs;
+    const bool wild = vs != 0.0f && (vs < kTameLow || vs > kTameHigh);
+    vs = vs == 0.0f ? kNoStep : vs < 0x1p-120f ? 0x1p-120f : vs;
     const float lg = __log2f(vs);
     KeySteps k;
     k.product = have ? ks * c : 0.0f;
     k.add = have ? lg + bias : -INFINITY;
     k.inverse = (have && vs == vs ? __builtin_amdgcn_rcpf(vs) : 1.0f) * kUnlift;       // (1 ulp)
-    k.wild = have && fabsf(lg) > kTameLog2;
+    k.wild = have && wild;
     return k;
 }
 

@@ -55,3 +55,116 @@ def test_very_many_small_weights(S, new, group, place):
     tol = 2.0 ** -11 + 2.0 ** -11 + n * 2.0 ** -34 + (2 * n / 16 + n / 64 + 64) * 2.0 ** -24
     off = (got.double() - 1).abs().amax((0, 2))
     assert (off <= tol).all(), f"off by {off.tolist()} where {tol} is allowed, {octaves.tolist()} octaves"
+
+
+# ---- keys whose values are all zero ----
+
+def with_zero_values(S, g, lengths, heads, page, dim, size, gap, scale, zero):
+    """(store, tables, direction [heads, dim]): values of about `size`; the tokens `zero(length)` of each sequence have none at all, and a logit of about `gap` for queries
+    along the direction, where the others' spread by about 1."""
+    width = -(-max(lengths) // page)
+    st = S.States.empty(len(lengths) * width, heads, page, dim)
+    tables = torch.randperm(len(lengths) * width, generator=g, device="cuda").to(torch.int32).view(len(lengths), width)
+    along = randn(g, heads, dim)
+    for s, n in enumerate(lengths):
+        k, v = randn(g, n, heads, dim) / (scale * dim ** 0.5), size * randn(g, n, heads, dim)
+        for z in zero(n):
+            k[z] = gap / scale * along / (along * along).sum(-1, keepdim=True)
+            v[z] = 0
+        t = torch.arange(n, device="cuda")
+        st.write(k, v, tables[s, t // page].long() * page + t % page)
+    return st, tables, along
+
+
+def queries(g, along, tokens, group, dtype):
+    heads, dim = along.shape
+    return (along[None, :, None] + 0.05 * randn(g, tokens, heads, group, dim)).reshape(tokens, heads * group, dim).to(dtype)
+
+
+ZERO_CHUNKS = [
+    # new tokens of each sequence, lengths, heads, group, dim, page, type
+    (1, [256], 2, 2, 128, 64, BF16),
+    (1, [300, 40], 1, 4, 64, 16, F16),
+    (1, [3000], 1, 2, 32, 32, F16),                  # cut, and joined
+    (70, [256, 133], 1, 2, 128, 64, F16),            # shared tiles
+    (50, [200], 1, 3, 64, 16, BF16),
+    (60, [1500], 1, 1, 96, 128, F16),                # shared tiles, cut, and joined
+]
+
+
+@pytest.mark.parametrize("new,lengths,heads,group,dim,page,dtype", ZERO_CHUNKS)
+@pytest.mark.parametrize("size,gap", [(0.1, 10.0), (0.01, 0.0), (0.01, 6.0), (0.01, 10.0), (1e-3, 6.0), (1e-5, 0.0)])
+@pytest.mark.parametrize("place", ["first", "middle", "many"])
+def test_keys_without_values(S, new, lengths, heads, group, dim, page, dtype, size, gap, place):
+    """A key whose values are all zero takes its share of the weights and changes nothing else, however much it weighs and however small the other values are."""
+    if dtype == F16 and size < 1e-2:
+        dtype = BF16                                 # (answers that binary16 would hold with few bits)
+    zero = {"first": lambda n: [0], "middle": lambda n: [n // 2 - 5], "many": lambda n: list(range(3, n - 8, 9))}[place]
+    g = gen(1000 * new + dim + int(gap))
+    scale = dim ** -0.5
+    st, tables, along = with_zero_values(S, g, lengths, heads, page, dim, size, gap, scale, zero)
+    q = queries(g, along, new * len(lengths), group, dtype)
+    want, tol = R.chunk(st, q, tables.cpu().numpy(), lengths, [i * new for i in range(len(lengths) + 1)], scale)
+    if dtype == F16:
+        tol = tol + 2.0 ** -25                       # half the distance of binary16's numbers below 2^-14
+    R.assert_close(st.attend_chunk(q, tables, dev(lengths), scale=scale), want, tol)
+
+
+@pytest.mark.parametrize("new,dim,page", [(1, 128, 64), (60, 64, 16)])
+@pytest.mark.parametrize("size,gap", [(0.01, 10.0), (1e-4, 3.0)])
+def test_passages_with_padding_in_the_store(S, new, dim, page, size, gap):
+    """Passages whose last tokens were written as zeros (padding), one that is nothing else, and tokens of the store that were never written."""
+    g = gen(7 + new)
+    scale, lengths = dim ** -0.5, [100, 64, 30, 250]
+    st, tables, along = with_zero_values(S, g, lengths, 1, page, dim, size, gap, scale, lambda n: range(n) if n == 30 else range(n - n // 4, n))
+    blank = torch.arange(-(-50 // page), device="cuda").to(torch.int32) + st.pages          # pages at the end of a larger store, never written
+    big = S.States.empty(st.pages + len(blank), 1, page, dim)
+    for name in ("k_codes", "v_codes", "k_scales", "v_scales"):
+        getattr(big, name)[:st.pages] = getattr(st, name)
+    wide = torch.zeros((5, max(tables.shape[1], len(blank))), dtype=torch.int32, device="cuda")
+    wide[:4, :tables.shape[1]] = tables
+    wide[4, :len(blank)] = blank
+    lengths = lengths + [50]
+    ids = np.array([[0, 4, 2], [3, 1, -1]])
+    scores = np.array([[0.5, 0.1, 0.0], [0.2, 0.3, 0.0]], np.float32)
+    q = queries(g, along, 2 * new, 4, BF16)
+    want, tol = R.passages(big, q, ids, wide.cpu().numpy(), lengths, [0, new, 2 * new], scores, -1.5, scale)
+    got = big.attend_passages(q, dev(ids, torch.int64), wide, dev(lengths), scores=dev(scores, torch.float32), score_weight=-1.5, scale=scale)
+    R.assert_close(got, want, tol)
+
+
+@pytest.mark.parametrize("new", [1, 80])
+@pytest.mark.parametrize("size", [1e-8, 1e-14, 1e-20, 1e-28])
+def test_keys_without_values_among_the_smallest(S, new, size):
+    """The same where the other values are far below what models have: the first tiles hold keys without values alone, or tame values, the later ones tiny values."""
+    g = gen(21)
+    scale, dim, n = 0.125, 64, 700
+    for head in ("zeros", "tame"):
+        st = S.States.empty(-(-n // 16), 1, 16, dim)
+        k, v = randn(g, n, 1, dim), size * randn(g, n, 1, dim)
+        v[:130] = 0
+        if head == "tame":
+            v[20:60], k[20:60] = 1e-6 * randn(g, 40, 1, dim), 0.01 * k[20:60]
+        v[300:310] = 0
+        st.write(k, v, torch.arange(n, device="cuda"))
+        q = randn(g, new, 2, dim).to(BF16)
+        tables = torch.arange(st.pages, dtype=torch.int32, device="cuda")[None]
+        want, tol = R.chunk(st, q, tables.cpu().numpy(), [n], [0, new], scale)
+        R.assert_close(st.attend_chunk(q, tables, dev([n]), scale=scale), want, tol, head)
+
+
+@pytest.mark.parametrize("new", [1, 100])
+def test_nothing_but_zero_values(S, new):
+    """An answer of zeros from 40000 keys without values; with one value among them, its share."""
+    n, dim = 40_000, 32
+    st = S.States.empty(n // 64, 1, 64, dim)
+    tables = torch.arange(st.pages, dtype=torch.int32, device="cuda")[None]
+    q = randn(gen(5), new, 2, dim).to(BF16)
+    assert (st.attend_chunk(q, tables, dev([n])) == 0).all()
+    one = torch.full((1, 1, dim), 3.0, device="cuda")
+    st.write(0 * one, one, torch.tensor([n - 500], device="cuda"))
+    want = 3.0 / (n - new + 1 + torch.arange(new, dtype=torch.float64, device="cuda"))           # (every logit is 0)
+    got = st.attend_chunk(q, tables, dev([n])).double()
+    # the answer's rounding, and sums of 40000 terms in float of which each adds the same: at most n 2^-24 relative
+    tol = (2.0 ** -8 + n * 2.0 ** -24) * want
+    assert ((got - want[:, None, None]).abs() <= tol[:, None, None]).all()
