@@ -9,8 +9,8 @@
  *   lorann_attend_passages   attention over the states of the passages found for each sequence: takes the ids as lorann_search leaves them
  *
  * Conventions shared by the entry points
- *   - Every pointer inside the structures and every array argument is device memory of the current HIP device; the structures themselves
- *     are host memory.  The library keeps no caller pointer and no state between calls: the store's memory and the workspace are the caller's.
+ *   - Every pointer inside the structures and every array argument is device memory of the current HIP device (host memory and that of another
+ *     GPU are refused); the structures themselves are host memory.  The library keeps no caller pointer and no state between calls: the store's memory and the workspace are the caller's.
  *   - Work is enqueued on `hip_stream` (a hipStream_t; NULL: the null stream) and the call returns.  Nothing is allocated, copied to the host
  *     or waited for, so a call can be captured into a HIP graph.  Calls that write and read the same slots are ordered by the caller
  *     (one stream, or events).

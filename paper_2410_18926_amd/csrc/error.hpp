@@ -8,7 +8,8 @@ namespace lorann {
 
 // Stores the message for lorann_last_error() and returns `code`.
 __attribute__((visibility("hidden"), format(printf, 2, 3))) int fail(int code, const char* fmt, ...);
-__attribute__((visibility("hidden"))) bool is_device_ptr(const void* p);
+// Device memory (or managed memory, which every GPU reaches); `gpu`: the GPU that it is on, -1 for managed memory.
+__attribute__((visibility("hidden"))) bool is_device_ptr(const void* p, int* gpu = nullptr);
 
 #define HIP_TRY(expr)                                                                                      \
     do {                                                                                                   \

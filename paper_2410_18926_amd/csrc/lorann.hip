@@ -54,13 +54,14 @@ int lorann::fail(int code, const char* fmt, ...) {
     return code;
 }
 
-bool lorann::is_device_ptr(const void* p) {
+bool lorann::is_device_ptr(const void* p, int* gpu) {
     hipPointerAttribute_t at;
     hipError_t e = hipPointerGetAttributes(&at, p);
     if (e != hipSuccess) {
         (void)hipGetLastError();   // plain host memory: clear the sticky error
         return false;
     }
+    if (gpu) *gpu = at.type == hipMemoryTypeManaged ? -1 : at.device;
     return at.type == hipMemoryTypeDevice || at.type == hipMemoryTypeManaged;
 }
 

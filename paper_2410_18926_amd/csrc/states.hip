@@ -31,20 +31,24 @@ int check_sizes(const lorann_states* st) {
     return LORANN_OK;
 }
 
-int check_device(const void* p, const char* name) {
+// `current`: the current device, -1 until the first pointer asks for it (a call checks up to twelve).
+int check_device(const void* p, const char* name, int& current) {
     if (!p) return fail(LORANN_E_INVAL, "%s is NULL", name);
-    if (!is_device_ptr(p)) return fail(LORANN_E_INVAL, "%s is not a device pointer", name);
+    int gpu = -1;
+    if (!is_device_ptr(p, &gpu)) return fail(LORANN_E_INVAL, "%s is not a device pointer", name);
+    if (current < 0) HIP_TRY(hipGetDevice(&current));
+    if (gpu >= 0 && gpu != current) return fail(LORANN_E_INVAL, "%s is memory of GPU %d, the current device is %d", name, gpu, current);
     return LORANN_OK;
 }
 
-int check_store(const lorann_states* st) {
+int check_store(const lorann_states* st, int& gpu) {
     int rc;
     if ((rc = check_sizes(st))) return rc;
     if (!st->k_codes || !st->v_codes || !st->k_scales || !st->v_scales) return fail(LORANN_E_INVAL, "an array of the store is NULL");
     if (!aligned(st->k_codes, 16) || !aligned(st->v_codes, 16)) return fail(LORANN_E_INVAL, "the store's codes are not 16-byte aligned");
     if (!aligned(st->k_scales, 4) || !aligned(st->v_scales, 4)) return fail(LORANN_E_INVAL, "the store's steps are not 4-byte aligned");
-    if ((rc = check_device(st->k_codes, "k_codes")) || (rc = check_device(st->v_codes, "v_codes"))) return rc;
-    if ((rc = check_device(st->k_scales, "k_scales")) || (rc = check_device(st->v_scales, "v_scales"))) return rc;
+    if ((rc = check_device(st->k_codes, "k_codes", gpu)) || (rc = check_device(st->v_codes, "v_codes", gpu))) return rc;
+    if ((rc = check_device(st->k_scales, "k_scales", gpu)) || (rc = check_device(st->v_scales, "v_scales", gpu))) return rc;
     return LORANN_OK;
 }
 
@@ -158,15 +162,15 @@ void launch_attend(const Plan& p, const AttendArgs& a, dim3 grid, dim3 block, hi
 }
 
 int attend(const lorann_states* st, const lorann_questions* qs, const int64_t* ids, int32_t found, const float* scores, float score_weight,
-           const int32_t* tables, int32_t width, const int32_t* lengths, int64_t passages, void* workspace, int64_t workspace_bytes, hipStream_t stream) {
+           const int32_t* tables, int32_t width, const int32_t* lengths, int64_t passages, void* workspace, int64_t workspace_bytes, hipStream_t stream, int& gpu) {
     int rc;
     if (qs->tokens == 0 || qs->sequences == 0) return LORANN_OK;
-    if ((rc = check_store(st))) return rc;
+    if ((rc = check_store(st, gpu))) return rc;
     if (!qs->q_start && qs->tokens % qs->sequences) return fail(LORANN_E_INVAL, "%lld tokens do not divide over %lld sequences", (long long)qs->tokens, (long long)qs->sequences);
-    if ((rc = check_device(qs->q, "q")) || (rc = check_device(qs->out, "out"))) return rc;
+    if ((rc = check_device(qs->q, "q", gpu)) || (rc = check_device(qs->out, "out", gpu))) return rc;
     if (!aligned(qs->q, 2) || !aligned(qs->out, 2)) return fail(LORANN_E_INVAL, "q or out is not aligned to its type");
-    if (qs->q_start && (rc = check_device(qs->q_start, "q_start"))) return rc;
-    if (width > 0 && (!ids || passages > 0) && (!ids || found > 0) && ((rc = check_device(tables, "tables")) || (rc = check_device(lengths, "lengths")))) return rc;
+    if (qs->q_start && (rc = check_device(qs->q_start, "q_start", gpu))) return rc;
+    if (width > 0 && (!ids || passages > 0) && (!ids || found > 0) && ((rc = check_device(tables, "tables", gpu)) || (rc = check_device(lengths, "lengths", gpu)))) return rc;
     const Plan p = plan_of(st, qs, found, width);
     const int64_t blocks = p.tiles * st->heads * p.splits;
     if (p.tiles > 0x7fffffff || blocks > 0xffffffffLL / (64 * std::max(p.waves, kAttendWaves)))       // (threads of a grid)
@@ -174,7 +178,7 @@ int attend(const lorann_states* st, const lorann_questions* qs, const int64_t* i
     if (p.workspace) {
         if (!workspace || workspace_bytes < p.workspace) return fail(LORANN_E_INVAL, "the workspace holds %lld bytes, %lld are needed", (long long)(workspace ? workspace_bytes : 0), (long long)p.workspace);
         if (!aligned(workspace, 16)) return fail(LORANN_E_INVAL, "the workspace is not 16-byte aligned");
-        if ((rc = check_device(workspace, "workspace"))) return rc;
+        if ((rc = check_device(workspace, "workspace", gpu))) return rc;
     }
     AttendArgs a{};
     a.st = view(st);
@@ -212,11 +216,11 @@ extern "C" {
 
 int lorann_states_write(const lorann_states* st, const void* k, const void* v, int32_t type, int64_t tokens,
                         int64_t k_token, int64_t k_head, int64_t v_token, int64_t v_head, const int64_t* slots, void* hip_stream) {
-    int rc;
+    int rc, gpu = -1;
     if ((rc = check_sizes(st)) || (rc = check_tokens(st, type, tokens))) return rc;
     if (tokens == 0) return LORANN_OK;
-    if ((rc = check_store(st))) return rc;
-    if ((rc = check_device(k, "k")) || (rc = check_device(v, "v")) || (rc = check_device(slots, "slots"))) return rc;
+    if ((rc = check_store(st, gpu))) return rc;
+    if ((rc = check_device(k, "k", gpu)) || (rc = check_device(v, "v", gpu)) || (rc = check_device(slots, "slots", gpu))) return rc;
     if (!aligned(k, element_size(type)) || !aligned(v, element_size(type))) return fail(LORANN_E_INVAL, "k or v is not aligned to its type");
     const dim3 grid((unsigned)ceil_div(tokens, kBlockTokens), (unsigned)st->heads, 2);
     const TokenRows kr = rows_of(const_cast<void*>(k), k_token, k_head, type), vr = rows_of(const_cast<void*>(v), v_token, v_head, type);
@@ -230,12 +234,12 @@ int lorann_states_write(const lorann_states* st, const void* k, const void* v, i
 
 int lorann_states_read(const lorann_states* st, const int64_t* slots, int64_t tokens, void* k, void* v, int32_t type,
                        int64_t k_token, int64_t k_head, int64_t v_token, int64_t v_head, void* hip_stream) {
-    int rc;
+    int rc, gpu = -1;
     if ((rc = check_sizes(st)) || (rc = check_tokens(st, type, tokens))) return rc;
     if (tokens == 0 || (!k && !v)) return LORANN_OK;
-    if ((rc = check_store(st))) return rc;
-    if ((rc = check_device(slots, "slots"))) return rc;
-    if ((k && (rc = check_device(k, "k"))) || (v && (rc = check_device(v, "v")))) return rc;
+    if ((rc = check_store(st, gpu))) return rc;
+    if ((rc = check_device(slots, "slots", gpu))) return rc;
+    if ((k && (rc = check_device(k, "k", gpu))) || (v && (rc = check_device(v, "v", gpu)))) return rc;
     if (!aligned(k, element_size(type)) || !aligned(v, element_size(type))) return fail(LORANN_E_INVAL, "k or v is not aligned to its type");
     const dim3 grid((unsigned)ceil_div(tokens, kBlockTokens), (unsigned)st->heads, 2);
     const TokenRows kr = rows_of(k, k_token, k_head, type), vr = rows_of(v, v_token, v_head, type);
@@ -256,24 +260,24 @@ int64_t lorann_attend_workspace(const lorann_states* st, const lorann_questions*
 
 int lorann_attend_chunk(const lorann_states* st, const lorann_questions* qs, const int32_t* tables, int32_t width, const int32_t* lengths,
                         void* workspace, int64_t workspace_bytes, void* hip_stream) {
-    int rc;
+    int rc, gpu = -1;
     if ((rc = check_sizes(st)) || (rc = check_questions(st, qs, 0, width))) return rc;
-    return attend(st, qs, nullptr, 0, nullptr, 0.0f, tables, width, lengths, 0, workspace, workspace_bytes, (hipStream_t)hip_stream);
+    return attend(st, qs, nullptr, 0, nullptr, 0.0f, tables, width, lengths, 0, workspace, workspace_bytes, (hipStream_t)hip_stream, gpu);
 }
 
 int lorann_attend_passages(const lorann_states* st, const lorann_questions* qs, const int64_t* ids, int32_t found, const float* scores,
                            float score_weight, const int32_t* tables, int32_t width, const int32_t* lengths, int64_t passages,
                            void* workspace, int64_t workspace_bytes, void* hip_stream) {
-    int rc;
+    int rc, gpu = -1;
     if ((rc = check_sizes(st)) || (rc = check_questions(st, qs, found, width))) return rc;
     if (passages < 0) return fail(LORANN_E_INVAL, "%lld passages", (long long)passages);
     if (passages > 0x7fffffff) return fail(LORANN_E_UNSUPPORTED, "%lld passages are more than 32 bits count", (long long)passages);
     if (!(std::fabs(score_weight) <= 1.0e38f)) return fail(LORANN_E_INVAL, "the weight of the scores is not finite");
     if (found < 1) return fail(LORANN_E_INVAL, "%d passages per sequence", found);
     if (qs->tokens > 0 && qs->sequences > 0) {
-        if ((rc = check_device(ids, "ids")) || (scores && (rc = check_device(scores, "scores")))) return rc;
+        if ((rc = check_device(ids, "ids", gpu)) || (scores && (rc = check_device(scores, "scores", gpu)))) return rc;
     }
-    return attend(st, qs, ids, found, scores, score_weight, tables, width, lengths, passages, workspace, workspace_bytes, (hipStream_t)hip_stream);
+    return attend(st, qs, ids, found, scores, score_weight, tables, width, lengths, passages, workspace, workspace_bytes, (hipStream_t)hip_stream, gpu);
 }
 
 }  // extern "C"
