@@ -14,6 +14,7 @@
  *   - Work is enqueued on `hip_stream` (a hipStream_t; NULL: the null stream) and the call returns.  Nothing is allocated, copied to the host
  *     or waited for, so a call can be captured into a HIP graph.  Calls that write and read the same slots are ordered by the caller
  *     (one stream, or events).
+ *   - There are no gradients: the store holds rounded codes, and nothing here keeps what a backward pass would need.
  *   - Return value: LORANN_OK or a negative error code of lorann.h, with the message in lorann_last_error(); on error nothing is enqueued.
  *   - Page numbers, slots, ids, lengths and offsets in device memory are checked on the device against the sizes that the call names: what
  *     lies outside is left out, as stated at each, and never read or written through.

@@ -2,6 +2,9 @@
 
 Tensors live on the GPU and are handed over as pointers with their strides; nothing is copied or converted here, a tensor of another type or
 layout than asked for is refused.  Work is enqueued on torch's current stream of the current device and the calls return.
+
+There are no gradients: the store holds rounded codes.  An answer to queries (or scores) that require one can be used forwards, a backward pass that
+reaches it raises; what is written into the store is cut off from its graph, as a cast to integers is.
 """
 from __future__ import annotations
 
@@ -69,6 +72,19 @@ def _strides(x, what):
     if value != 1 and x.shape[2] > 1:
         raise ValueError(f"{what}: the values of a row must be consecutive")
     return token, head
+
+
+class _NoGradient(torch.autograd.Function):
+    """The answer as it is, in a graph that ends here with an error instead of leaving the inputs' gradients out."""
+
+    @staticmethod
+    def forward(ctx, out, *inputs):
+        ctx.mark_dirty(out)
+        return out
+
+    @staticmethod
+    def backward(ctx, grad):
+        raise NotImplementedError("attention over the state store has no gradient (the store holds rounded codes): detach its inputs, or call it under torch.no_grad()")
 
 
 class States:
@@ -192,7 +208,7 @@ class States:
                                        ws, size, self._stream())
         if rc:
             _raise(rc)
-        return out
+        return _NoGradient.apply(out, q) if q.requires_grad and torch.is_grad_enabled() else out
 
     def attend_passages(self, q, ids, tables, lengths, q_start=None, scores=None, score_weight=1.0, scale=None, out=None, workspace=None):
         """The queries of each sequence attend to all tokens of the passages found for it.
@@ -210,4 +226,6 @@ class States:
                                           ws, size, self._stream())
         if rc:
             _raise(rc)
+        if (q.requires_grad or (scores is not None and scores.requires_grad)) and torch.is_grad_enabled():
+            return _NoGradient.apply(out, q, scores)
         return out
