@@ -27,6 +27,9 @@ class PageAllocator:
         taken, self.free = self.free[:n], self.free[n:]
         return taken
 
+    def give_back(self, pages: list):
+        self.free = self.free + pages
+
 
 class Reader:
     """A decoder of one layer over a store of passages: self-attention, cross-attention to the found passages, both with `group` query heads to a head of
@@ -42,7 +45,7 @@ class Reader:
         self.heads, self.group, self.dim, self.page_size, self.dtype, self.device = heads, group, dim, page_size, dtype, device
         need = [-(-len(p) // page_size) for p in passages]
         self.states = States.empty(sum(need) + own_pages, heads, page_size, dim, device)
-        self.pages = PageAllocator(self.states.pages)
+        self.pages, self.taken = PageAllocator(self.states.pages), []
         # the passages' states: written once, found by number afterwards
         tables = torch.zeros(len(passages), max(need), dtype=torch.int32)
         for i, n in enumerate(need):
@@ -55,10 +58,14 @@ class Reader:
         self.states.write(kv[:, :heads], kv[:, heads:], slots.to(device))
 
     def start(self, conversations: int, tokens: int):
-        """Pages for conversations of up to `tokens` tokens each."""
+        """Pages for conversations of up to `tokens` tokens each.  Those of the conversations before are given back (what reads them has been enqueued on the
+        same stream): step() goes on with the new ones."""
+        self.pages.give_back(self.taken)
+        self.taken, self.past, self.most = [], 0, 0
         width = -(-tokens // self.page_size)
-        self.own = torch.tensor([self.pages.take(width) for _ in range(conversations)], dtype=torch.int32, device=self.device)
-        self.past, self.most = 0, tokens
+        self.taken = self.pages.take(conversations * width)
+        self.own = torch.tensor(self.taken, dtype=torch.int32).view(conversations, width).to(self.device)
+        self.most = tokens
 
     def step(self, hidden, ids, dists):
         """Hidden states [conversations, new tokens, width] of the newest tokens -> the same after the layer.  ids, dists [conversations, found] as the
