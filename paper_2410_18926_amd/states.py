@@ -178,6 +178,8 @@ class States:
 
     def _workspace(self, qs, found, width, workspace):
         if workspace is not None:
+            if not workspace.is_contiguous():          # (its size would not be the memory it has)
+                raise ValueError("workspace must be contiguous")
             return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
         need = lib().lorann_attend_workspace(self._st, qs, found, width)
         if need < 0:
