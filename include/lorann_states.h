@@ -114,7 +114,7 @@ int lorann_attend_chunk(const lorann_states *st, const lorann_questions *qs, con
  *   ids       [sequences][found] int64: passage numbers, as lorann_search returns them for a corpus whose row ids are passage numbers; a number
  *             outside [0, passages) (the search's -1 among them) is left out, a number that stands twice counts twice
  *   scores    [sequences][found] float, or NULL (no term).  With the search's distances and a negative score_weight a nearer passage weighs
- *             more.  A passage whose term is -inf is left out.
+ *             more: only the terms' differences from the largest count, so they may be large.  A passage whose term is -inf is left out.
  *   tables    [passages][width] int32, lengths [passages] int32: pages and tokens of each passage, with the meaning above
  * No passages, or none with tokens: the answer is zeros.
  */

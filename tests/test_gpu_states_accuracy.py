@@ -168,3 +168,34 @@ def test_nothing_but_zero_values(S, new):
     # the answer's rounding, and sums of 40000 terms in float of which each adds the same: at most n 2^-24 relative
     tol = (2.0 ** -8 + n * 2.0 ** -24) * want
     assert ((got - want[:, None, None]).abs() <= tol[:, None, None]).all()
+
+
+# ---- terms of the passages that are large against their differences ----
+
+@pytest.mark.parametrize("new", [1, 50])
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("level,weight", [(1e5, -1.0), (3e6, -0.25), (-2e5, 3.0)])
+def test_large_scores_with_small_differences(S, new, dtype, level, weight):
+    """Distances of 10^5 that differ by a few: only their differences count.  Tolerance: as in states_reference for the differences from the largest term (the scores'
+    own differences are exact in 64 bits and within 2^-24 in float)."""
+    g, rng = gen(91), np.random.default_rng(17)
+    heads, group, dim, page, lengths = 2, 4, 64, 16, [130, 64, 300, 17, 1, 90]
+    width = -(-max(lengths) // page)
+    st = S.States.empty(len(lengths) * width, heads, page, dim)
+    n = st.pages * page
+    st.write(randn(g, n, heads, dim), randn(g, n, heads, dim), torch.arange(n, device="cuda"))
+    tables = np.arange(len(lengths) * width, dtype=np.int32).reshape(len(lengths), width)
+    found = 40
+    ids = rng.integers(0, len(lengths), (2, found))
+    ids[0, 5], ids[1, 30] = -1, 100
+    scores = (level + rng.choice([0.0, 0.5, 1.0, 1.75, 3.0], (2, found))).astype(np.float32)
+    scores[0, 5] = np.float32(-10 * level)                       # (of no passage)
+    if level > 0:
+        scores[1, 7] = np.inf                                    # left out
+    q = randn(g, 2 * new, heads * group, dim).to(dtype)
+    live = np.where((ids >= 0) & (ids < len(lengths)), weight * scores.astype(np.float64), -np.inf)
+    differences = np.maximum(live - live.max(1, keepdims=True), -1e30) / weight          # what is left when the largest term is taken off: the same softmax
+    differences = np.where(np.isneginf(live), -np.sign(weight) * np.inf, differences)
+    want, tol = R.passages(st, q, ids, tables, lengths, [0, new, 2 * new], differences, weight, 0.125)
+    args = dict(scores=dev(scores, torch.float32), score_weight=weight, scale=0.125)
+    R.assert_close(st.attend_passages(q, dev(ids, torch.int64), dev(tables), dev(lengths), **args), want, tol)
