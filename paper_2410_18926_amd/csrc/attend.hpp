@@ -44,7 +44,7 @@ struct AttendArgs {
 
 // Which head, split and row tile a block has.  Consecutive blocks, which go to different dies (each with an L2 and a share of the memory bandwidth of its own), are the heads
 // and then the splits of one row tile: one long sequence among short ones is read by all of them.  (With the row tiles consecutive, a token after 131072 keys
-// beside 63 after 1000 took 808 us, all of it on one die; 156 us so.)
+// beside 63 after 1000, 64 heads on 8 of 128, takes 1028 us, all of it on one die; 200 us so.)
 struct BlockWork { int head, split, tile; };
 __device__ __forceinline__ BlockWork block_work(const AttendArgs& a) {
     const int rest = blockIdx.x / a.st.heads, tile = rest / a.splits;
@@ -60,7 +60,7 @@ struct RowTile {
 
 // Tile `x` of the sequences' row tiles.  With q_start the tiles are counted by every wavefront, 64 sequences at a time.  false: none left.
 // LONGEST: up to 64 sequences that read their own tables come in the order of their lengths instead of their own, so that what runs last is short
-// (12 sequences of 128 to 500 new tokens and 1000 to 3500 keys, 16 heads of 64: 126 us in their own order, 104 so).
+// (12 sequences of 128 to 500 new tokens and 1000 to 3500 keys, 16 heads of 64: 124 us in their own order, 104 so).
 template <int ROWS, bool LONGEST>
 __device__ __forceinline__ bool find_tile(const AttendArgs& a, int x, RowTile& t) {
     const int each = (int)(a.tokens / a.sequences);

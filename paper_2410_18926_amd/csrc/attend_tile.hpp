@@ -1,11 +1,12 @@
 // Attention of many query rows (a chunk of new tokens, questions over passages).  Mathematics in attend.hpp.
 //
-// What bounds it: per 64 keys and 32 rows a wavefront issues D / 4 matrix instructions of 32 cycles (D = 128: 1024 cycles) and some 260 vector instructions
-// (per score: y, half a maximum, y - M, the exponential at a quarter of the rate, the sum, half a conversion; then the codes' conversion), some 1460 cycles,
-// and the two overlap little: 2750 cycles measured for a wavefront's tile at D = 128, 2190 at D = 64.  The clock falls to 1.9 - 2.0 GHz meanwhile.
-// Measured: 4096 tokens of 32 heads after 28672 (8 heads of 128) 2.25 ms, 0.9 PFLOP/s; 12 sequences of up to 500 tokens after up to 3000 (16 heads of 64)
-// 104 us, 0.32 PFLOP/s of a CU's longest pair of blocks; 24 questions of up to 96 tokens over 10 passages of up to 512 keys 165 us, 0.45 PFLOP/s
-// (456 blocks that have rows for 256 CUs, a fifth of their rows empty).
+// What bounds it: per 64 keys and 32 rows a wavefront issues D / 4 matrix instructions of 32 cycles (D = 128: 1024 cycles) and 240 to 310 vector instructions
+// of 4, its 32 exponentials of 8 (per score: y, half a maximum, y - M, the exponential, the sum, half a conversion; then the codes' conversion).  Counted at D = 128: 1224 cycles of
+// vector instructions with 8 wavefronts, 1505 with 4; at D = 64 with pages of 16: 1394.  The two overlap little: where blocks are many and alike, a wavefront's tile
+// takes 2471 cycles of its SIMD at D = 128, half of them with a vector instruction, 41 % with a matrix instruction.  The clock falls to 2.0 - 2.2 GHz meanwhile.
+// Measured: 4096 tokens of 32 heads after 28672 (8 heads of 128) 2.2 ms, 0.93 PFLOP/s; 12 sequences of up to 500 tokens after up to 3000 (16 heads of 64)
+// 90 - 102 us, a tile's SIMD time 3009 cycles (blocks of unequal length: some SIMDs have nothing left); 24 questions of up to 96 tokens over 10 passages of up to 512 keys 142 - 166 us,
+// 3958 cycles (448 blocks that have rows for 256 CUs, a fifth of their rows empty).
 #pragma once
 #include "attend.hpp"
 

@@ -82,17 +82,21 @@ struct Plan {
     int64_t workspace;
 };
 
-// Splitting.  Two blocks of either kernel fit a CU: 512 fill the GPU, more only add to what is joined (a token after 131071 keys: 53 us with 512, 59 with
-// 1024, 68 with 1536).  The host does not know the lengths, only the tables' width: where that is long, a block still gets at most so many keys, so that one
-// long sequence among short ones does not run on a few CUs alone.
+// Splitting.  Two blocks of either kernel fit a CU: 512 fill the GPU, more only add to what is joined (a token of 64 heads after 131071 keys: 50 us with 256 or 512, 54
+// with 1024, 62 with 1536).  The host does not know the lengths, only the tables' width: where that is long, a block still gets at most so many keys, so that one long sequence
+// among short ones does not run on a few CUs alone.  One token each of 64 sequences, one of 131072 keys, the others of 1000: 169 / 178 / 289 us with at most 8192 / 16384 / 32768
+// keys a block, 1012 uncut; 300 tokens each of 4 sequences, one of 131072 keys: 1116 / 1114 / 1633 with 16384 / 32768 / 65536, 3205 uncut.
 constexpr int64_t kBlocksWanted = 512;
 constexpr int64_t kMostKeys = 16384, kMostTileKeys = 32768, kMostPartRows = 1 << 17;      // (and no more than that many rows of partial answers)
 // Rows per sequence and head (tokens x group) up to which k_attend_rows is taken, which reads the states once for every 16 rows.  32 sequences of 4096 keys, 8 heads
-// of 128, us of k_attend_rows / k_attend_tile: 16 rows 53 / 118, 32 rows 67 / 109, 48 rows 95 / 108, 64 rows 115 / 107, 128 rows 210 / 121.
+// of 128, us of k_attend_rows / k_attend_tile: 16 rows 50 / 97, 32 rows 58 / 94, 48 rows 83 / 99, 64 rows 105 / 100, 128 rows 198 / 118.
+// The rows are the call's mean, one kernel takes all its sequences, and the figures are of sequences alike.  Pieces of prompts beside single tokens may do better in calls of
+// their own: 200 single tokens and a piece of 512, each over 2000 keys, 227 us together, 157 + 60 apart; 63 and 1024: 174, 44 + 83; 255 and 2048: 497, 189 + 153.
 constexpr int64_t kMostFewRows = 48;
 // Blocks of k_attend_tile have 4 wavefronts, or 8 where they still fill the GPU and little of them is empty: then the codes are converted for 256 rows at once.
-// us of 4 / 8 wavefronts: 4096 tokens of 32 heads over 32768 keys 2550 / 2430, 16 x 256 tokens over 4352 keys 355 / 345; 8 heads of 96, 4096 tokens over 12288
-// keys 780 / 730; but one with 256 blocks, 2048 tokens over 16384 keys, 633 / 648; and up to a dimension of 64 either is faster by up to 4 %.
+// us of 4 / 8 wavefronts: 4096 tokens of 32 heads over 32768 keys 2336 / 2161, 16 x 256 tokens over 4352 keys 344 / 324; 8 heads of 96, 4096 tokens over 12288
+// keys 724 / 679; with 256 blocks only, 2048 tokens over 16384 keys, 610 / 595; at a dimension of 64, 4096 tokens over 16384 keys 769 / 729, but 16 x 512 over 2048
+// 234 / 236 and 12 x 512 over 3500 with pages of 16 171 / 194.
 constexpr int64_t kManyBlocks = 512, kManyRows = 1024;
 constexpr int kDimForFour = 64;
 constexpr int64_t kKeysPerBlock = 64 * kAttendWaves;
