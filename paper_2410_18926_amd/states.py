@@ -87,6 +87,14 @@ class _NoGradient(torch.autograd.Function):
         raise NotImplementedError("attention over the state store has no gradient (the store holds rounded codes): detach its inputs, or call it under torch.no_grad()")
 
 
+def _no_gradient(out, *inputs):
+    if not torch.is_grad_enabled():
+        return out
+    if out.grad_fn is not None and out.grad_fn.name() == "_NoGradientBackward":       # (a buffer used again: one such end is enough, a chain would grow with every call)
+        return out
+    return _NoGradient.apply(out, *inputs)
+
+
 class States:
     """Keys and values of tokens in 8 bits with one step per token and head, in pages.
 
@@ -210,7 +218,7 @@ class States:
                                        ws, size, self._stream())
         if rc:
             _raise(rc)
-        return _NoGradient.apply(out, q) if q.requires_grad and torch.is_grad_enabled() else out
+        return _no_gradient(out, q) if q.requires_grad else out
 
     def attend_passages(self, q, ids, tables, lengths, q_start=None, scores=None, score_weight=1.0, scale=None, out=None, workspace=None):
         """The queries of each sequence attend to all tokens of the passages found for it.
@@ -228,6 +236,4 @@ class States:
                                           ws, size, self._stream())
         if rc:
             _raise(rc)
-        if (q.requires_grad or (scores is not None and scores.requires_grad)) and torch.is_grad_enabled():
-            return _NoGradient.apply(out, q, scores)
-        return out
+        return _no_gradient(out, q, scores) if q.requires_grad or (scores is not None and scores.requires_grad) else out

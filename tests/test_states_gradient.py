@@ -49,3 +49,14 @@ def test_forward_use_is_left_alone(attend):
             assert not call(queries(device, True)).requires_grad
         out = torch.empty((1, 4, 64), dtype=torch.bfloat16, device=device)
         assert call(queries(device, False), out=out) is out
+
+
+def test_a_buffer_used_again_grows_no_chain(attend):
+    device, calls = attend
+    for call in calls:
+        out = torch.empty((1, 4, 64), dtype=torch.bfloat16, device=device)
+        for _ in range(5):
+            y = call(queries(device, True), out=out)
+            assert y is out and all(f is None or f.name().endswith("AccumulateGrad") for f, _ in y.grad_fn.next_functions)
+        with pytest.raises(NotImplementedError, match="no gradient"):
+            y.float().sum().backward()
