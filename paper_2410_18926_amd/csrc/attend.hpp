@@ -184,7 +184,7 @@ __device__ __forceinline__ void row_power(float top, float& to_half, float& back
 constexpr float kTameLow = 0x1p-45f, kTameHigh = 0x1p10f, kNoStep = 0x1p-84f;
 // The reference M of the weights is raised only when a score passes it by more than kSlack, so the answer's registers are rarely rescaled.  Weights stay below
 // 2^kSlack, and the operands 2^kLift w below 2^15, the last power of two but one that binary16 holds.  (Without the lift, weights below 2^-14 would lose bits and those
-// below 2^-25 become 0 in the numerator alone: an answer of one key 20 to 26 octaves above 2^19 others was up to 1.8 % off.)
+// below 2^-25 become 0 in the numerator alone: an answer of one key 20 to 26 octaves above 2^19 others was up to 1.8 % off.)  The kernels hold M - kLift, called M there.
 constexpr float kSlack = 6.0f, kLift = 9.0f;
 constexpr float kUnlift = 1.0f / 512;          // 2^-kLift
 struct KeySteps { float product, add, inverse; bool wild; };
@@ -200,10 +200,7 @@ __device__ __forceinline__ KeySteps key_steps(float ks, float vs, float c, float
     return k;
 }
 
-// The reference of the operands: 2^(y - lifted(M)) = 2^kLift w.
-__device__ __forceinline__ float lifted(float m) { return m == -INFINITY ? 0.0f : m - kLift; }
-
-// The sum's term of a key in units of 2^M, where steps span more than a float's exponent.  m: the lifted reference.
+// The sum's term of a key in units of the weights', where steps span more than a float's exponent.  m: the operands' reference (M - kLift in the formulas).
 __device__ __forceinline__ float sum_term(float y, float m, float inverse) {
     return y == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(y - m + __log2f(inverse));
 }
@@ -520,17 +517,17 @@ __global__ void __launch_bounds__(64 * kAttendWaves, 2) k_attend_rows(AttendArgs
         for (int b = 0; b < 4; ++b)
 #pragma unroll
             for (int j = 0; j < 4; ++j) top = fmaxf(top, s[b][j]);
-        if (__ballot(top > M + kSlack)) {
+        if (__ballot(top > M + (kSlack + kLift))) {
             top = fmaxf(top, __shfl_xor(top, 32, 64));
             top = fmaxf(top, __shfl_xor(top, 16, 64));
-            const float m_new = fmaxf(M, top), d = M - (m_new == -INFINITY ? 0.0f : m_new);
+            const float m_new = fmaxf(M, top - kLift), d = M - (m_new == -INFINITY ? 0.0f : m_new);
             const float shrink = __builtin_amdgcn_exp2f(d);
             L = times_exp2(L, d);
             M = m_new;
 #pragma unroll
             for (int i = 0; i < DT; ++i) acc[i] = acc[i] * shrink;
         }
-        const float m_use = lifted(M);
+        const float m_use = M == -INFINITY ? 0.0f : M;
         float l = 0.0f;                                         // the tile's part of the sum: terms far below the sum so far would each be rounded away
         if (wild) {
 #pragma unroll

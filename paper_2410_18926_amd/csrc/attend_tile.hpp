@@ -265,11 +265,11 @@ __global__ void __launch_bounds__(64 * NW, 2) k_attend_tile(AttendArgs a) {
             for (int j = 0; j < 16; ++j) top = fmaxf(top, s[b][j]);
         return top;
     };
-    // raises M where a row's largest score passes it by more than kSlack
+    // raises the reference where a row's largest score passes it by more than kSlack (M is kLift below it)
     auto raise = [&](float top) {
-        if (__ballot(top > M + kSlack)) {
+        if (__ballot(top > M + (kSlack + kLift))) {
             top = fmaxf(top, __shfl_xor(top, 32, 64));
-            const float m_new = fmaxf(M, top), d = M - (m_new == -INFINITY ? 0.0f : m_new);
+            const float m_new = fmaxf(M, top - kLift), d = M - (m_new == -INFINITY ? 0.0f : m_new);
             const float shrink = __builtin_amdgcn_exp2f(d);
             L = times_exp2(L, d);
             M = m_new;
@@ -281,7 +281,7 @@ __global__ void __launch_bounds__(64 * NW, 2) k_attend_tile(AttendArgs a) {
     };
     // the weights of a tile and their sum
     auto weights = [&](int vb, const f32x16 (&y)[2], f16x8 (&w)[2][2], bool wild_now) {
-        const float m_use = lifted(M);
+        const float m_use = M == -INFINITY ? 0.0f : M;
         float l = 0.0f;                  // the tile's part of the sum: terms far below the sum so far would each be rounded away
 #pragma unroll
         for (int b = 0; b < 2; ++b)
@@ -365,8 +365,8 @@ __global__ void __launch_bounds__(64 * NW, 2) k_attend_tile(AttendArgs a) {
             f32x16 s[2];
             f16x8 w[2][2];
             {
-                const float m_use = lifted(M);
-                float l = 0.0f;          // (as in weights)
+                const float m_use = M == -INFINITY ? 0.0f : M;
+                float l = 0.0f;          // (as in weights; the first term needs no addition)
                 __builtin_amdgcn_sched_barrier(0);
                 // operands are read from LDS two steps ahead of the products that use them
                 constexpr int STEPS = 4 * C;
@@ -397,7 +397,7 @@ __global__ void __launch_bounds__(64 * NW, 2) k_attend_tile(AttendArgs a) {
 #pragma unroll
                         for (int j = 2 * pr; j < 2 * pr + 2; ++j) {
                             const float e = __builtin_amdgcn_exp2f(y[b][j] - m_use);
-                            l = fmaf(e, iv[g % 2][j % 4], l);
+                            l = b == 0 && j == 0 ? e * iv[g % 2][j % 4] : fmaf(e, iv[g % 2][j % 4], l);
                             w[b][j / 8][j % 8] = (_Float16)e;
                         }
                     });
