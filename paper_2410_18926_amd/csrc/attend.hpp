@@ -11,7 +11,7 @@
 // the row's largest and 2^-39 (2^-27) of that below.  Scores, M, the sum and the answer are floats throughout.  (bfloat16 products instead would round the
 // weights to 8 bits, at the same rate.)
 #pragma once
-#include "states_store.hpp"
+#include "codes4.hpp"
 
 namespace lorann {
 
@@ -332,14 +332,20 @@ struct KeyTiles {
 // in-lane but for exchanges between the four quarters of the wavefront, and the weights are the second product's operand as they stand.
 // The next tile's keys are requested as soon as the first product has used this one's, its values after the second product, its page number one tile
 // earlier: a wavefront always has 8 to 16 KiB in flight.  WHOLE: pages of 64 tokens and more, a tile lies in one.
-template <typename T, int D, bool WHOLE>
+// BITS 4: a lane's piece of a key row has the 8 codes of each step (at 128 values, 32 consecutive ones: 16 bytes as well), a 16-byte piece of the values has two components; the
+// factors of a tile's keys and values go through LDS beside the steps.
+template <typename T, int D, bool WHOLE, int BITS>
 __global__ void __launch_bounds__(64 * kAttendWaves, 2) k_attend_rows(AttendArgs a) {
     constexpr int S32 = D / 32;                                 // steps of the first product, 32 values each
     constexpr int C = D / 64, ODD = S32 & 1;                    // 16-byte pieces of a lane's key row (two steps each), and one of 8 bytes
     constexpr int DT = D / 16;                                  // 16-value tiles of the answer
+    constexpr bool FOUR = BITS == 4;
+    constexpr int VT = FOUR ? DT / 2 : DT;                      // rows of the values' codes that a lane reads
     __shared__ __align__(16) float lds_step[kAttendWaves][3][kTileKeys];
     __shared__ __align__(16) float lds_acc[kAttendWaves][kRows][D + 4];
     __shared__ float lds_m[kAttendWaves][kRows], lds_l[kAttendWaves][kRows];
+    __shared__ uint32_t lds_kf[FOUR ? kAttendWaves : 1][kTileKeys];
+    __shared__ __align__(16) _Float16 lds_vf[FOUR ? kAttendWaves : 1][S32][kTileKeys];      // in the order of the second product
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n = lane & 15, quarter = lane >> 4;
@@ -358,9 +364,13 @@ __global__ void __launch_bounds__(64 * kAttendWaves, 2) k_attend_rows(AttendArgs
     // What does not depend on lengths is requested first: the queries, and (chunk: one unit of the sequence's own table) the pages of the wavefront's first tile.
     const int qh = head * a.group + (live ? row - tok * a.group : 0);
     const int64_t q_at = (int64_t)(tile.first + tok) * a.q_token + (int64_t)qh * a.q_head;
+    auto component = [&](int i) {                               // first of the lane's 8 in step i
+        if (FOUR && D == 128) return 32 * quarter + 8 * i;
+        return i < 2 * C ? 64 * (i >> 1) + 16 * quarter + 8 * (i & 1) : 64 * C + 8 * quarter;
+    };
     i32x4 raw[S32];
 #pragma unroll
-    for (int i = 0; i < S32; ++i) raw[i] = load8_raw(a.q, q_at + (i < 2 * C ? 64 * (i >> 1) + 16 * quarter + 8 * (i & 1) : 64 * C + 8 * quarter), a.q_wide);
+    for (int i = 0; i < S32; ++i) raw[i] = load8_raw(a.q, q_at + component(i), a.q_wide);
     int page = 0;                                               // lane = key of a tile: its page
     const bool ahead = !a.ids && a.width > 0;
     if (ahead) page = a.tables[(int64_t)tile.s * a.width + min((split * a.unit + wave * kTileKeys + lane) >> a.st.shift, a.width - 1)];
@@ -373,9 +383,11 @@ __global__ void __launch_bounds__(64 * kAttendWaves, 2) k_attend_rows(AttendArgs
     // Operands: row i of the first product's tile b (of four) is key 16 (i >> 2) + 4 b + (i & 3), so that a quarter's 16 results are 16 consecutive keys -
     // the 16 consecutive bytes of a component in the transposed values.
     const int my_key = 16 * (n >> 2) + (n & 3);                 // (+ 4 b)
-    const uint32_t page_bytes = (uint32_t)D << a.st.shift;
-    i32x4 kr[4][C > 0 ? C : 1], vr[DT];
+    constexpr int ROW = D * BITS / 8;                           // bytes of a key row
+    const uint32_t page_bytes = (uint32_t)ROW << a.st.shift;
+    i32x4 kr[4][C > 0 && !FOUR ? C : 1], vr[VT];                // (4 bits: one piece, of which a lane uses D / 8 bytes)
     uint2 ko[4];
+    uint32_t rkf = 0, rvf = 0;
     float rks = 0.0f, rvs = 0.0f;
     bool rhave = false;
     int row_of_key = 0, row_of_tile = 0, place = 0;             // page * heads + head, per lane and (WHOLE) for the tile; place in the page
@@ -389,7 +401,25 @@ __global__ void __launch_bounds__(64 * kAttendWaves, 2) k_attend_rows(AttendArgs
         const uint64_t at = ((uint64_t)(uint32_t)(WHOLE ? row_of_tile : row_of_key) << a.st.shift) + (uint32_t)((place + lane) & (P - 1));
         rks = a.st.ks[at];
         rvs = a.st.vs[at];
-        if constexpr (WHOLE) {
+        if constexpr (FOUR) {
+            rkf = a.st.kf[at];
+            rvf = a.st.vf[at];
+        }
+        if constexpr (FOUR) {
+            const int8_t* base = WHOLE ? a.st.kc + (uint64_t)(uint32_t)row_of_tile * page_bytes + (uint32_t)(place * ROW) : nullptr;
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+                const int key = my_key + 4 * b;
+                const int8_t* kp = WHOLE ? base + here(key * ROW) : a.st.kc + (uint64_t)(uint32_t)__shfl(row_of_key, key, 64) * page_bytes + (uint32_t)((key & (P - 1)) * ROW);
+                if constexpr (D == 128) kr[b][0] = *(const i32x4*)(kp + 16 * quarter);
+                if constexpr (C == 1) {
+                    const i32x2 two = *(const i32x2*)(kp + 8 * quarter);
+                    kr[b][0][0] = two[0];
+                    kr[b][0][1] = two[1];
+                }
+                if constexpr (ODD) kr[b][0][2 * C] = *(const int*)(kp + 32 * C + 4 * quarter);
+            }
+        } else if constexpr (WHOLE) {
             const int8_t* base = a.st.kc + (uint64_t)(uint32_t)row_of_tile * page_bytes + (uint32_t)(place * D);
 #pragma unroll
             for (int b = 0; b < 4; ++b) {
@@ -415,11 +445,11 @@ __global__ void __launch_bounds__(64 * kAttendWaves, 2) k_attend_rows(AttendArgs
         if constexpr (WHOLE) {
             const int8_t* base = a.st.vc + (uint64_t)(uint32_t)row_tile * page_bytes + (uint32_t)at;
 #pragma unroll
-            for (int i = 0; i < DT; ++i) vr[i] = *(const i32x4*)(base + here(((n + 16 * i) << a.st.shift) + key));
+            for (int i = 0; i < VT; ++i) vr[i] = *(const i32x4*)(base + here(((n + 16 * i) << a.st.shift) + key));
         } else {
             const int8_t* vp = a.st.vc + (uint64_t)(uint32_t)__shfl(row_key, key, 64) * page_bytes + (uint32_t)((n << a.st.shift) + (key & (P - 1)));
 #pragma unroll
-            for (int i = 0; i < DT; ++i) vr[i] = *(const i32x4*)(vp + ((uint32_t)(16 * i) << a.st.shift));
+            for (int i = 0; i < VT; ++i) vr[i] = *(const i32x4*)(vp + ((uint32_t)(16 * i) << a.st.shift));
         }
     };
     it.skip(a, tile.s, behind, 1 + wave);
@@ -473,6 +503,11 @@ __global__ void __launch_bounds__(64 * kAttendWaves, 2) k_attend_rows(AttendArgs
             lds_step[wave][0][lane] = ks.product;
             lds_step[wave][1][lane] = ks.add;
             lds_step[wave][2][lane] = ks.inverse;
+            if constexpr (FOUR) {
+                lds_kf[wave][lane] = rkf;
+#pragma unroll
+                for (int g = 0; g < S32; ++g) lds_vf[wave][g][(lane & ~7) + token_place(lane & 7)] = factor_half(rvf, g);
+            }
             wild = wild || __ballot(ks.wild);
             wave_lds_order();
         }
@@ -480,17 +515,27 @@ __global__ void __launch_bounds__(64 * kAttendWaves, 2) k_attend_rows(AttendArgs
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
             s[b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            if constexpr (FOUR) {
+                const uint32_t factors = lds_kf[wave][my_key + 4 * b];
+                f16x8 r;
 #pragma unroll
-            for (int i = 0; i < C; ++i) {
-                f16x8 lo, hi;
-                codes_to_half(kr[b][i], lo, hi);
-                s[b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo, qf[2 * i], s[b], 0, 0, 0);
-                s[b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi, qf[2 * i + 1], s[b], 0, 0, 0);
-            }
-            if constexpr (ODD) {
-                f16x8 lo, hi;
-                codes_to_half(i32x4{(int)ko[b].x, (int)ko[b].y, 0, 0}, lo, hi);
-                s[b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo, qf[2 * C], s[b], 0, 0, 0);
+                for (int i = 0; i < S32; ++i) {
+                    if (i == 0 || (D != 128 && i == 2 * C)) r = spread(factor_pair(factors, (uint32_t)component(i) / 32));      // (128 values: the lane's 32 share one)
+                    s[b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes4_to_half((uint32_t)kr[b][0][i]) * r, qf[i], s[b], 0, 0, 0);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < C; ++i) {
+                    f16x8 lo, hi;
+                    codes_to_half(kr[b][i], lo, hi);
+                    s[b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo, qf[2 * i], s[b], 0, 0, 0);
+                    s[b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi, qf[2 * i + 1], s[b], 0, 0, 0);
+                }
+                if constexpr (ODD) {
+                    f16x8 lo, hi;
+                    codes_to_half(i32x4{(int)ko[b].x, (int)ko[b].y, 0, 0}, lo, hi);
+                    s[b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo, qf[2 * C], s[b], 0, 0, 0);
+                }
             }
         }
         __builtin_amdgcn_sched_barrier(0);
@@ -543,11 +588,23 @@ __global__ void __launch_bounds__(64 * kAttendWaves, 2) k_attend_rows(AttendArgs
             for (int j = 0; j < 4; ++j) {
                 const float e = __builtin_amdgcn_exp2f(s[b][j] - m_use);
                 if (!wild) l = fmaf(e, iv[j], l);
-                w[b >> 1][4 * (b & 1) + j] = (_Float16)e;
+                w[b >> 1][FOUR ? token_place(4 * (b & 1) + j) : 4 * (b & 1) + j] = (_Float16)e;
             }
         }
         L += l;
         asm volatile("" : "+v"(L));                             // (the sum is formed here: kept for later, its terms would fill the registers)
+        if constexpr (FOUR) {
+#pragma unroll
+            for (int i = 0; i < VT; ++i)
+#pragma unroll
+                for (int o = 0; o < 2; ++o) {
+                    const f16x8 r = *(const f16x8*)&lds_vf[wave][i][16 * quarter + 8 * o];
+                    uint32_t low, high;
+                    split_values4((uint32_t)vr[i][2 * o], (uint32_t)vr[i][2 * o + 1], low, high);
+                    acc[2 * i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes4_to_half(low) * r, w[o], acc[2 * i], 0, 0, 0);
+                    acc[2 * i + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes4_to_half(high) * r, w[o], acc[2 * i + 1], 0, 0, 0);
+                }
+        } else
 #pragma unroll
         for (int i = 0; i < DT; ++i) {
             f16x8 lo, hi;
@@ -605,7 +662,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, 2) k_attend_rows(AttendArgs
 
 // Joins the splits of each row: out = (sum_s 2^(M_s - M) acc_s) / (sum_s 2^(M_s - M) l_s), acc lifted.  Bound by latency for one token (3 us with 16 to 512 splits).  D / 4 threads hold a row's values; `sides` such groups share a row's splits (a power of two, as many as there are splits
 // while the block has room), each with a running reference of its own, and the block's other groups take other rows.
-template <typename T, int D>
+template <typename T, int D, int BITS>          // (BITS: the store's, a name of its own in each library file)
 __global__ void __launch_bounds__(256) k_attend_join(AttendArgs a, int sides) {
     constexpr int Q = D / 4, GROUPS = 256 / Q;
     __shared__ __align__(16) f32x4 lds_o[GROUPS][Q];

@@ -28,16 +28,22 @@ __device__ __forceinline__ void unrolled(F&& f) {
 // is used; one barrier per tile).  As in k_attend_rows the scores come out transposed, a lane holds scores of one row, and the weights
 // are the second product's operand as they stand.  Conversion once per block is why a block has 128 or 256 rows and why LDS is used at all: straight to
 // registers, as k_attend_rows does, each wavefront would convert all codes itself (320 instructions per tile at D = 128 instead of 80 or 40).
-template <typename T, int D, int NW, bool WHOLE>
+// BITS 4: a piece has 16 codes all the same, in 8 bytes: of a key, or of two components and 8 tokens, which come to lie in the order of token_place (the weights likewise).  A piece's codes
+// are multiplied by their factors as they are converted; the values' factors are in LDS one tile ahead, written with the steps.
+template <typename T, int D, int NW, bool WHOLE, int BITS>
 __global__ void __launch_bounds__(64 * NW, 2) k_attend_tile(AttendArgs a) {
     constexpr int C = D / 32, ROWS = NW * 32, THREADS = 64 * NW;
     constexpr int KS = D + 8, VS = kTileKeys + 8;               // row strides in LDS (16 bytes of padding: rows start in other banks)
     constexpr int PIECES = kTileKeys * D / 16;                  // 16-code pieces of the keys, and of the values
     constexpr int PER = (PIECES + THREADS - 1) / THREADS;
+    constexpr bool FOUR = BITS == 4;
+    constexpr int ROW = D * BITS / 8;                           // bytes of a key row
+    typedef std::conditional_t<FOUR, i32x2, i32x4> Piece;
     __shared__ __align__(16) _Float16 lds_k[2][kTileKeys * KS];
     __shared__ __align__(16) _Float16 lds_v[2][D * VS];
     __shared__ __align__(16) float lds_step[3][3][kTileKeys];
     __shared__ int lds_flag[NW], lds_wild[3];
+    __shared__ __align__(16) _Float16 lds_vf[FOUR ? 3 : 1][C][kTileKeys];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = lane & 31, half = lane >> 5;
@@ -128,10 +134,11 @@ __global__ void __launch_bounds__(64 * NW, 2) k_attend_tile(AttendArgs a) {
         }
     };
     auto row_of = [&](int page) { return ((uint32_t)page < (uint64_t)a.st.pages ? page : 0) * a.st.heads + head; };
-    i32x4 ck[PER], cv[PER];
+    Piece ck[PER], cv[PER];
+    uint32_t fk[PER], rvf = 0;                                  // 4 bits: factors of the pieces' keys, and of the values of the lane's key
     float rks = 0.0f, rvs = 0.0f;
     bool rhave = false;
-    const uint32_t page_bytes = (uint32_t)D << a.st.shift;
+    const uint32_t page_bytes = (uint32_t)ROW << a.st.shift;
     int off_v = 0;                                              // place in the page of the tile whose values are requested next
     bool have_v = false;
     // requests the keys of a tile, its steps in wavefront `by`, and notes where its values are
@@ -143,18 +150,20 @@ __global__ void __launch_bounds__(64 * NW, 2) k_attend_tile(AttendArgs a) {
         if constexpr (WHOLE) {
             const int page = __builtin_amdgcn_readfirstlane(pg[0]);
             pv[0] = row_of(page);
-            const int8_t* base = a.st.kc + (uint64_t)(uint32_t)pv[0] * page_bytes + (uint32_t)(off * D);
+            const int8_t* base = a.st.kc + (uint64_t)(uint32_t)pv[0] * page_bytes + (uint32_t)(off * ROW);
+            const uint64_t at = ((uint64_t)(uint32_t)pv[0] << a.st.shift) + (uint32_t)off;
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
                 const int p = tid + i * THREADS;
                 if (PIECES % THREADS && p >= PIECES) break;
-                ck[i] = *(const i32x4*)(base + here(16 * p));
+                ck[i] = *(const Piece*)(base + here((int)sizeof(Piece) * p));
+                if constexpr (FOUR) fk[i] = *(const uint32_t*)((const char*)(a.st.kf + at) + here(4 * (p / (D / 16))));
             }
             if (wave == by) {
                 rhave = kt.k + lane < kt.length && (uint32_t)page < (uint64_t)a.st.pages;
-                const uint64_t at = ((uint64_t)(uint32_t)pv[0] << a.st.shift) + (uint32_t)off;
                 rks = *(const float*)((const char*)(a.st.ks + at) + here(4 * lane));
                 rvs = *(const float*)((const char*)(a.st.vs + at) + here(4 * lane));
+                if constexpr (FOUR) rvf = *(const uint32_t*)((const char*)(a.st.vf + at) + here(4 * lane));
             }
         } else {
 #pragma unroll
@@ -162,14 +171,16 @@ __global__ void __launch_bounds__(64 * NW, 2) k_attend_tile(AttendArgs a) {
                 const int p = tid + i * THREADS;
                 if (PIECES % THREADS && p >= PIECES) break;
                 const int key = p / (D / 16), part = p % (D / 16);
-                ck[i] = *(const i32x4*)(a.st.kc + (uint64_t)(uint32_t)row_of(pg[i]) * page_bytes + (uint32_t)((key & (P - 1)) * D + 16 * part));
-                pv[i] = page_at(kt, 16 * (p % 4));
+                ck[i] = *(const Piece*)(a.st.kc + (uint64_t)(uint32_t)row_of(pg[i]) * page_bytes + (uint32_t)((key & (P - 1)) * ROW + (int)sizeof(Piece) * part));
+                if constexpr (FOUR) fk[i] = a.st.kf[((uint64_t)(uint32_t)row_of(pg[i]) << a.st.shift) + (uint32_t)(key & (P - 1))];
+                pv[i] = page_at(kt, FOUR ? 8 * (p % 8) : 16 * (p % 4));
             }
             if (wave == by) {
                 rhave = kt.k + lane < kt.length && (uint32_t)pg_step < (uint64_t)a.st.pages;
                 const uint64_t at = ((uint64_t)(uint32_t)row_of(pg_step) << a.st.shift) + (uint32_t)(lane & (P - 1));
                 rks = a.st.ks[at];
                 rvs = a.st.vs[at];
+                if constexpr (FOUR) rvf = a.st.vf[at];
             }
         }
     };
@@ -179,9 +190,15 @@ __global__ void __launch_bounds__(64 * NW, 2) k_attend_tile(AttendArgs a) {
         for (int i = 0; i < PER; ++i) {
             const int p = tid + i * THREADS;
             if (PIECES % THREADS && p >= PIECES) break;
-            const int comp = p / 4, grp = p % 4;
-            if constexpr (WHOLE) cv[i] = *(const i32x4*)(a.st.vc + (uint64_t)(uint32_t)pv[0] * page_bytes + (uint32_t)off_v + here((comp << a.st.shift) + 16 * grp));
-            else cv[i] = *(const i32x4*)(a.st.vc + (uint64_t)(uint32_t)row_of(pv[i]) * page_bytes + (uint32_t)((comp << a.st.shift) + ((16 * grp) & (P - 1))));
+            if constexpr (FOUR) {
+                const int row = p / 8, key = 8 * (p % 8);
+                if constexpr (WHOLE) cv[i] = *(const Piece*)(a.st.vc + (uint64_t)(uint32_t)pv[0] * page_bytes + (uint32_t)off_v + here((row << a.st.shift) + key));
+                else cv[i] = *(const Piece*)(a.st.vc + (uint64_t)(uint32_t)row_of(pv[i]) * page_bytes + (uint32_t)((row << a.st.shift) + (key & (P - 1))));
+            } else {
+                const int comp = p / 4, grp = p % 4;
+                if constexpr (WHOLE) cv[i] = *(const Piece*)(a.st.vc + (uint64_t)(uint32_t)pv[0] * page_bytes + (uint32_t)off_v + here((comp << a.st.shift) + 16 * grp));
+                else cv[i] = *(const Piece*)(a.st.vc + (uint64_t)(uint32_t)row_of(pv[i]) * page_bytes + (uint32_t)((comp << a.st.shift) + ((16 * grp) & (P - 1))));
+            }
         }
     };
     auto put = [&](_Float16* to, const i32x4 codes) {
@@ -196,19 +213,36 @@ __global__ void __launch_bounds__(64 * NW, 2) k_attend_tile(AttendArgs a) {
         const int key = p / (D / 16), part = p % (D / 16);
         // key 32 h + 16 b + 4 g + q is row 32 b + 8 g + 4 h + q of the first product
         const int krow = (key & 16) * 2 + (key >> 2 & 3) * 8 + (key >> 5) * 4 + (key & 3);
-        put(&lds_k[kb][krow * KS + 16 * part], ck[i]);
+        if constexpr (FOUR) {
+            const f16x8 r = spread(factor_pair(fk[i], (uint32_t)part / 2));
+            *(f16x8*)&lds_k[kb][krow * KS + 16 * part] = codes4_to_half((uint32_t)ck[i][0]) * r;
+            *(f16x8*)&lds_k[kb][krow * KS + 16 * part + 8] = codes4_to_half((uint32_t)ck[i][1]) * r;
+        } else put(&lds_k[kb][krow * KS + 16 * part], ck[i]);
     };
-    auto stage_values = [&](int kb, int i) {
+    auto stage_values = [&](int kb, int i, int sb) {            // sb: the steps' buffer of the same tile
         const int p = tid + i * THREADS;
         if (PIECES % THREADS && p >= PIECES) return;
-        put(&lds_v[kb][p / 4 * VS + 16 * (p % 4)], cv[i]);
+        if constexpr (FOUR) {
+            const int row = p / 8, g = row / 16, comp = 16 * g + row, at = 8 * (p % 8);
+            const f16x8 r = *(const f16x8*)&lds_vf[sb][g][at];
+            uint32_t low, high;
+            split_values4((uint32_t)cv[i][0], (uint32_t)cv[i][1], low, high);
+            *(f16x8*)&lds_v[kb][comp * VS + at] = codes4_to_half(low) * r;
+            *(f16x8*)&lds_v[kb][(comp + 16) * VS + at] = codes4_to_half(high) * r;
+        } else put(&lds_v[kb][p / 4 * VS + 16 * (p % 4)], cv[i]);
     };
+    // where the weight of key j of eight stands
+    auto place_of = [](int j) { return FOUR ? token_place(j) : j; };
     auto stage_steps = [&](int vb, const KeyTile& kt) {         // (by the wavefront that requested them: tiles go round)
         if (wave != vb) return;
         const KeySteps ks = key_steps(rks, rvs, c, kt.bias, rhave);
         lds_step[vb][0][lane] = ks.product;
         lds_step[vb][1][lane] = ks.add;
         lds_step[vb][2][lane] = ks.inverse;
+        if constexpr (FOUR) {
+#pragma unroll
+            for (int g = 0; g < C; ++g) lds_vf[vb][g][(lane & ~7) + token_place(lane & 7)] = factor_half(rvf, g);
+        }
         const int w = __ballot(ks.wild) != 0;
         if (lane == 0) lds_wild[vb] = w;
     };
@@ -292,7 +326,7 @@ __global__ void __launch_bounds__(64 * NW, 2) k_attend_tile(AttendArgs a) {
                 for (int j = 0; j < 4; ++j) {
                     const float e = __builtin_amdgcn_exp2f(y[b][4 * g + j] - m_use);
                     l = wild_now ? l + sum_term(y[b][4 * g + j], m_use, iv[j]) : fmaf(e, iv[j], l);
-                    w[b][g >> 1][4 * (g & 1) + j] = (_Float16)e;
+                    w[b][g >> 1][place_of(4 * (g & 1) + j)] = (_Float16)e;
                 }
             }
         L += l;
@@ -322,8 +356,11 @@ __global__ void __launch_bounds__(64 * NW, 2) k_attend_tile(AttendArgs a) {
     fetch_keys(d0, 0);
     fetch_values();
 #pragma unroll
-    for (int i = 0; i < PER; ++i) { stage_keys(0, i); stage_values(0, i); }
+    for (int i = 0; i < PER; ++i) stage_keys(0, i);
     stage_steps(0, d0);
+    if constexpr (FOUR) __syncthreads();                        // (the values' factors)
+#pragma unroll
+    for (int i = 0; i < PER; ++i) stage_values(0, i, 0);
     it.next(a, tile.s, behind);
     d1 = it.t;
     find_pages(d1);
@@ -398,7 +435,7 @@ __global__ void __launch_bounds__(64 * NW, 2) k_attend_tile(AttendArgs a) {
                         for (int j = 2 * pr; j < 2 * pr + 2; ++j) {
                             const float e = __builtin_amdgcn_exp2f(y[b][j] - m_use);
                             l = b == 0 && j == 0 ? e * iv[g % 2][j % 4] : fmaf(e, iv[g % 2][j % 4], l);
-                            w[b][j / 8][j % 8] = (_Float16)e;
+                            w[b][j / 8][place_of(j % 8)] = (_Float16)e;
                         }
                     });
                     asm volatile("" : "+v"(l));       // (the sum is formed here, not where it is next used)
@@ -434,7 +471,7 @@ __global__ void __launch_bounds__(64 * NW, 2) k_attend_tile(AttendArgs a) {
                     if constexpr (x < FIRST) {
                         unrolled<2 * PER * x / FIRST, 2 * PER * (x + 1) / FIRST>([&](auto uc) {
                             constexpr int u = decltype(uc)::value;
-                            if constexpr (u & 1) stage_values(kb ^ 1, u >> 1); else stage_keys(kb, u >> 1);
+                            if constexpr (u & 1) stage_values(kb ^ 1, u >> 1, v1); else stage_keys(kb, u >> 1);
                         });
                     } else {
                         unrolled<8 * (x - FIRST) / (STEPS - FIRST), 8 * (x - FIRST + 1) / (STEPS - FIRST)>([&](auto bg) {
@@ -477,7 +514,7 @@ __global__ void __launch_bounds__(64 * NW, 2) k_attend_tile(AttendArgs a) {
         gather(kb, w);
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < PER; ++i) { stage_keys(kb, i); stage_values(kb ^ 1, i); }
+        for (int i = 0; i < PER; ++i) { stage_keys(kb, i); stage_values(kb ^ 1, i, v1); }
         stage_steps(v2, d2);
         advance();
         __syncthreads();

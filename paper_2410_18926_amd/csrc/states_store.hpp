@@ -25,6 +25,7 @@ struct Store {
     float *ks, *vs;
     int64_t pages;
     int32_t heads, shift;      // page size = 1 << shift
+    uint32_t *kf, *vf;         // 4-bit store: four bytes of factors for each row (codes4.hpp)
 
     __device__ __forceinline__ int64_t row(int64_t page, int head) const { return (page * heads + head) << shift; }   // first token's place in the scales
 };

@@ -31,6 +31,11 @@ class CQuestions(C.Structure):
                 ("q_token", C.c_int64), ("q_head", C.c_int64), ("out_token", C.c_int64), ("out_head", C.c_int64), ("q_start", C.c_void_p), ("scale", C.c_float)]
 
 
+class CStates4(C.Structure):
+    _fields_ = [("k_codes", C.c_void_p), ("v_codes", C.c_void_p), ("k_factors", C.c_void_p), ("v_factors", C.c_void_p), ("k_scales", C.c_void_p), ("v_scales", C.c_void_p),
+                ("pages", C.c_int64), ("heads", C.c_int32), ("page_size", C.c_int32), ("dim", C.c_int32)]
+
+
 _raw_stream, _current_device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
 _lib = None
 
@@ -39,17 +44,15 @@ def lib() -> C.CDLL:
     global _lib
     if _lib is None:
         L = _base_lib()
-        vp, i32, i64, st, qs = C.c_void_p, C.c_int32, C.c_int64, C.POINTER(CStates), C.POINTER(CQuestions)
-        L.lorann_states_write.restype = C.c_int
-        L.lorann_states_write.argtypes = [st, vp, vp, i32, i64, i64, i64, i64, i64, vp, vp]
-        L.lorann_states_read.restype = C.c_int
-        L.lorann_states_read.argtypes = [st, vp, i64, vp, vp, i32, i64, i64, i64, i64, vp]
-        L.lorann_attend_chunk.restype = C.c_int
-        L.lorann_attend_chunk.argtypes = [st, qs, vp, i32, vp, vp, i64, vp]
-        L.lorann_attend_passages.restype = C.c_int
-        L.lorann_attend_passages.argtypes = [st, qs, vp, i32, vp, C.c_float, vp, i32, vp, i64, vp, i64, vp]
-        L.lorann_attend_workspace.restype = C.c_int64
-        L.lorann_attend_workspace.argtypes = [st, qs, i32, i32]
+        vp, i32, i64, qs = C.c_void_p, C.c_int32, C.c_int64, C.POINTER(CQuestions)
+        for bits, st in (("", C.POINTER(CStates)), ("4", C.POINTER(CStates4))):
+            for name, result, args in ((f"lorann_states{bits}_write", C.c_int, [st, vp, vp, i32, i64, i64, i64, i64, i64, vp, vp]),
+                                       (f"lorann_states{bits}_read", C.c_int, [st, vp, i64, vp, vp, i32, i64, i64, i64, i64, vp]),
+                                       (f"lorann_attend{bits}_chunk", C.c_int, [st, qs, vp, i32, vp, vp, i64, vp]),
+                                       (f"lorann_attend{bits}_passages", C.c_int, [st, qs, vp, i32, vp, C.c_float, vp, i32, vp, i64, vp, i64, vp]),
+                                       (f"lorann_attend{bits}_workspace", C.c_int64, [st, qs, i32, i32])):
+                f = getattr(L, name)
+                f.restype, f.argtypes = result, args
         _lib = L
     return _lib
 
@@ -102,6 +105,8 @@ class States:
     k_scales  [pages, heads, page_size] float32         v_scales  the same
     The tensors stay the caller's; slot = page * page_size + place in the page."""
 
+    _call = dict(write="lorann_states_write", read="lorann_states_read", chunk="lorann_attend_chunk", passages="lorann_attend_passages", workspace="lorann_attend_workspace")
+
     def __init__(self, k_codes, v_codes, k_scales, v_scales):
         self.k_codes, self.v_codes, self.k_scales, self.v_scales = k_codes, v_codes, k_scales, v_scales
         if k_codes.dim() != 4:
@@ -116,6 +121,9 @@ class States:
                                           (k_scales, torch.float32, steps, "k_scales"), (v_scales, torch.float32, steps, "v_scales")):
                 _array(t, dtype, shape, what)          # (says which)
         self._st = CStates(k_codes.data_ptr(), v_codes.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(), n, h, p, d)
+
+    def _run(self, what):
+        return getattr(lib(), self._call[what])
 
     @property
     def device(self):
@@ -149,7 +157,7 @@ class States:
         vt, vh = self._rows(v, n, "v")
         if k.dtype != v.dtype or k.dtype not in _TYPE:
             raise ValueError(f"k and v must both be float32, float16 or bfloat16, got {k.dtype} and {v.dtype}")
-        rc = lib().lorann_states_write(self._st, k.data_ptr(), v.data_ptr(), _TYPE[k.dtype], n, kt, kh, vt, vh, _array(slots, torch.int64, (n,), "slots"), self._stream())
+        rc = self._run("write")(self._st, k.data_ptr(), v.data_ptr(), _TYPE[k.dtype], n, kt, kh, vt, vh, _array(slots, torch.int64, (n,), "slots"), self._stream())
         if rc:
             _raise(rc)
 
@@ -166,7 +174,7 @@ class States:
         vt, vh = self._rows(v, n, "out[1]")
         if k.dtype != v.dtype or k.dtype not in _TYPE:
             raise ValueError(f"keys and values are read as float32, float16 or bfloat16, got {k.dtype} and {v.dtype}")
-        rc = lib().lorann_states_read(self._st, _array(slots, torch.int64, (n,), "slots"), n, k.data_ptr(), v.data_ptr(), _TYPE[k.dtype], kt, kh, vt, vh, self._stream())
+        rc = self._run("read")(self._st, _array(slots, torch.int64, (n,), "slots"), n, k.data_ptr(), v.data_ptr(), _TYPE[k.dtype], kt, kh, vt, vh, self._stream())
         if rc:
             _raise(rc)
         return k, v
@@ -189,7 +197,7 @@ class States:
             if not workspace.is_contiguous():          # (its size would not be the memory it has)
                 raise ValueError("workspace must be contiguous")
             return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
-        need = lib().lorann_attend_workspace(self._st, qs, found, width)
+        need = self._run("workspace")(self._st, qs, found, width)
         if need < 0:
             _raise(need)
         if not need:
@@ -200,7 +208,7 @@ class States:
     def workspace_bytes(self, q, sequences: int, width: int, found: int = 0, ragged: bool = False) -> int:
         """Bytes of `workspace` that a call with these queries and sizes needs (found = 0: attend_chunk; ragged: with q_start)."""
         qs = CQuestions(None, None, _TYPE.get(q.dtype, -1), q.shape[1], q.shape[0], sequences, 0, 0, 0, 0, 1 if ragged else None, 1.0)
-        need = lib().lorann_attend_workspace(self._st, qs, found, width)
+        need = self._run("workspace")(self._st, qs, found, width)
         if need < 0:
             _raise(need)
         return need
@@ -214,7 +222,7 @@ class States:
         n, width = tables.shape
         qs, out = self._questions(q, q_start, n, scale, out)
         ws, size, keep = self._workspace(qs, 0, width, workspace)
-        rc = lib().lorann_attend_chunk(self._st, qs, _array(tables, torch.int32, (n, width), "tables"), width, _array(lengths, torch.int32, (n,), "lengths"),
+        rc = self._run("chunk")(self._st, qs, _array(tables, torch.int32, (n, width), "tables"), width, _array(lengths, torch.int32, (n,), "lengths"),
                                        ws, size, self._stream())
         if rc:
             _raise(rc)
@@ -230,7 +238,7 @@ class States:
         passages, width = tables.shape
         qs, out = self._questions(q, q_start, n, scale, out)
         ws, size, keep = self._workspace(qs, found, width, workspace)
-        rc = lib().lorann_attend_passages(self._st, qs, _array(ids, torch.int64, (n, found), "ids"), found,
+        rc = self._run("passages")(self._st, qs, _array(ids, torch.int64, (n, found), "ids"), found,
                                           None if scores is None else _array(scores, torch.float32, (n, found), "scores"), score_weight,
                                           _array(tables, torch.int32, (passages, width), "tables"), width, _array(lengths, torch.int32, (passages,), "lengths"), passages,
                                           ws, size, self._stream())
