@@ -7,7 +7,7 @@ import subprocess
 import tempfile
 
 HERE = pathlib.Path(__file__).resolve().parent
-SRCS = [HERE / "csrc" / n for n in ("lorann.hip", "states.hip", "states4.hip")]      # the search; the state stores of 8 and 4 bits and their attention
+SRCS = [HERE / "csrc" / n for n in ("lorann.hip", "states.hip", "states4.hip", "evict.hip")]      # the search; the state stores of 8 and 4 bits and their attention; eviction from them
 LIB = HERE / "liblorann.so"
 
 FLAGS = [

@@ -1,0 +1,597 @@
+// The weight that causal attention gives each key, added up over the queries of a sequence and the query heads of a head (include/lorann_evict.h).
+//
+//   y_ij = <q_i, K_j> (scale log2 e) step_j;   m_i = max_j y_ij;   l_i = sum_j 2^(y_ij - m_i);   sums_j += sum_i 2^(y_ij - m_i) / l_i
+//
+// A weight needs its row's sum, so the scores are needed twice.  Few rows: k_weights_scores forms them once, bound by reading the keys, and keeps them in the workspace (4 bytes a score
+// where a key and head has D + 4 or D / 2 + 8), from which k_weights_add takes them.  Many rows: they are formed twice on the matrix cores, first with a block's rows held
+// and the keys passing by (k_weights_rows: m and l), then with a block's keys held and the rows passing by (k_weights_keys: the sums stay in registers, no atomics, one order).
+// Products are exact in binary16 as in attend.hpp; everything after them is float.
+#pragma once
+#include "attend.hpp"
+
+namespace lorann {
+
+struct WeightArgs {
+    AttendArgs a;              // out, part_acc, scores: not used
+    float* y;                  // few rows: [heads][tokens * group][row_keys]
+    int64_t row_keys;          // keys of a table, rounded up to whole tiles
+    const float* before;       // [sequences][heads][keys], or NULL
+    float* sums;
+    int64_t keys;              // of a table
+    // many rows: rows of a sequence begin at a multiple of 32 (padded_row)
+    int64_t padded;            // rows of a head
+    f16x8* q16;                // [heads][padded / 32][D / 16][64]: operands of the matrix instructions, as the lanes hold them
+    float* back;               // [heads][padded]: what a product of such a row is to be multiplied by, scale log2 e included
+    float *row_m, *row_inv;    // [heads][padded]: m, 1 / l
+};
+
+// Sequence s's rows begin here: ru(x) + ru(y) <= ru(x + y) + 32, so no two sequences' tiles of 32 overlap.
+__device__ __forceinline__ int64_t padded_row(int64_t first_row, int s) { return (first_row + 31) / 32 * 32 + 32 * (int64_t)s; }
+
+// (m, l) of two parts of a row; l = 0 where a part has no key.
+__device__ __forceinline__ void join_sums(float& m, float& l, float m2, float l2) {
+    const float top = fmaxf(m, m2), use = top == -INFINITY ? 0.0f : top;
+    l = l * __builtin_amdgcn_exp2f(m - use) + l2 * __builtin_amdgcn_exp2f(m2 - use);
+    m = top;
+}
+
+// Eight codes of a key from component `at` on (a multiple of 8), as binary16 operands: code, or r_g * code.
+template <int D, int BITS>
+__device__ __forceinline__ f16x8 key_operand(const int8_t* row, int at, uint32_t factors) {
+    if constexpr (BITS == 4) return codes4_to_half(*(const uint32_t*)(row + at / 2)) * spread(factor_pair(factors, (uint32_t)at / 32));
+    else {
+        const i32x2 c = *(const i32x2*)(row + at);
+        f16x8 lo, hi;
+        codes_to_half(i32x4{c[0], c[1], 0, 0}, lo, hi);
+        return lo;
+    }
+}
+
+// Few rows.  A block has up to 16 rows of one head and a range of keys; its wavefronts take tiles of 64 keys in turn, codes straight from memory into registers, the next tile's in flight
+// (as k_attend_rows).  A lane keeps a maximum and a sum of its own until the end.
+template <typename T, int D, int BITS>
+__global__ void __launch_bounds__(64 * kAttendWaves, 2) k_weights_scores(WeightArgs wa) {
+    const AttendArgs& a = wa.a;
+    constexpr int S32 = D / 32, ROW = D * BITS / 8;
+    constexpr int PIECE = BITS == 8 ? 8 : 4;                    // bytes of a lane's eight codes
+    __shared__ __align__(16) float lds_step[kAttendWaves][2][kTileKeys];
+    __shared__ float lds_m[kAttendWaves][kRows], lds_l[kAttendWaves][kRows];
+
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n = lane & 15, quarter = lane >> 4;
+    const BlockWork work = block_work(a);
+    const int head = work.head, split = work.split;
+    RowTile tile;
+    if (!find_tile<kRows, false>(a, work.tile, tile)) return;
+    const int rows = tile.count * a.group;
+    const int row = tile.row0 + n;
+    const bool live = row < rows;
+    const int tok = live ? row / a.group : 0;
+    const int see_after = tile.count - 1 - tok;
+    const int behind = tile.count - 1 - (min(rows, tile.row0 + kRows) - 1) / a.group, first_behind = tile.count - 1 - tile.row0 / a.group;
+    const int P = 1 << a.st.shift;
+
+    const int qh = head * a.group + (live ? row - tok * a.group : 0);
+    const int64_t q_at = (int64_t)(tile.first + tok) * a.q_token + (int64_t)qh * a.q_head;
+    auto component = [&](int i) { return (D / 4) * quarter + 8 * i; };         // first of the lane's 8 in step i
+    i32x4 raw[S32];
+#pragma unroll
+    for (int i = 0; i < S32; ++i) raw[i] = load8_raw(a.q, q_at + component(i), a.q_wide);
+    int page = 0;
+    KeyTiles it;
+    it.start(a, tile.s, split);
+    auto find_page = [&](const KeyTile& kt) {
+        if (kt.have) page = kt.pages[min(kt.k + lane, kt.length - 1) >> a.st.shift];
+    };
+    const int my_key = 16 * (n >> 2) + (n & 3);                 // (+ 4 b: a quarter's 16 results are 16 consecutive keys)
+    const uint32_t page_bytes = (uint32_t)ROW << a.st.shift;
+    uint32_t kr[4][S32][PIECE / 4], rkf[4];
+    float rks = 0.0f;
+    bool rhave = false;
+    auto fetch_keys = [&](const KeyTile& kt) {
+        if (!kt.have) return;
+        const bool known = (uint32_t)page < (uint64_t)a.st.pages;
+        rhave = known && kt.k + lane < kt.length;
+        const int row_of_key = (known ? page : 0) * a.st.heads + head, place = (kt.k + lane) & (P - 1);
+        rks = a.st.ks[((uint64_t)(uint32_t)row_of_key << a.st.shift) + (uint32_t)place];
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            const int key = my_key + 4 * b;
+            const uint64_t r = (uint32_t)__shfl(row_of_key, key, 64);
+            const uint32_t at = (uint32_t)((kt.k + key) & (P - 1));
+            const int8_t* kp = a.st.kc + r * page_bytes + at * ROW + component(0) * BITS / 8;
+#pragma unroll
+            for (int i = 0; i < S32; ++i)
+#pragma unroll
+                for (int j = 0; j < PIECE / 4; ++j) kr[b][i][j] = *(const uint32_t*)(kp + PIECE * i + 4 * j);
+            if constexpr (BITS == 4) rkf[b] = a.st.kf[(r << a.st.shift) + at];
+        }
+    };
+    it.skip(a, tile.s, behind, 1 + wave);
+    KeyTile cur = it.t;
+    find_page(cur);
+    fetch_keys(cur);
+    it.skip(a, tile.s, behind, kAttendWaves);
+    find_page(it.t);
+
+    f16x8 qf[S32];
+    float q_back;
+    {
+        float top = 0.0f;
+#pragma unroll
+        for (int i = 0; i < S32; ++i) {
+            if (!live) raw[i] = i32x4{0, 0, 0, 0};
+            float f[8];
+            widen8<T>(raw[i], f);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float m = fabsf(f[j]);
+                if (m <= 3.4028235e38f) top = fmaxf(top, m);
+            }
+        }
+        top = fmaxf(top, __shfl_xor(top, 32, 64));
+        top = fmaxf(top, __shfl_xor(top, 16, 64));
+        float up;
+        row_power(top, up, q_back);
+#pragma unroll
+        for (int i = 0; i < S32; ++i) {
+            float f[8];
+            widen8<T>(raw[i], f);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) qf[i][j] = (_Float16)(f[j] * up);
+        }
+    }
+
+    float* const y_row = wa.y + ((int64_t)head * a.tokens * a.group + (int64_t)tile.first * a.group + row) * wa.row_keys + 16 * quarter;
+    float M = -INFINITY, L = 0.0f;
+    while (cur.have) {
+        wave_lds_order();                                       // the previous tile's steps have been read
+        lds_step[wave][0][lane] = rhave ? rks * a.c : 0.0f;
+        lds_step[wave][1][lane] = rhave ? 0.0f : -INFINITY;
+        wave_lds_order();
+        f32x4 s[4];
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            s[b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int i = 0; i < S32; ++i) {
+                f16x8 k;
+                if constexpr (BITS == 4) k = codes4_to_half(kr[b][i][0]) * spread(factor_pair(rkf[b], (uint32_t)component(i) / 32));
+                else {
+                    f16x8 hi;
+                    codes_to_half(i32x4{(int)kr[b][i][0], (int)kr[b][i][PIECE / 4 - 1], 0, 0}, k, hi);
+                }
+                s[b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, qf[i], s[b], 0, 0, 0);
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        const KeyTile nxt = it.t;
+        fetch_keys(nxt);
+        it.skip(a, tile.s, behind, kAttendWaves);
+        find_page(it.t);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            const f32x4 sk = *(const f32x4*)&lds_step[wave][0][16 * quarter + 4 * b], lv = *(const f32x4*)&lds_step[wave][1][16 * quarter + 4 * b];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) s[b][j] = fmaf(s[b][j] * q_back, sk[j], lv[j]);
+        }
+        if (cur.k + kTileKeys > cur.length - first_behind) {    // some row may not see all of it
+            const int see = cur.length - see_after - cur.k - 16 * quarter;
+#pragma unroll
+            for (int b = 0; b < 4; ++b)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) s[b][j] = 4 * b + j < see ? s[b][j] : -INFINITY;
+        }
+        if (live) {
+#pragma unroll
+            for (int b = 0; b < 4; ++b) *(f32x4*)(y_row + cur.k + 4 * b) = s[b];
+        }
+        float top = M;
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) top = fmaxf(top, s[b][j]);
+        const float use = top == -INFINITY ? 0.0f : top;
+        float l = L * __builtin_amdgcn_exp2f(M - use);
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) l += __builtin_amdgcn_exp2f(s[b][j] - use);
+        L = l;
+        M = top;
+        cur = nxt;
+    }
+    join_sums(M, L, __shfl_xor(M, 32, 64), __shfl_xor(L, 32, 64));
+    join_sums(M, L, __shfl_xor(M, 16, 64), __shfl_xor(L, 16, 64));
+    if (quarter == 0) { lds_m[wave][n] = M; lds_l[wave][n] = L; }
+    __syncthreads();
+    if (threadIdx.x < kRows && live) {
+#pragma unroll
+        for (int w = 1; w < kAttendWaves; ++w) join_sums(M, L, lds_m[w][n], lds_l[w][n]);
+        const int64_t all = (int64_t)a.tokens * a.group, at = ((int64_t)split * a.st.heads + head) * all + (int64_t)tile.first * a.group + row;
+        a.part_m[at] = M;
+        a.part_l[at] = L;
+    }
+}
+
+// Tokens of sequence s.
+__device__ __forceinline__ void tokens_of(const AttendArgs& a, int s, int& first, int& count) {
+    const int each = (int)(a.tokens / a.sequences);
+    first = a.q_start ? min(max(a.q_start[s], 0), (int)a.tokens) : s * each;
+    count = a.q_start ? max(min(a.q_start[s + 1], (int)a.tokens) - first, 0) : each;
+}
+
+constexpr int kAddKeys = 1024;         // keys of a block: four a thread
+constexpr int kAddRows = 32;           // rows whose sums are joined at a time
+
+// Few rows, second half: bound by reading the scores.  Blocks: (chunk of keys, head, sequence).
+__global__ void __launch_bounds__(256) k_weights_add(WeightArgs wa) {
+    const AttendArgs& a = wa.a;
+    __shared__ float lds_m[kAddRows], lds_inv[kAddRows];
+    const int head = blockIdx.y, s = blockIdx.z, tid = threadIdx.x;
+    const int64_t j0 = (int64_t)blockIdx.x * kAddKeys + 4 * tid;
+    int first, count;
+    tokens_of(a, s, first, count);
+    const int length = a.found ? min(max(a.lengths[s], 0), a.width << a.st.shift) : 0;
+    const int rows = (int64_t)blockIdx.x * kAddKeys < length ? count * a.group : 0;
+    const int64_t at = ((int64_t)s * a.st.heads + head) * wa.keys + j0;
+    const bool mine = j0 < wa.keys;                             // (keys of a table are a multiple of 16)
+    float sum[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) sum[j] = mine && wa.before ? wa.before[at + j] : 0.0f;
+    const int64_t all = (int64_t)a.tokens * a.group, row_at = (int64_t)first * a.group;
+    float more[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int r0 = 0; r0 < rows; r0 += kAddRows) {
+        const int many = min(kAddRows, rows - r0);
+        {
+            // eight threads a row join its splits
+            const int r = tid >> 3, part = tid & 7;
+            float m = -INFINITY, l = 0.0f;
+            if (r < many)
+                for (int p = part; p < a.splits; p += 8) {
+                    const int64_t i = ((int64_t)p * a.st.heads + head) * all + row_at + r0 + r;
+                    join_sums(m, l, a.part_m[i], a.part_l[i]);
+                }
+#pragma unroll
+            for (int o = 1; o < 8; o <<= 1) join_sums(m, l, __shfl_xor(m, o, 64), __shfl_xor(l, o, 64));
+            if (r < many && part == 0) {
+                lds_m[r] = m == -INFINITY ? 0.0f : m;
+                lds_inv[r] = l == 0.0f ? 0.0f : 1.0f / l;
+            }
+        }
+        __syncthreads();
+        if (mine) {
+            const float* y = wa.y + ((int64_t)head * all + row_at + r0) * wa.row_keys + j0;
+            for (int r = 0; r < many; ++r) {
+                const int see = length - count + (r0 + r) / a.group + 1 - (int)j0;       // keys that the row sees from j0 on
+                if (see <= 0) continue;
+                const f32x4 v = *(const f32x4*)(y + r * wa.row_keys);
+                const float m = lds_m[r], inv = lds_inv[r];
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (j < see && v[j] != -INFINITY) more[j] = fmaf(__builtin_amdgcn_exp2f(v[j] - m), inv, more[j]);
+            }
+        }
+        __syncthreads();
+    }
+    if (!mine) return;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) wa.sums[at + j] = sum[j] + more[j];
+}
+
+// Many rows: queries as operands.  A wavefront has 32 rows; lane n + 32 half holds components D / 2 half .. of row n.
+template <typename T, int D>
+__global__ void __launch_bounds__(64) k_weights_queries(WeightArgs wa) {
+    const AttendArgs& a = wa.a;
+    constexpr int N = D / 16;
+    const int head = blockIdx.y, lane = threadIdx.x, n = lane & 31, half = lane >> 5;
+    RowTile tile;
+    if (!find_tile<32, false>(a, blockIdx.x, tile)) return;
+    const int row = tile.row0 + n;
+    const bool live = row < tile.count * a.group;
+    const int tok = live ? row / a.group : 0, qh = head * a.group + (live ? row - tok * a.group : 0);
+    const int64_t at = (int64_t)(tile.first + tok) * a.q_token + (int64_t)qh * a.q_head + D / 2 * half;
+    i32x4 raw[N];
+    float top = 0.0f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        raw[i] = load8_raw(a.q, at + 8 * i, a.q_wide);
+        if (!live) raw[i] = i32x4{0, 0, 0, 0};
+        float f[8];
+        widen8<T>(raw[i], f);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float m = fabsf(f[j]);
+            if (m <= 3.4028235e38f) top = fmaxf(top, m);
+        }
+    }
+    top = fmaxf(top, __shfl_xor(top, 32, 64));
+    float up, back;
+    row_power(top, up, back);
+    const int64_t slot = padded_row((int64_t)tile.first * a.group, tile.s) + tile.row0;          // a multiple of 32
+    f16x8* to = wa.q16 + ((int64_t)head * wa.padded + slot) / 32 * N * 64 + lane;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        float f[8];
+        widen8<T>(raw[i], f);
+        f16x8 q;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) q[j] = (_Float16)(f[j] * up);
+        to[64 * i] = q;
+    }
+    if (half == 0) wa.back[(int64_t)head * wa.padded + slot + n] = back * a.c;
+}
+
+// Many rows: m and l.  A block has 128 rows of one head, a wavefront 32; keys pass by, 64 at a time, converted once for the block into LDS.
+template <int D, int BITS>
+__global__ void __launch_bounds__(256, 2) k_weights_rows(WeightArgs wa) {
+    const AttendArgs& a = wa.a;
+    constexpr int N = D / 16, KS = D + 8, ROW = D * BITS / 8;
+    constexpr int PIECES = kTileKeys * D / 8, PER = PIECES / 256;              // pieces of eight codes
+    __shared__ __align__(16) _Float16 lds_k[2][kTileKeys * KS];
+    __shared__ __align__(16) float lds_step[2][2][kTileKeys];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, half = lane >> 5;
+    const BlockWork work = block_work(a);
+    const int head = work.head, split = work.split;
+    RowTile tile;
+    if (!find_tile<128, true>(a, work.tile, tile)) return;
+    const int rows = tile.count * a.group, row = tile.row0 + wave * 32 + n, P = 1 << a.st.shift;
+    const bool live = row < rows;
+    const int see_after = tile.count - 1 - (live ? row / a.group : 0);
+    const int behind = tile.count - 1 - (min(rows, tile.row0 + 128) - 1) / a.group, first_behind = tile.count - 1 - tile.row0 / a.group;
+    const int64_t slot = (int64_t)head * wa.padded + padded_row((int64_t)tile.first * a.group, tile.s) + tile.row0 + wave * 32;      // of the wavefront's first row
+    const bool any = tile.row0 + wave * 32 < rows;              // (a wavefront without rows has no operands either)
+    f16x8 q[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        if (any) q[i] = wa.q16[(slot / 32 * N + i) * 64 + lane];
+        else q[i] = f16x8{0, 0, 0, 0, 0, 0, 0, 0};
+    }
+    const float back = any ? wa.back[slot + n] : 0.0f;
+
+    const uint32_t page_bytes = (uint32_t)ROW << a.st.shift;
+    int pg[PER], pg_step = 0;
+    auto page_at = [&](const KeyTile& kt, int key) { return kt.pages[min(kt.k + key, kt.length - 1) >> a.st.shift]; };
+    auto find_pages = [&](const KeyTile& kt) {
+        if (!kt.have) return;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) pg[i] = page_at(kt, (tid + i * 256) / (D / 8));
+        pg_step = page_at(kt, lane);
+    };
+    auto row_of = [&](int page) { return (uint64_t)(uint32_t)(((uint32_t)page < (uint64_t)a.st.pages ? page : 0) * a.st.heads + head); };
+    i32x2 ck[PER];
+    uint32_t fk[PER];
+    float rks = 0.0f;
+    bool rhave = false;
+    auto fetch = [&](const KeyTile& kt) {
+        if (!kt.have) return;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int p = tid + i * 256, key = p / (D / 8), part = p % (D / 8);
+            const uint64_t r = row_of(pg[i]);
+            const uint32_t at = (uint32_t)((kt.k + key) & (P - 1));
+            const int8_t* from = a.st.kc + r * page_bytes + at * ROW + part * BITS;
+            if constexpr (BITS == 8) ck[i] = *(const i32x2*)from;
+            else {
+                ck[i][0] = *(const int*)from;
+                fk[i] = a.st.kf[(r << a.st.shift) + at];
+            }
+        }
+        if (wave == 0) {
+            rhave = kt.k + lane < kt.length && (uint32_t)pg_step < (uint64_t)a.st.pages;
+            rks = a.st.ks[(row_of(pg_step) << a.st.shift) + (uint32_t)((kt.k + lane) & (P - 1))];
+        }
+    };
+    auto stage = [&](int kb) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int p = tid + i * 256, key = p / (D / 8), part = p % (D / 8);
+            f16x8 k, hi;
+            if constexpr (BITS == 8) codes_to_half(i32x4{ck[i][0], ck[i][1], 0, 0}, k, hi);
+            else k = codes4_to_half((uint32_t)ck[i][0]) * spread(factor_pair(fk[i], (uint32_t)part / 4));
+            // key 32 h + 16 b + 4 g + r is row 32 b + 8 g + 4 h + r of the product, whose 32 results of a lane are then consecutive keys
+            const int krow = (key & 16) * 2 + (key >> 2 & 3) * 8 + (key >> 5) * 4 + (key & 3);
+            *(f16x8*)&lds_k[kb][krow * KS + 8 * part] = k;
+        }
+        if (wave == 0) {
+            lds_step[kb][0][lane] = rhave ? rks : 0.0f;
+            lds_step[kb][1][lane] = rhave ? 0.0f : -INFINITY;
+        }
+    };
+    KeyTiles it;
+    it.start(a, tile.s, split);
+    it.next(a, tile.s, behind);
+    KeyTile cur = it.t;
+    find_pages(cur);
+    fetch(cur);
+    it.next(a, tile.s, behind);
+    find_pages(it.t);
+    if (cur.have) stage(0);
+    KeyTile nxt = it.t;
+    fetch(nxt);
+    it.next(a, tile.s, behind);
+    find_pages(it.t);
+    int kb = 0;
+    float M = -INFINITY, L = 0.0f;
+    while (cur.have) {
+        __syncthreads();                                        // tile `cur` is in buffer kb; the other has been read
+        f32x16 s[2];
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) s[b][j] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                const f16x8 k = *(const f16x8*)&lds_k[kb][(32 * b + n) * KS + D / 2 * half + 8 * i];
+                s[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, q[i], s[b], 0, 0, 0);
+            }
+        if (nxt.have) stage(kb ^ 1);
+        const KeyTile after = it.t;
+        fetch(after);
+        it.next(a, tile.s, behind);
+        find_pages(it.t);
+        float top = M;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const f32x4 sk = *(const f32x4*)&lds_step[kb][0][32 * half + 16 * b + 4 * g], lv = *(const f32x4*)&lds_step[kb][1][32 * half + 16 * b + 4 * g];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) s[b][4 * g + j] = fmaf(s[b][4 * g + j] * back, sk[j], lv[j]);
+            }
+        if (cur.k + kTileKeys > cur.length - first_behind) {
+            const int see = cur.length - see_after - cur.k - 32 * half;
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) s[b][j] = 16 * b + j < see ? s[b][j] : -INFINITY;
+        }
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) top = fmaxf(top, s[b][j]);
+        const float use = top == -INFINITY ? 0.0f : top;
+        float l = L * __builtin_amdgcn_exp2f(M - use);
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) l += __builtin_amdgcn_exp2f(s[b][j] - use);
+        L = l;
+        M = top;
+        cur = nxt;
+        nxt = after;
+        kb ^= 1;
+    }
+    join_sums(M, L, __shfl_xor(M, 32, 64), __shfl_xor(L, 32, 64));
+    if (!any || half) return;
+    if (a.splits == 1) {
+        wa.row_m[slot + n] = M == -INFINITY ? 0.0f : M;
+        wa.row_inv[slot + n] = live && L != 0.0f ? 1.0f / L : 0.0f;
+    } else {
+        const int64_t at = (int64_t)split * a.st.heads * wa.padded + slot + n;
+        a.part_m[at] = M;
+        a.part_l[at] = live ? L : 0.0f;
+    }
+}
+
+// Joins the splits of each row (rows of no sequence hold anything).
+__global__ void __launch_bounds__(256) k_weights_join(WeightArgs wa) {
+    const AttendArgs& a = wa.a;
+    const int64_t all = a.st.heads * wa.padded, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= all) return;
+    float m = -INFINITY, l = 0.0f;
+    for (int p = 0; p < a.splits; ++p) join_sums(m, l, a.part_m[p * all + i], a.part_l[p * all + i]);
+    wa.row_m[i] = m == -INFINITY ? 0.0f : m;
+    wa.row_inv[i] = l == 0.0f ? 0.0f : 1.0f / l;
+}
+
+// Many rows: the sums.  A wavefront holds 64 keys as operands, rows pass by, 32 at a time.  SHARE: the block's four wavefronts have the same keys and take the rows in turn; else each
+// has keys of its own.  Blocks: (chunk of keys, head, sequence).
+template <int D, int BITS, bool SHARE>
+__global__ void __launch_bounds__(256, 2) k_weights_keys(WeightArgs wa) {
+    const AttendArgs& a = wa.a;
+    constexpr int N = D / 16, ROW = D * BITS / 8;
+    __shared__ float lds_sum[4][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 31, half = lane >> 5;
+    const int head = blockIdx.y, s = blockIdx.z, P = 1 << a.st.shift;
+    const int64_t k0 = ((int64_t)blockIdx.x * (SHARE ? 1 : 4) + (SHARE ? 0 : wave)) * 64;
+    int first, count;
+    tokens_of(a, s, first, count);
+    const int length = a.found ? min(max(a.lengths[s], 0), a.width << a.st.shift) : 0;
+    const int rows = k0 < length ? count * a.group : 0;
+    // the lane's two keys as operands; of its 32 results the keys are 32 half + 16 b + 4 g + r, as in k_weights_rows: row 32 b + n of the product is that key
+    f16x8 k[2][N];
+    float step[2][16];
+    const int32_t* pages = a.tables + (int64_t)s * a.width;
+    auto row_at = [&](int key, uint64_t& r, uint32_t& at) -> bool {
+        const int64_t j = k0 + key;
+        const int page = j < length ? pages[j >> a.st.shift] : -1;
+        const bool ok = (uint32_t)page < (uint64_t)a.st.pages;
+        r = (uint64_t)(uint32_t)((ok ? page : 0) * a.st.heads + head);
+        at = (uint32_t)(j & (P - 1));
+        return ok;
+    };
+    if (rows > 0) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            const int key = 32 * (n >> 2 & 1) + 16 * b + 4 * (n >> 3) + (n & 3);
+            uint64_t r;
+            uint32_t at;
+            row_at(key, r, at);
+            const int8_t* from = a.st.kc + ((r << a.st.shift) + at) * ROW;
+            uint32_t factors = 0;
+            if constexpr (BITS == 4) factors = a.st.kf[(r << a.st.shift) + at];
+#pragma unroll
+            for (int i = 0; i < N; ++i) k[b][i] = key_operand<D, BITS>(from, D / 2 * half + 8 * i, factors);
+        }
+        // the step of the lane's own key, spread over the results (a key that is not there: a step of 0 and, below, no weight)
+        uint64_t r;
+        uint32_t at;
+        const bool ok = row_at(lane, r, at);
+        const float mine = ok ? a.st.ks[(r << a.st.shift) + at] : -INFINITY;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) step[b][j] = __shfl(mine, 32 * half + 16 * b + j, 64);
+    }
+    float sum[2][16];
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) sum[b][j] = 0.0f;
+    // the first row that sees key k0
+    const int from_row = (int)max((int64_t)0, k0 - (length - count)) * a.group / 32 * 32;
+    const int64_t base = (int64_t)head * wa.padded + padded_row((int64_t)first * a.group, s);
+    const f16x8* q16 = wa.q16 + base / 32 * N * 64 + lane;
+    for (int r0 = from_row + (SHARE ? wave * 32 : 0); r0 < rows; r0 += SHARE ? 128 : 32) {
+        f32x16 y[2];
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) y[b][j] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const f16x8 q = q16[((int64_t)(r0 / 32) * N + i) * 64];
+#pragma unroll
+            for (int b = 0; b < 2; ++b) y[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k[b][i], q, y[b], 0, 0, 0);
+        }
+        const int row = r0 + n;
+        const float back = wa.back[base + row], m = wa.row_m[base + row], inv = row < rows ? wa.row_inv[base + row] : 0.0f;
+        const int see = row < rows ? (int)(length - count + row / a.group + 1 - k0) - 32 * half : 0;
+        const bool whole = __ballot(see < 32) == 0;             // every row sees all of the lane's keys
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                const float e = __builtin_amdgcn_exp2f(fmaf(y[b][j] * back, step[b][j], -m)) * inv;
+                if (whole) sum[b][j] += step[b][j] == -INFINITY ? 0.0f : e;
+                else sum[b][j] += 16 * b + j < see && step[b][j] != -INFINITY ? e : 0.0f;
+            }
+    }
+    // the 32 rows of a lane's results, then the lane that has the key's place writes it
+    float mine = 0.0f;
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            float t = sum[b][j];
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) t += __shfl_xor(t, o, 64);
+            if (n == 16 * b + j) mine = t;
+        }
+    const int64_t key = k0 + lane;
+    if constexpr (SHARE) {
+        lds_sum[wave][lane] = mine;
+        __syncthreads();
+        if (wave) return;
+        mine = ((lds_sum[0][lane] + lds_sum[1][lane]) + lds_sum[2][lane]) + lds_sum[3][lane];
+    }
+    if (key >= wa.keys) return;
+    const int64_t at = ((int64_t)s * a.st.heads + head) * wa.keys + key;
+    wa.sums[at] = (wa.before ? wa.before[at] : 0.0f) + mine;
+}
+
+}  // namespace lorann

@@ -1,0 +1,214 @@
+// C ABI (include/lorann_evict.h): weights that attention gives each key, and eviction by them.  No call allocates, waits or keeps anything.
+#include "../../include/lorann_evict.h"
+#include "attend_weights.hpp"
+#include "evict.hpp"
+#include "states_host.hpp"
+
+using namespace lorann;
+
+namespace {
+
+struct WeightPlan {
+    bool many;
+    int64_t tiles, tiles32, padded, row_keys;
+    int32_t unit, splits;
+    int64_t y, parts, q16, rows, workspace;      // bytes: scores; m and l of the splits; operands; back, m, 1 / l of a row
+};
+
+// Rows per sequence and head (their mean over the call) up to which the scores are kept, and how much memory they may take: otherwise they are formed twice.
+constexpr int64_t kFewWeightRows = 32, kMostScores = (int64_t)1 << 30;
+
+template <typename St>
+WeightPlan weight_plan(const St* st, const lorann_questions* qs, int32_t width) {
+    WeightPlan p{};
+    const int64_t group = qs->heads / st->heads, rows = qs->tokens * group, mean_rows = rows / qs->sequences;
+    const int64_t keys = (int64_t)width * st->page_size;
+    auto tiles_of = [&](int64_t n) { return qs->q_start ? rows / n + qs->sequences : qs->sequences * ceil_div(mean_rows, n); };
+    p.row_keys = ceil_div(std::max<int64_t>(keys, 1), kTileKeys) * kTileKeys;
+    p.y = rows * st->heads * p.row_keys * 4;
+    p.many = mean_rows > kFewWeightRows || p.y > kMostScores;
+    p.tiles = tiles_of(p.many ? 128 : kRows);
+    const int64_t blocks = std::max<int64_t>(p.tiles * st->heads, 1);
+    const int64_t want = std::max<int64_t>(1, std::min(kBlocksWanted / blocks, ceil_div(keys, kKeysPerBlock)));
+    const int64_t most = std::max(want, ceil_div(keys, p.many ? kMostTileKeys : kMostKeys));
+    p.unit = (int32_t)(ceil_div(ceil_div(std::max<int64_t>(keys, 1), most), kKeysPerBlock) * kKeysPerBlock);
+    p.splits = (int32_t)ceil_div(std::max<int64_t>(keys, 1), p.unit);
+    if (p.many) {
+        p.tiles32 = tiles_of(32);
+        p.padded = ceil_div(rows, 32) * 32 + 32 * qs->sequences;
+        p.y = 0;
+        p.q16 = p.padded * st->heads * st->dim * 2;
+        p.rows = 3 * p.padded * st->heads * 4;
+        p.parts = p.splits > 1 ? 2 * (int64_t)p.splits * p.padded * st->heads * 4 : 0;
+    } else p.parts = 2 * (int64_t)p.splits * rows * st->heads * 4;
+    p.workspace = ceil_div(p.y + p.parts + p.q16 + p.rows, 16) * 16;
+    return p;
+}
+
+template <typename St>
+int check_weights(const St* st, const lorann_questions* qs, int32_t width) {
+    int rc;
+    if ((rc = check_sizes(st)) || (rc = check_questions(st, qs, 0, width))) return rc;
+    if (qs->sequences > 65535) return fail(LORANN_E_UNSUPPORTED, "%lld sequences are more than 65535", (long long)qs->sequences);          // (a dimension of a grid)
+    return LORANN_OK;
+}
+
+template <int D, int BITS>
+void launch_weights(const WeightPlan& p, const WeightArgs& w, int32_t type, hipStream_t stream) {
+    const AttendArgs& a = w.a;
+    const dim3 grid((unsigned)(p.tiles * a.st.heads * a.splits));
+    if (!p.many) {
+        if (type == LORANN_F16) hipLaunchKernelGGL((k_weights_scores<_Float16, D, BITS>), grid, dim3(64 * kAttendWaves), 0, stream, w);
+        else hipLaunchKernelGGL((k_weights_scores<__bf16, D, BITS>), grid, dim3(64 * kAttendWaves), 0, stream, w);
+        return;
+    }
+    const dim3 queries((unsigned)p.tiles32, (unsigned)a.st.heads);
+    if (type == LORANN_F16) hipLaunchKernelGGL((k_weights_queries<_Float16, D>), queries, dim3(64), 0, stream, w);
+    else hipLaunchKernelGGL((k_weights_queries<__bf16, D>), queries, dim3(64), 0, stream, w);
+    hipLaunchKernelGGL((k_weights_rows<D, BITS>), grid, dim3(256), 0, stream, w);
+    if (a.splits > 1) hipLaunchKernelGGL(k_weights_join, dim3((unsigned)ceil_div(a.st.heads * w.padded, 256)), dim3(256), 0, stream, w);
+    const bool share = ceil_div(w.keys, 256) * a.st.heads * a.sequences < kBlocksWanted;
+    const dim3 chunks((unsigned)ceil_div(w.keys, share ? 64 : 256), (unsigned)a.st.heads, (unsigned)a.sequences);
+    if (share) hipLaunchKernelGGL((k_weights_keys<D, BITS, true>), chunks, dim3(256), 0, stream, w);
+    else hipLaunchKernelGGL((k_weights_keys<D, BITS, false>), chunks, dim3(256), 0, stream, w);
+}
+
+template <typename St>
+int attend_weights(const St* st, const lorann_questions* qs, const int32_t* tables, int32_t width, const int32_t* lengths, const float* before, float* sums,
+                   void* workspace, int64_t workspace_bytes, hipStream_t stream) {
+    constexpr int bits = std::is_same_v<St, lorann_states4> ? 4 : 8;
+    int rc, gpu = -1;
+    if ((rc = check_weights(st, qs, width))) return rc;
+    if (qs->sequences == 0 || width == 0) return LORANN_OK;
+    if (!qs->q_start && qs->tokens % qs->sequences) return fail(LORANN_E_INVAL, "%lld tokens do not divide over %lld sequences", (long long)qs->tokens, (long long)qs->sequences);
+    if ((rc = check_store(st, gpu))) return rc;
+    if (qs->tokens > 0) {
+        if ((rc = check_device(qs->q, "q", gpu))) return rc;
+        if (!aligned(qs->q, 2)) return fail(LORANN_E_INVAL, "q is not aligned to its type");
+        if (qs->q_start && (rc = check_device(qs->q_start, "q_start", gpu))) return rc;
+    }
+    if ((rc = check_device(tables, "tables", gpu)) || (rc = check_device(lengths, "lengths", gpu))) return rc;
+    if ((before && (rc = check_device(before, "before", gpu))) || (rc = check_device(sums, "sums", gpu))) return rc;
+    if (!aligned(before, 4) || !aligned(sums, 4)) return fail(LORANN_E_INVAL, "before or sums is not 4-byte aligned");
+    WeightPlan p = weight_plan(st, qs, width);
+    const int64_t blocks = p.tiles * st->heads * p.splits;
+    if (p.tiles > 0x7fffffff || blocks > 0xffffffffLL / 256) return fail(LORANN_E_UNSUPPORTED, "%lld tokens of %lld sequences are more than one launch holds", (long long)qs->tokens, (long long)qs->sequences);
+    if (p.workspace) {
+        if (!workspace || workspace_bytes < p.workspace) return fail(LORANN_E_INVAL, "the workspace holds %lld bytes, %lld are needed", (long long)(workspace ? workspace_bytes : 0), (long long)p.workspace);
+        if (!aligned(workspace, 16)) return fail(LORANN_E_INVAL, "the workspace is not 16-byte aligned");
+        if ((rc = check_device(workspace, "workspace", gpu))) return rc;
+    }
+    WeightArgs w{};
+    AttendArgs& a = w.a;
+    a.st = view(st);
+    a.q = qs->q;
+    a.q_token = qs->q_token; a.q_head = qs->q_head;
+    a.tokens = qs->tokens; a.sequences = (int32_t)qs->sequences; a.group = qs->heads / st->heads;
+    a.q_start = qs->tokens > 0 ? qs->q_start : nullptr;
+    a.c = qs->scale * 1.44269504088896341f;
+    a.tables = tables; a.width = width; a.lengths = lengths;
+    a.found = 1;
+    a.unit = p.unit; a.units = a.splits = p.splits; a.per_split = 1;
+    a.q_wide = aligned(qs->q, 16) && qs->q_token % 8 == 0 && qs->q_head % 8 == 0;
+    w.before = before; w.sums = sums; w.keys = (int64_t)width * st->page_size; w.row_keys = p.row_keys; w.padded = p.padded;
+    char* at = (char*)workspace;
+    if (p.many) {
+        w.q16 = (f16x8*)at;
+        at += p.q16;
+        w.back = (float*)at;
+        w.row_m = w.back + p.padded * st->heads;
+        w.row_inv = w.row_m + p.padded * st->heads;
+        at += p.rows;
+    } else {
+        w.y = (float*)at;
+        at += p.y;
+    }
+    a.part_m = (float*)at;
+    a.part_l = a.part_m + p.parts / 8;
+    if (qs->tokens > 0) {
+        switch (st->dim) {
+            case 32: launch_weights<32, bits>(p, w, qs->type, stream); break;
+            case 64: launch_weights<64, bits>(p, w, qs->type, stream); break;
+            case 96: launch_weights<96, bits>(p, w, qs->type, stream); break;
+            default: launch_weights<128, bits>(p, w, qs->type, stream); break;
+        }
+    }
+    if (qs->tokens == 0 || !p.many) hipLaunchKernelGGL(k_weights_add, dim3((unsigned)ceil_div(w.keys, kAddKeys), (unsigned)st->heads, (unsigned)qs->sequences), dim3(256), 0, stream, w);
+    HIP_TRY(hipGetLastError());
+    return LORANN_OK;
+}
+
+template <typename St>
+int64_t attend_weights_workspace(const St* st, const lorann_questions* qs, int32_t width) {
+    int rc;
+    if ((rc = check_weights(st, qs, width))) return rc;
+    if (qs->sequences == 0 || width == 0 || qs->tokens == 0) return 0;
+    return weight_plan(st, qs, width).workspace;
+}
+
+template <typename St>
+int evict(const St* st, const int32_t* tables, int32_t width, const int32_t* lengths, int64_t sequences, const float* sums, int32_t budget, int32_t recent, const int32_t* to_tables,
+          int32_t to_width, int32_t* kept, int32_t* kept_lengths, float* kept_sums, void* workspace, int64_t workspace_bytes, hipStream_t stream) {
+    constexpr int bits = std::is_same_v<St, lorann_states4> ? 4 : 8;
+    int rc, gpu = -1;
+    if ((rc = check_sizes(st))) return rc;
+    if (sequences < 0 || width < 0 || to_width < 0) return fail(LORANN_E_INVAL, "%lld sequences, tables of width %d and %d", (long long)sequences, width, to_width);
+    if (sequences > 65535) return fail(LORANN_E_UNSUPPORTED, "%lld sequences are more than 65535", (long long)sequences);
+    if (budget < 0 || recent < 0 || recent > budget) return fail(LORANN_E_INVAL, "a budget of %d tokens, %d of them the newest", budget, recent);
+    if ((int64_t)width * st->page_size > (1 << 30) || (int64_t)to_width * st->page_size > (1 << 30))
+        return fail(LORANN_E_UNSUPPORTED, "tables of %d and %d pages of %d tokens are longer than 2^30 tokens", width, to_width, st->page_size);
+    if ((int64_t)to_width * st->page_size < budget) return fail(LORANN_E_INVAL, "destinations of %d pages hold no %d tokens", to_width, budget);
+    if (sequences == 0) return LORANN_OK;
+    if ((rc = check_store(st, gpu))) return rc;
+    if (width > 0 && ((rc = check_device(tables, "tables", gpu)) || (rc = check_device(sums, "sums", gpu)))) return rc;
+    if ((rc = check_device(lengths, "lengths", gpu)) || (rc = check_device(kept_lengths, "kept_lengths", gpu))) return rc;
+    if (budget > 0 && ((rc = check_device(to_tables, "to_tables", gpu)) || (rc = check_device(kept, "kept", gpu)))) return rc;
+    if (kept_sums && to_width > 0 && (rc = check_device(kept_sums, "kept_sums", gpu))) return rc;
+    if (!aligned(sums, 4) || !aligned(kept, 4) || !aligned(kept_lengths, 4) || !aligned(kept_sums, 4)) return fail(LORANN_E_INVAL, "an array is not 4-byte aligned");
+    (void)workspace; (void)workspace_bytes;
+    EvictArgs a{};
+    a.st = view(st);
+    a.tables = tables; a.width = width; a.lengths = lengths; a.sums = sums; a.keys = (int64_t)width * st->page_size;
+    a.budget = budget; a.recent = recent; a.to_tables = to_tables; a.to_width = to_width;
+    a.kept = kept; a.kept_lengths = kept_lengths; a.kept_sums = to_width > 0 ? kept_sums : nullptr;
+    hipLaunchKernelGGL(k_evict_choose, dim3((unsigned)(sequences * st->heads)), dim3(kChooseThreads), 0, stream, a);
+    const int64_t tokens = kept_sums ? (int64_t)to_width * st->page_size : budget;
+    if (tokens > 0) hipLaunchKernelGGL((k_evict_move<bits>), dim3((unsigned)ceil_div(tokens, 64), (unsigned)st->heads, (unsigned)sequences), dim3(256), 0, stream, a, st->dim);
+    HIP_TRY(hipGetLastError());
+    return LORANN_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int lorann_attend_weights(const lorann_states* st, const lorann_questions* qs, const int32_t* tables, int32_t width, const int32_t* lengths,
+                          const float* before, float* sums, void* workspace, int64_t workspace_bytes, void* hip_stream) {
+    return attend_weights(st, qs, tables, width, lengths, before, sums, workspace, workspace_bytes, (hipStream_t)hip_stream);
+}
+
+int lorann_attend4_weights(const lorann_states4* st, const lorann_questions* qs, const int32_t* tables, int32_t width, const int32_t* lengths,
+                           const float* before, float* sums, void* workspace, int64_t workspace_bytes, void* hip_stream) {
+    return attend_weights(st, qs, tables, width, lengths, before, sums, workspace, workspace_bytes, (hipStream_t)hip_stream);
+}
+
+int64_t lorann_attend_weights_workspace(const lorann_states* st, const lorann_questions* qs, int32_t width) { return attend_weights_workspace(st, qs, width); }
+
+int64_t lorann_attend4_weights_workspace(const lorann_states4* st, const lorann_questions* qs, int32_t width) { return attend_weights_workspace(st, qs, width); }
+
+int lorann_states_evict(const lorann_states* st, const int32_t* tables, int32_t width, const int32_t* lengths, int64_t sequences, const float* sums, int32_t budget, int32_t recent,
+                        const int32_t* to_tables, int32_t to_width, int32_t* kept, int32_t* kept_lengths, float* kept_sums, void* workspace, int64_t workspace_bytes, void* hip_stream) {
+    return evict(st, tables, width, lengths, sequences, sums, budget, recent, to_tables, to_width, kept, kept_lengths, kept_sums, workspace, workspace_bytes, (hipStream_t)hip_stream);
+}
+
+int lorann_states4_evict(const lorann_states4* st, const int32_t* tables, int32_t width, const int32_t* lengths, int64_t sequences, const float* sums, int32_t budget, int32_t recent,
+                         const int32_t* to_tables, int32_t to_width, int32_t* kept, int32_t* kept_lengths, float* kept_sums, void* workspace, int64_t workspace_bytes, void* hip_stream) {
+    return evict(st, tables, width, lengths, sequences, sums, budget, recent, to_tables, to_width, kept, kept_lengths, kept_sums, workspace, workspace_bytes, (hipStream_t)hip_stream);
+}
+
+int64_t lorann_evict_workspace(int32_t heads, int64_t table_tokens, int64_t sequences) {
+    if (heads < 1 || table_tokens < 0 || sequences < 0) return fail(LORANN_E_INVAL, "%d heads, tables of %lld tokens, %lld sequences", heads, (long long)table_tokens, (long long)sequences);
+    return 0;
+}
+
+}  // extern "C"

@@ -1,4 +1,4 @@
-"""Binding of the state store and its attention (include/lorann_states.h): argument marshalling only, everything runs inside the HIP library.
+"""Binding of the state store and its attention (include/lorann_states.h), and of eviction from it (include/lorann_evict.h): argument marshalling only, everything runs inside the HIP library.
 
 Tensors live on the GPU and are handed over as pointers with their strides; nothing is copied or converted here, a tensor of another type or
 layout than asked for is refused.  Work is enqueued on torch's current stream of the current device and the calls return.
@@ -17,6 +17,9 @@ from .binding import LorannError, lib as _base_lib
 F32, F16, BF16 = 0, 1, 2
 MIN_PAGE, MAX_PAGE, MAX_DIM, MAX_HEADS, MAX_FOUND = 16, 256, 128, 1024, 4096
 EXPORTS = ["lorann_states_write", "lorann_states_read", "lorann_attend_chunk", "lorann_attend_passages", "lorann_attend_workspace"]
+
+EVICT_EXPORTS = ["lorann_attend_weights", "lorann_attend4_weights", "lorann_attend_weights_workspace", "lorann_attend4_weights_workspace", "lorann_states_evict", "lorann_states4_evict",
+                 "lorann_evict_workspace"]
 
 _TYPE = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}
 
@@ -50,9 +53,13 @@ def lib() -> C.CDLL:
                                        (f"lorann_states{bits}_read", C.c_int, [st, vp, i64, vp, vp, i32, i64, i64, i64, i64, vp]),
                                        (f"lorann_attend{bits}_chunk", C.c_int, [st, qs, vp, i32, vp, vp, i64, vp]),
                                        (f"lorann_attend{bits}_passages", C.c_int, [st, qs, vp, i32, vp, C.c_float, vp, i32, vp, i64, vp, i64, vp]),
-                                       (f"lorann_attend{bits}_workspace", C.c_int64, [st, qs, i32, i32])):
+                                       (f"lorann_attend{bits}_workspace", C.c_int64, [st, qs, i32, i32]),
+                                       (f"lorann_attend{bits}_weights", C.c_int, [st, qs, vp, i32, vp, vp, vp, vp, i64, vp]),
+                                       (f"lorann_attend{bits}_weights_workspace", C.c_int64, [st, qs, i32]),
+                                       (f"lorann_states{bits}_evict", C.c_int, [st, vp, i32, vp, i64, vp, i32, i32, vp, i32, vp, vp, vp, vp, i64, vp])):
                 f = getattr(L, name)
                 f.restype, f.argtypes = result, args
+        L.lorann_evict_workspace.restype, L.lorann_evict_workspace.argtypes = i64, [i32, i64, i64]
         _lib = L
     return _lib
 
@@ -105,7 +112,8 @@ class States:
     k_scales  [pages, heads, page_size] float32         v_scales  the same
     The tensors stay the caller's; slot = page * page_size + place in the page."""
 
-    _call = dict(write="lorann_states_write", read="lorann_states_read", chunk="lorann_attend_chunk", passages="lorann_attend_passages", workspace="lorann_attend_workspace")
+    _call = dict(write="lorann_states_write", read="lorann_states_read", chunk="lorann_attend_chunk", passages="lorann_attend_passages", workspace="lorann_attend_workspace",
+                 weights="lorann_attend_weights", weights_workspace="lorann_attend_weights_workspace", evict="lorann_states_evict")
 
     def __init__(self, k_codes, v_codes, k_scales, v_scales):
         self.k_codes, self.v_codes, self.k_scales, self.v_scales = k_codes, v_codes, k_scales, v_scales
@@ -193,11 +201,14 @@ class States:
                           None if q_start is None else _array(q_start, torch.int32, (sequences + 1,), "q_start"), dim ** -0.5 if scale is None else scale), out
 
     def _workspace(self, qs, found, width, workspace):
+        return self._room(workspace, lambda: self._run("workspace")(self._st, qs, found, width))
+
+    def _room(self, workspace, needed):
         if workspace is not None:
             if not workspace.is_contiguous():          # (its size would not be the memory it has)
                 raise ValueError("workspace must be contiguous")
             return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
-        need = self._run("workspace")(self._st, qs, found, width)
+        need = needed()
         if need < 0:
             _raise(need)
         if not need:
@@ -245,3 +256,63 @@ class States:
         if rc:
             _raise(rc)
         return _no_gradient(out, q, scores) if q.requires_grad or (scores is not None and scores.requires_grad) else out
+
+    def _weight_questions(self, q, q_start, sequences, scale):
+        tokens, heads, dim = q.shape
+        if dim != self.dim:
+            raise ValueError(f"q must be [tokens, heads, {self.dim}], got {tuple(q.shape)}")
+        qt, qh = _strides(q, "q")
+        return CQuestions(q.data_ptr(), None, _TYPE.get(q.dtype, -1), heads, tokens, sequences, qt, qh, 0, 0,
+                          None if q_start is None else _array(q_start, torch.int32, (sequences + 1,), "q_start"), dim ** -0.5 if scale is None else scale)
+
+    def weights_workspace_bytes(self, q, sequences: int, width: int, ragged: bool = False) -> int:
+        """Bytes of `workspace` that attend_weights with these queries and sizes needs (ragged: with q_start)."""
+        qs = CQuestions(None, None, _TYPE.get(q.dtype, -1), q.shape[1], q.shape[0], sequences, 0, 0, 0, 0, 1 if ragged else None, 1.0)
+        need = self._run("weights_workspace")(self._st, qs, width)
+        if need < 0:
+            _raise(need)
+        return need
+
+    def attend_weights(self, q, tables, lengths, q_start=None, scale=None, before=None, out=None, workspace=None):
+        """The weight that attend_chunk with the same arguments gives each key, added up over a sequence's queries and the query heads of each head.
+
+        before [sequences, heads, width * page_size] float32: what the sums start from (None: zeros).  Returns out (may be `before`), the same shape."""
+        n, width = tables.shape
+        qs = self._weight_questions(q, q_start, n, scale)
+        shape = (n, self.heads, width * self.page_size)
+        if out is None:
+            out = torch.empty(shape, dtype=torch.float32, device=self.k_codes.device)
+        ws, size, keep = self._room(workspace, lambda: self._run("weights_workspace")(self._st, qs, width))
+        rc = self._run("weights")(self._st, qs, _array(tables, torch.int32, (n, width), "tables"), width, _array(lengths, torch.int32, (n,), "lengths"),
+                                  None if before is None else _array(before, torch.float32, shape, "before"), _array(out, torch.float32, shape, "out"), ws, size, self._stream())
+        if rc:
+            _raise(rc)
+        return _no_gradient(out, q, before) if q.requires_grad or (before is not None and before.requires_grad) else out
+
+    def evict_workspace_bytes(self, sequences: int, width: int) -> int:
+        """Bytes of `workspace` that evict with tables of these sizes needs."""
+        need = lib().lorann_evict_workspace(self.heads, width * self.page_size, sequences)
+        if need < 0:
+            _raise(need)
+        return need
+
+    def evict(self, tables, lengths, sums, budget: int, to_tables, recent: int = 0, out=None, workspace=None):
+        """Keeps of every sequence and head `budget` keys - the last `recent` ones, then those with the largest sums - and copies their states, in order, to the pages of `to_tables`.
+
+        tables [sequences, width] and lengths [sequences] int32; sums [sequences, heads, width * page_size] float32 (attend_weights); to_tables [sequences, to_width] int32, pages
+        that are none of `tables`.  Returns (kept [sequences, heads, budget] int32: numbers of the keys, -1 behind the last; lengths [sequences] int32; sums [sequences, heads,
+        to_width * page_size] float32 of the kept keys), or writes to the three tensors of `out`."""
+        n, width = tables.shape
+        to_width = to_tables.shape[1]
+        shapes = (n, self.heads, budget), (n,), (n, self.heads, to_width * self.page_size)
+        if out is None:
+            out = tuple(torch.empty(s, dtype=t, device=self.k_codes.device) for s, t in zip(shapes, (torch.int32, torch.int32, torch.float32)))
+        kept, left, kept_sums = out
+        ws, size, keep = self._room(workspace, lambda: lib().lorann_evict_workspace(self.heads, width * self.page_size, n))
+        rc = self._run("evict")(self._st, _array(tables, torch.int32, (n, width), "tables"), width, _array(lengths, torch.int32, (n,), "lengths"), n,
+                                _array(sums, torch.float32, (n, self.heads, width * self.page_size), "sums"), budget, recent,
+                                _array(to_tables, torch.int32, (n, to_width), "to_tables"), to_width, _array(kept, torch.int32, shapes[0], "out[0]"),
+                                _array(left, torch.int32, shapes[1], "out[1]"), _array(kept_sums, torch.float32, shapes[2], "out[2]"), ws, size, self._stream())
+        if rc:
+            _raise(rc)
+        return kept, left, kept_sums
