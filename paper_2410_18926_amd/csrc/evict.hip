@@ -146,6 +146,14 @@ int64_t attend_weights_workspace(const St* st, const lorann_questions* qs, int32
     return weight_plan(st, qs, width).workspace;
 }
 
+// Tables whose keys fit a block's registers (16 a thread) are chosen from in one launch, longer ones in chunks.
+constexpr int64_t kChooseKeys = 16 * kChooseThreads;
+int64_t evict_chunks(int64_t keys) { return ceil_div(keys, kChunk); }
+int64_t evict_room(int64_t seats, int64_t keys) {
+    if (keys <= kChooseKeys) return 0;
+    return ceil_div(seats * evict_chunks(keys) * (2 * kBins + 1) * 4 + seats * 16, 16) * 16;
+}
+
 template <typename St>
 int evict(const St* st, const int32_t* tables, int32_t width, const int32_t* lengths, int64_t sequences, const float* sums, int32_t budget, int32_t recent, const int32_t* to_tables,
           int32_t to_width, int32_t* kept, int32_t* kept_lengths, float* kept_sums, void* workspace, int64_t workspace_bytes, hipStream_t stream) {
@@ -165,14 +173,40 @@ int evict(const St* st, const int32_t* tables, int32_t width, const int32_t* len
     if (budget > 0 && ((rc = check_device(to_tables, "to_tables", gpu)) || (rc = check_device(kept, "kept", gpu)))) return rc;
     if (kept_sums && to_width > 0 && (rc = check_device(kept_sums, "kept_sums", gpu))) return rc;
     if (!aligned(sums, 4) || !aligned(kept, 4) || !aligned(kept_lengths, 4) || !aligned(kept_sums, 4)) return fail(LORANN_E_INVAL, "an array is not 4-byte aligned");
-    (void)workspace; (void)workspace_bytes;
+    const int64_t seats = sequences * st->heads, keys = (int64_t)width * st->page_size, room = evict_room(seats, keys), chunks = evict_chunks(keys);
+    const int64_t tokens = kept_sums ? (int64_t)to_width * st->page_size : budget;
+    if (seats * (room ? chunks : 1) > 0xffffffffLL / kChooseThreads || ceil_div(tokens, 64) > 0xffffffffLL / 256)       // (threads of a grid)
+        return fail(LORANN_E_UNSUPPORTED, "%lld sequences of %d heads, tables of %lld tokens are more than one launch holds", (long long)sequences, st->heads, (long long)keys);
+    if (room) {
+        if (!workspace || workspace_bytes < room) return fail(LORANN_E_INVAL, "the workspace holds %lld bytes, %lld are needed", (long long)(workspace ? workspace_bytes : 0), (long long)room);
+        if (!aligned(workspace, 16)) return fail(LORANN_E_INVAL, "the workspace is not 16-byte aligned");
+        if ((rc = check_device(workspace, "workspace", gpu))) return rc;
+    }
     EvictArgs a{};
     a.st = view(st);
-    a.tables = tables; a.width = width; a.lengths = lengths; a.sums = sums; a.keys = (int64_t)width * st->page_size;
+    a.tables = tables; a.width = width; a.lengths = lengths; a.sums = sums; a.keys = keys;
     a.budget = budget; a.recent = recent; a.to_tables = to_tables; a.to_width = to_width;
     a.kept = kept; a.kept_lengths = kept_lengths; a.kept_sums = to_width > 0 ? kept_sums : nullptr;
-    hipLaunchKernelGGL(k_evict_choose, dim3((unsigned)(sequences * st->heads)), dim3(kChooseThreads), 0, stream, a);
-    const int64_t tokens = kept_sums ? (int64_t)to_width * st->page_size : budget;
+    const bool wide = aligned(sums, 16);
+    if (!room) {
+        const dim3 grid((unsigned)seats), block(kChooseThreads);
+        if (keys <= 4 * kChooseThreads) hipLaunchKernelGGL(k_evict_choose<4>, grid, block, 0, stream, a, wide);
+        else if (keys <= 8 * kChooseThreads) hipLaunchKernelGGL(k_evict_choose<8>, grid, block, 0, stream, a, wide);
+        else hipLaunchKernelGGL(k_evict_choose<16>, grid, block, 0, stream, a, wide);
+    } else {
+        ChunkArgs c{};
+        c.a = a;
+        c.chunks = (int32_t)chunks;
+        c.hist[0] = (uint32_t*)workspace;
+        c.hist[1] = c.hist[0] + seats * chunks * kBins;
+        c.place = c.hist[1] + seats * chunks * kBins;
+        c.state = c.place + seats * chunks;
+        const dim3 grid((unsigned)(seats * chunks)), block(kChooseThreads);
+        hipLaunchKernelGGL(k_evict_chunks<0>, grid, block, 0, stream, c, wide);
+        hipLaunchKernelGGL(k_evict_chunks<1>, grid, block, 0, stream, c, wide);
+        hipLaunchKernelGGL(k_evict_chunks<2>, grid, block, 0, stream, c, wide);
+        hipLaunchKernelGGL(k_evict_chunks<3>, grid, block, 0, stream, c, wide);
+    }
     if (tokens > 0) hipLaunchKernelGGL((k_evict_move<bits>), dim3((unsigned)ceil_div(tokens, 64), (unsigned)st->heads, (unsigned)sequences), dim3(256), 0, stream, a, st->dim);
     HIP_TRY(hipGetLastError());
     return LORANN_OK;
@@ -208,7 +242,8 @@ int lorann_states4_evict(const lorann_states4* st, const int32_t* tables, int32_
 
 int64_t lorann_evict_workspace(int32_t heads, int64_t table_tokens, int64_t sequences) {
     if (heads < 1 || table_tokens < 0 || sequences < 0) return fail(LORANN_E_INVAL, "%d heads, tables of %lld tokens, %lld sequences", heads, (long long)table_tokens, (long long)sequences);
-    return 0;
+    if (table_tokens > 1 << 30 || sequences > 65535) return fail(LORANN_E_UNSUPPORTED, "tables of %lld tokens, %lld sequences", (long long)table_tokens, (long long)sequences);
+    return evict_room(heads * sequences, table_tokens);
 }
 
 }  // extern "C"

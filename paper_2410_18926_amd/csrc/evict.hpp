@@ -21,8 +21,11 @@ struct EvictArgs {
 // Larger sums first; -0 and +0 are alike, a NaN comes after every number.
 __device__ __forceinline__ uint32_t sum_key(float x) { return x != x ? 0u : float_key_asc(x); }
 
+// The choice.  The threshold - the key of the last sum that is still kept - is found 11, 11 and 10 bits at a time from histograms of the old keys' sums (eleven bits spread a run of
+// exponents over many bins: with eight, most lanes of a wavefront add to one bin and wait for each other); keys above it are kept, and of those that equal it the first.
 constexpr int kChooseThreads = 1024, kChooseWaves = kChooseThreads / 64;
-constexpr int kEach = 4;               // consecutive keys of a thread
+constexpr int kBins = 2048, kBinsEach = kBins / kChooseThreads;
+constexpr int kShift[3] = {21, 10, 0}, kBits[3] = {11, 11, 10};
 
 __device__ __forceinline__ uint32_t wave_prefix_u32(uint32_t v) {          // sum of the lanes up to and with this one
 #pragma unroll
@@ -50,100 +53,248 @@ __device__ __forceinline__ uint32_t block_prefix(uint32_t v, uint32_t* lds, uint
     return before + upto - v;
 }
 
-// A block chooses for one sequence and head.  The threshold - the key of the last sum that is still kept - is found a byte at a time from histograms; keys above it are kept, and of those
-// that equal it the first.
-__global__ void __launch_bounds__(kChooseThreads) k_evict_choose(EvictArgs a) {
-    __shared__ uint32_t hist[kChooseWaves][256];
-    __shared__ uint32_t part[kChooseWaves];
-    __shared__ uint32_t found[3];
-    const int tid = threadIdx.x, wave = tid >> 6, s = blockIdx.x / a.st.heads, head = blockIdx.x - s * a.st.heads;
-    const int n = (int)min((int64_t)max(a.lengths[s], 0), a.keys), old = max(n - a.recent, 0), P = 1 << a.st.shift;
-    const int32_t* pages = a.tables + (int64_t)s * a.width;
-    const float* sums = a.sums + ((int64_t)s * a.st.heads + head) * a.keys;
-    int32_t* kept = a.kept + ((int64_t)s * a.st.heads + head) * a.budget;
-    auto there = [&](int j) { return (uint32_t)pages[j >> a.st.shift] < (uint64_t)a.st.pages; };
-    // how many keys there are, and of them old ones
-    uint32_t all, olds;
-    {
+// A sequence and head: where its arrays are, how long it is.
+struct Seat {
+    int s, head, n, old;
+    const int32_t* pages;
+    const float* sums;
+    int32_t* kept;
+
+    __device__ __forceinline__ Seat(const EvictArgs& a, int seat) {
+        s = seat / a.st.heads;
+        head = seat - s * a.st.heads;
+        n = (int)min((int64_t)max(a.lengths[s], 0), a.keys);
+        old = max(n - a.recent, 0);
+        pages = a.tables + (int64_t)s * a.width;
+        sums = a.sums + (int64_t)seat * a.keys;
+        kept = a.kept + (int64_t)seat * a.budget;
+    }
+    __device__ __forceinline__ bool there(const EvictArgs& a, int j) const { return (uint32_t)pages[j >> a.st.shift] < (uint64_t)a.st.pages; }
+};
+
+// How many keys of a sequence there are and how many are to be chosen from the old ones.
+struct Wanted {
+    uint32_t all, olds, want, choose;
+    __device__ __forceinline__ Wanted(const EvictArgs& a, const Seat& q, uint32_t* lds) {
         uint32_t mine = 0, mine_old = 0;
-        for (int p = tid; p << a.st.shift < n; p += kChooseThreads) {
+        const int P = 1 << a.st.shift;
+        for (int p = threadIdx.x; (int64_t)p << a.st.shift < q.n; p += kChooseThreads) {
             const int j = p << a.st.shift;
-            if (there(j)) {
-                mine += min(P, n - j);
-                mine_old += min(P, max(old - j, 0));
+            if (q.there(a, j)) {
+                mine += min(P, q.n - j);
+                mine_old += min(P, max(q.old - j, 0));
             }
         }
-        block_prefix(mine, part, all);
-        block_prefix(mine_old, part, olds);
+        block_prefix(mine, lds, all);
+        block_prefix(mine_old, lds, olds);
+        want = min(all, (uint32_t)a.budget);
+        choose = want - min(all - olds, want);                  // (recent <= budget: the newest are at most `want`)
     }
-    const uint32_t want = min(all, (uint32_t)a.budget), newest = all - olds;
-    const uint32_t choose = want - min(newest, want);           // of the old ones (recent <= budget: newest <= want)
-    uint32_t threshold = 0, equal = choose;                     // choose = all of them: every key is >= 0
-    if (choose > 0 && choose < olds) {
-        uint32_t rank = choose;                                 // among those that begin with `threshold`
-#pragma unroll 1
-        for (int shift = 24; shift >= 0; shift -= 8) {
-            for (int i = tid; i < kChooseWaves * 256; i += kChooseThreads) ((uint32_t*)hist)[i] = 0;
-            __syncthreads();
-            const uint32_t mask = shift == 24 ? 0u : ~0u << (shift + 8);
-            for (int j = tid; j < old; j += kChooseThreads) {
-                if (!there(j)) continue;
-                const uint32_t key = sum_key(sums[j]);
-                if ((key & mask) == threshold) atomicAdd(&hist[wave][key >> shift & 255u], 1u);
-            }
-            __syncthreads();
-            uint32_t mine = 0;                                  // bin 255 - tid: the largest come first
-            if (tid < 256)
+};
+
+// A thread's EACH consecutive keys from j0 on: the sums' keys, and bits of those that are old or new (none: not there).
+template <int EACH>
+struct Mine {
+    uint32_t key[EACH];
+    uint32_t old, fresh;
+    __device__ __forceinline__ Mine(const EvictArgs& a, const Seat& q, int64_t j0, bool wide) {
+        old = fresh = 0;
+        float x[EACH];
+        if (wide && j0 + EACH <= a.keys) {                      // (16-byte rows: requested together)
 #pragma unroll
-                for (int w = 0; w < kChooseWaves; ++w) mine += hist[w][255 - tid];
-            uint32_t total;
-            const uint32_t above = block_prefix(mine, part, total);
-            if (tid < 256 && above < rank && rank <= above + mine) { found[0] = 255 - tid; found[1] = above; }
-            __syncthreads();
-            threshold |= found[0] << shift;
-            rank -= found[1];
-            __syncthreads();
+            for (int i = 0; i < EACH; i += 4) {
+                const f32x4 v = *(const f32x4*)(q.sums + j0 + i);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) x[i + k] = v[k];
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < EACH; ++i) x[i] = j0 + i < a.keys ? q.sums[j0 + i] : 0.0f;
         }
-        equal = rank;
-    } else if (choose == 0) {
-        threshold = ~0u;                                        // (no sum has this key: it would be a NaN's)
-        equal = 0;
+        // (EACH divides a page or is 16, a page's least: the thread's keys stand on one)
+        const bool there = j0 < q.n && q.there(a, (int)j0);
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            key[i] = sum_key(x[i]);
+            if (there && j0 + i < q.old) old |= 1u << i;
+            else if (there && j0 + i < q.n) fresh |= 1u << i;
+        }
     }
-    // in order
-    uint32_t kept_before = 0, equal_before = 0;
-    for (int j0 = 0; j0 < n; j0 += kChooseThreads * kEach) {
-        uint32_t keep = 0, same = 0;                            // bits of the thread's keys
+    // Adds the next bits of old keys that agree with the threshold so far.
+    __device__ __forceinline__ void count(uint32_t* hist, int pass, uint32_t threshold) const {
+        const uint32_t mask = pass == 0 ? 0u : ~0u << kShift[pass - 1];
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            const int j = j0 + tid * kEach + i;
-            if (j >= n || !there(j)) continue;
-            if (j >= old) keep |= 1u << i;
-            else {
-                const uint32_t key = sum_key(sums[j]);
-                if (key > threshold) keep |= 1u << i;
-                else if (key == threshold) same |= 1u << i;
+        for (int i = 0; i < EACH; ++i)
+            if (old >> i & 1u && (key[i] & mask) == threshold) atomicAdd(&hist[key[i] >> kShift[pass] & ((1u << kBits[pass]) - 1)], 1u);
+    }
+    // Writes the kept ones: `above` kept and `same` equal ones come before the block's.
+    __device__ __forceinline__ void write(const Seat& q, int64_t j0, uint32_t threshold, uint32_t equal, uint32_t above, uint32_t same, uint32_t* lds) const {
+        uint32_t keep = fresh, is = 0;
+#pragma unroll
+        for (int i = 0; i < EACH; ++i)
+            if (old >> i & 1u) {
+                if (key[i] > threshold) keep |= 1u << i;
+                else if (key[i] == threshold) is |= 1u << i;
             }
-        }
         uint32_t total;
-        const uint32_t counts = (uint32_t)__popc(keep) | (uint32_t)__popc(same) << 16;
-        const uint32_t before = block_prefix(counts, part, total);
-        uint32_t eq = equal_before + (before >> 16);            // equal ones before the thread's
-        uint32_t at = kept_before + (before & 0xffffu) + min(eq, equal);
+        const uint32_t before = block_prefix((uint32_t)__popc(keep) | (uint32_t)__popc(is) << 16, lds, total);
+        uint32_t eq = same + (before >> 16), at = above + (before & 0xffffu) + min(eq, equal);
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            const bool is = same >> i & 1u;
-            if (keep >> i & 1u || (is && eq < equal)) kept[at++] = j0 + tid * kEach + i;
-            eq += is;
+        for (int i = 0; i < EACH; ++i) {
+            const bool e = is >> i & 1u;
+            if (keep >> i & 1u || (e && eq < equal)) q.kept[at++] = (int)j0 + i;
+            eq += e;
         }
-        kept_before += total & 0xffffu;
-        equal_before += total >> 16;
     }
-    for (int i = (int)want + tid; i < a.budget; i += kChooseThreads) kept[i] = -1;
-    if (head == 0 && tid == 0) a.kept_lengths[s] = (int)want;
+};
+
+// Of the thread's bins (the largest first: thread t has bins kBins - 1 - kBinsEach t and the ones below), which one the rank falls into.  Returns that bin and how many keys are above it.
+__device__ __forceinline__ void find_bin(const uint32_t (&mine)[kBinsEach], uint32_t rank, uint32_t* lds, uint32_t* found, uint32_t& bin, uint32_t& above) {
+    uint32_t sum = 0, total;
+#pragma unroll
+    for (int i = 0; i < kBinsEach; ++i) sum += mine[i];
+    uint32_t upto = block_prefix(sum, lds, total);
+#pragma unroll
+    for (int i = 0; i < kBinsEach; ++i) {
+        if (upto < rank && rank <= upto + mine[i]) { found[0] = kBins - 1 - kBinsEach * threadIdx.x - i; found[1] = upto; }
+        upto += mine[i];
+    }
+    __syncthreads();
+    bin = found[0];
+    above = found[1];
+    __syncthreads();
+}
+
+// Tables of up to 1024 EACH keys: a block does it all for a sequence and head, keys in registers.  32 sequences of up to 6000 keys of 8 heads: bound by the latency of its steps.
+template <int EACH>
+__global__ void __launch_bounds__(kChooseThreads) k_evict_choose(EvictArgs a, bool wide) {
+    __shared__ uint32_t hist[kBins], part[kChooseWaves], found[2];
+    const Seat q(a, blockIdx.x);
+    const int64_t j0 = (int64_t)threadIdx.x * EACH;
+    const Mine<EACH> mine(a, q, j0, wide);
+    const Wanted w(a, q, part);
+    uint32_t threshold = 0, equal = w.choose;                   // all of the old ones: every key is >= 0
+    if (w.choose == 0) threshold = ~0u;                         // (no sum has this key: it would be a NaN's)
+    else if (w.choose < w.olds) {
+#pragma unroll
+        for (int pass = 0; pass < 3; ++pass) {
+#pragma unroll
+            for (int i = 0; i < kBinsEach; ++i) hist[threadIdx.x + i * kChooseThreads] = 0;
+            __syncthreads();
+            mine.count(hist, pass, threshold);
+            __syncthreads();
+            uint32_t bins[kBinsEach], bin, above;
+#pragma unroll
+            for (int i = 0; i < kBinsEach; ++i) bins[i] = hist[kBins - 1 - kBinsEach * threadIdx.x - i];
+            find_bin(bins, equal, part, found, bin, above);
+            threshold |= bin << kShift[pass];
+            equal -= above;
+        }
+    }
+    mine.write(q, j0, threshold, equal, 0, 0, part);
+    for (int i = (int)w.want + threadIdx.x; i < a.budget; i += kChooseThreads) q.kept[i] = -1;
+    if (q.head == 0 && threadIdx.x == 0) a.kept_lengths[q.s] = (int)w.want;
+}
+
+// Longer tables: a block has a chunk of kChunk keys, the histograms of a sequence's chunks are joined by each of its blocks in the next of four launches (PASS 0 .. 3; the last one
+// writes).  Sums over the chunks before a block's own tell where its kept keys go.
+constexpr int kChunkEach = 8, kChunk = kChooseThreads * kChunkEach;
+struct ChunkArgs {
+    EvictArgs a;
+    int32_t chunks;
+    uint32_t* hist[2];         // [seats][chunks][kBins], of this and of the last pass in turn
+    uint32_t* place;           // [seats][chunks]: old keys above the threshold so far in the chunks before
+    uint32_t* state;           // [2][seats][2]: threshold so far, rank among the keys that begin with it, of this and of the last pass in turn
+};
+template <int PASS>
+__global__ void __launch_bounds__(kChooseThreads) k_evict_chunks(ChunkArgs c, bool wide) {
+    __shared__ uint32_t hist[kBins], part[kChooseWaves], found[2];
+    const EvictArgs& a = c.a;
+    const int seats = gridDim.x / c.chunks, seat = blockIdx.x / c.chunks, chunk = blockIdx.x - seat * c.chunks;
+    const Seat q(a, seat);
+    const int64_t j0 = (int64_t)chunk * kChunk + threadIdx.x * kChunkEach;
+    const int chunks = min(c.chunks, (int)((q.n + (int64_t)kChunk - 1) / kChunk));          // that hold keys
+    if (chunk >= max(chunks, 1)) return;
+    const Mine<kChunkEach> mine(a, q, j0, wide);
+    const Wanted w(a, q, part);
+    const bool all = w.choose == w.olds;                        // (nothing is to be searched for)
+    uint32_t threshold = 0, rank = w.choose, above_before = 0, equal_before = 0;
+    if (PASS > 0 && !all && w.choose > 0) {
+        const uint32_t* last = c.hist[(PASS + 1) & 1] + (int64_t)seat * c.chunks * kBins;
+        uint32_t bins[kBinsEach], before[kBinsEach], bin, above;
+#pragma unroll
+        for (int i = 0; i < kBinsEach; ++i) bins[i] = before[i] = 0;
+        static_assert(kBinsEach == 2, "two bins of a thread are read together");
+        for (int k = 0; k < chunks; ++k) {
+            const uint2 h = *(const uint2*)(last + (int64_t)k * kBins + kBins - 2 - 2 * threadIdx.x);
+            bins[0] += h.y;
+            bins[1] += h.x;
+            if (k < chunk) { before[0] += h.y; before[1] += h.x; }
+        }
+        if (PASS > 1) {
+            const uint32_t* st = c.state + ((int64_t)((PASS + 1) & 1) * seats + seat) * 2;
+            threshold = st[0];
+            rank = st[1];
+        }
+        find_bin(bins, rank, part, found, bin, above);
+        threshold |= bin << kShift[PASS > 0 ? PASS - 1 : 0];
+        rank -= above;
+        // of the chunks before: keys in the bins above, and in the bin itself
+        uint32_t more = 0, same = 0;
+#pragma unroll
+        for (int i = 0; i < kBinsEach; ++i) {
+            const uint32_t b = kBins - 1 - kBinsEach * threadIdx.x - i;
+            if (b > bin) more += before[i];
+            if (b == bin) same += before[i];
+        }
+        block_prefix(more, part, above_before);
+        block_prefix(same, part, equal_before);
+        uint32_t* place = c.place + (int64_t)seat * c.chunks + chunk;
+        if (PASS > 1) above_before += *place;
+        __syncthreads();
+        if (PASS < 3 && threadIdx.x == 0) {
+            *place = above_before;
+            if (chunk == 0) {
+                uint32_t* st = c.state + ((int64_t)(PASS & 1) * seats + seat) * 2;
+                st[0] = threshold;
+                st[1] = rank;
+            }
+        }
+    }
+    if constexpr (PASS < 3) {
+        if (all || w.choose == 0) return;
+#pragma unroll
+        for (int i = 0; i < kBinsEach; ++i) hist[threadIdx.x + i * kChooseThreads] = 0;
+        __syncthreads();
+        mine.count(hist, PASS, threshold);
+        __syncthreads();
+        uint32_t* to = c.hist[PASS & 1] + ((int64_t)seat * c.chunks + chunk) * kBins;
+#pragma unroll
+        for (int i = 0; i < kBinsEach; ++i) to[threadIdx.x + i * kChooseThreads] = hist[threadIdx.x + i * kChooseThreads];
+    } else {
+        // keys there before the chunk: the newest count as kept, the old ones where all of them are
+        uint32_t mine_new = 0, mine_old = 0, news, olds;
+        const int first = chunk * kChunk, P = 1 << a.st.shift;
+        for (int p = threadIdx.x; p << a.st.shift < min(first, q.n); p += kChooseThreads) {
+            const int j = p << a.st.shift;
+            if (q.there(a, j)) {
+                const int o = min(P, max(q.old - j, 0));
+                mine_old += o;
+                mine_new += min(P, q.n - j) - o;
+            }
+        }
+        block_prefix(mine_new, part, news);
+        block_prefix(mine_old, part, olds);
+        if (w.choose == 0) { threshold = ~0u; rank = 0; }       // (as in k_evict_choose)
+        else if (all) { rank = ~0u; above_before = olds; }      // all old keys, those that equal the threshold (0) among them
+        mine.write(q, j0, threshold, rank, above_before + news, equal_before, part);
+        for (int i = (int)w.want + chunk * kChooseThreads + threadIdx.x; i < a.budget; i += max(chunks, 1) * kChooseThreads) q.kept[i] = -1;
+        if (q.head == 0 && chunk == 0 && threadIdx.x == 0) a.kept_lengths[q.s] = (int)w.want;
+    }
 }
 
 // Moves the kept tokens: a block has 64 consecutive ones of a sequence and head, at the destination's keys 64 blockIdx.x on.  Bound by memory where most lines of the source's values are
-// needed; a component's row of the values is gathered token by token.
+// needed; a row of the values is gathered byte by byte.
 template <int BITS>
 __global__ void __launch_bounds__(256) k_evict_move(EvictArgs a, int dim) {
     __shared__ int64_t from[64], to[64];                        // (page * heads + head) << shift | place; -1: none
@@ -180,12 +331,36 @@ __global__ void __launch_bounds__(256) k_evict_move(EvictArgs a, int dim) {
         const int t = i / pieces, p = i - t * pieces;
         if (to[t] >= 0) *(i32x4*)(a.st.kc + to[t] * row + 16 * p) = *(const i32x4*)(a.st.kc + from[t] * row + 16 * p);
     }
-    for (int i = tid; i < 64 * row; i += 256) {
-        const int t = i & 63, c = i >> 6;
-        if (to[t] < 0) continue;
-        // (a page's values: row << shift bytes at (page * heads + head) << shift times row)
-        const int64_t f = from[t], d = to[t];
-        a.st.vc[(d >> a.st.shift << a.st.shift) * row + ((int64_t)c << a.st.shift) + (d & (P - 1))] = a.st.vc[(f >> a.st.shift << a.st.shift) * row + ((int64_t)c << a.st.shift) + (f & (P - 1))];
+    // four tokens of a row of the values a thread, 16 threads a row: the destination's four bytes lie together (a page's values: row << shift bytes at (page * heads + head) << shift times row)
+    auto place = [&](int64_t at) { return a.st.vc + (at >> a.st.shift << a.st.shift) * row + (at & (P - 1)); };
+    const int t0 = (tid & 15) * 4;
+    const bool any = to[t0] >= 0;                               // (the four stand on one page: the first of them tells)
+    const bool four = to[t0 + 3] >= 0;
+    int8_t* const d = place(any ? to[t0] : 0);
+    const int8_t* f[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) f[j] = place(from[t0 + j] >= 0 ? from[t0 + j] : from[t0]);
+    if (!any) return;
+    constexpr int AHEAD = 4;
+    for (int c0 = tid >> 4; c0 < row; c0 += 16 * AHEAD) {
+        uint32_t x[AHEAD][4];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            const int64_t at = (int64_t)min(c0 + 16 * k, row - 1) << a.st.shift;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[k][j] = (uint8_t)f[j][at];
+        }
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            if (c0 + 16 * k >= row) break;
+            int8_t* const at = d + ((int64_t)(c0 + 16 * k) << a.st.shift);
+            if (four) *(uint32_t*)at = x[k][0] | x[k][1] << 8 | x[k][2] << 16 | x[k][3] << 24;
+            else {
+#pragma unroll
+                for (int j = 0; j < 3; ++j)
+                    if (to[t0 + j] >= 0) at[j] = (int8_t)x[k][j];
+            }
+        }
     }
 }
 

@@ -182,6 +182,12 @@ EVICTIONS = [
     ([5000, 4096, 4097], 1025, 0, 1, 32, 256),
     ([20000], 3001, 77, 2, 64, 128),
     ([130, 131], 129, 128, 1, 128, 128),
+    # tables of every size that one block holds, and longer ones in chunks: sequences that end in the first chunk, within one, at the border of one; that have nothing at all
+    ([8000, 4000], 1000, 10, 1, 32, 32),
+    ([16384, 12000], 5000, 10, 1, 32, 128),
+    ([40000, 5, 0, 9000, 8192, 16384, 8193], 2500, 300, 1, 32, 64),
+    ([70000], 65536, 0, 1, 32, 256),
+    ([17000, 16500], 16400, 16390, 1, 32, 16),
 ]
 
 
@@ -191,7 +197,8 @@ def test_evict(B, lengths, budget, recent, heads, dim, page, kind):
     check_evict(B, lengths, budget, recent, heads, dim, page, kind, spare=budget % 2)
 
 
-@pytest.mark.parametrize("lengths,budget,recent,heads,dim,page", [([100, 40, 64, 65], 40, 8, 3, 128, 16), ([300, 299, 170], 64, 64, 2, 96, 32), ([2000, 900], 700, 100, 1, 64, 64)])
+@pytest.mark.parametrize("lengths,budget,recent,heads,dim,page", [([100, 40, 64, 65], 40, 8, 3, 128, 16), ([300, 299, 170], 64, 64, 2, 96, 32), ([2000, 900], 700, 100, 1, 64, 64),
+                                                                  ([20000, 100], 300, 100, 1, 32, 64)])
 @pytest.mark.parametrize("kind", ["spread", "ties"])
 def test_evict_around_pages_that_are_not_there(B, lengths, budget, recent, heads, dim, page, kind):
     check_evict(B, lengths, budget, recent, heads, dim, page, kind, holes=True)
