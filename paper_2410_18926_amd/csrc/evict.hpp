@@ -225,11 +225,18 @@ __global__ void __launch_bounds__(kChooseThreads) k_evict_chunks(ChunkArgs c, bo
 #pragma unroll
         for (int i = 0; i < kBinsEach; ++i) bins[i] = before[i] = 0;
         static_assert(kBinsEach == 2, "two bins of a thread are read together");
-        for (int k = 0; k < chunks; ++k) {
-            const uint2 h = *(const uint2*)(last + (int64_t)k * kBins + kBins - 2 - 2 * threadIdx.x);
-            bins[0] += h.y;
-            bins[1] += h.x;
-            if (k < chunk) { before[0] += h.y; before[1] += h.x; }
+        for (int k0 = 0; k0 < chunks; k0 += 8) {                // (eight are requested together)
+            uint2 h[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) h[k] = *(const uint2*)(last + (int64_t)min(k0 + k, chunks - 1) * kBins + kBins - 2 - 2 * threadIdx.x);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const bool is = k0 + k < chunks, mine_after = k0 + k < chunk;
+                bins[0] += is ? h[k].y : 0u;
+                bins[1] += is ? h[k].x : 0u;
+                before[0] += mine_after ? h[k].y : 0u;
+                before[1] += mine_after ? h[k].x : 0u;
+            }
         }
         if (PASS > 1) {
             const uint32_t* st = c.state + ((int64_t)((PASS + 1) & 1) * seats + seat) * 2;
@@ -293,72 +300,111 @@ __global__ void __launch_bounds__(kChooseThreads) k_evict_chunks(ChunkArgs c, bo
     }
 }
 
-// Moves the kept tokens: a block has 64 consecutive ones of a sequence and head, at the destination's keys 64 blockIdx.x on.  Bound by memory where most lines of the source's values are
-// needed; a row of the values is gathered byte by byte.
+// Moves the kept tokens: a block has 64 consecutive ones of a sequence and head, at the destination's keys 64 blockIdx.x on.  Their keys are rows of their own.  Their values lie byte by
+// byte in rows of components: the 16-byte groups that hold any of the 64 are read into LDS (in order, so that lanes read neighbouring groups) and the bytes picked there - each
+// byte read from memory by a lane of its own costs a cycle of the address unit, whatever the cache holds (32 sequences of up to 6000 keys cut to 2048, 4 bits, 8 heads of 128: 64 us).
+// Bound by memory: where few keys are kept, most lines of the source's values are read all the same.
+constexpr int kMoveRoom = 1024;        // 16-byte groups in LDS
 template <int BITS>
 __global__ void __launch_bounds__(256) k_evict_move(EvictArgs a, int dim) {
     __shared__ int64_t from[64], to[64];                        // (page * heads + head) << shift | place; -1: none
+    __shared__ int64_t group[64];                               // from of a token of each 16-token group
+    __shared__ uint8_t which[64];                               // a token's group
+    __shared__ int many;
+    __shared__ __align__(16) i32x4 lds[kMoveRoom];
     const int tid = threadIdx.x, head = blockIdx.y, s = blockIdx.z, P = 1 << a.st.shift;
-    const int r0 = blockIdx.x * 64, count = a.kept_lengths[s];
+    const int r0 = blockIdx.x * 64;
     const int64_t seat = (int64_t)s * a.st.heads + head;
+    float ks, vs;
+    uint32_t kf = 0, vf = 0;
     if (tid < 64) {
         const int r = r0 + tid;
+        const int key = r < a.budget ? a.kept[seat * a.budget + r] : -1;
+        const int to_page = (r >> a.st.shift) < a.to_width ? a.to_tables[(int64_t)s * a.to_width + (r >> a.st.shift)] : -1;
         int64_t src = -1, dst = -1;
-        int key = -1;
-        if (r < count) {
-            key = a.kept[seat * a.budget + r];
-            const int page = a.tables[(int64_t)s * a.width + (key >> a.st.shift)], to_page = a.to_tables[(int64_t)s * a.to_width + (r >> a.st.shift)];
-            src = a.st.row(page, head) + (key & (P - 1));
+        if (key >= 0) {
+            src = a.st.row(a.tables[(int64_t)s * a.width + (key >> a.st.shift)], head) + (key & (P - 1));
             if ((uint32_t)to_page < (uint64_t)a.st.pages) dst = a.st.row(to_page, head) + (r & (P - 1));
         }
         from[tid] = src;
         to[tid] = dst;
+        const int64_t mine = src >> 4, last = __shfl_up(mine, 1, 64);
+        const uint64_t first = __ballot(src >= 0 && (tid == 0 || mine != last));
+        const int g = __popcll(first & (2ull << tid) - 1) - 1;
+        which[tid] = (uint8_t)g;                                // (of a token that is not there: not used)
+        if (first >> tid & 1) group[g] = src;
+        if (tid == 0) many = __popcll(first);
         if (a.kept_sums && r < (int64_t)a.to_width << a.st.shift)
             a.kept_sums[seat * ((int64_t)a.to_width << a.st.shift) + r] = key < 0 ? 0.0f : a.sums[seat * a.keys + key];
+        if (dst >= 0) {
+            ks = a.st.ks[src];
+            vs = a.st.vs[src];
+            if constexpr (BITS == 4) { kf = a.st.kf[src]; vf = a.st.vf[src]; }
+        }
     }
     __syncthreads();
-    if (r0 >= count) return;
-    if (tid < 64 && to[tid] >= 0) {
-        a.st.ks[to[tid]] = a.st.ks[from[tid]];
-        a.st.vs[to[tid]] = a.st.vs[from[tid]];
-        if constexpr (BITS == 4) {
-            a.st.kf[to[tid]] = a.st.kf[from[tid]];
-            a.st.vf[to[tid]] = a.st.vf[from[tid]];
-        }
-    }
+    const int groups = many;
+    if (groups == 0) return;
     const int row = dim * BITS / 8, pieces = row / 16;          // bytes of a row of keys; rows of a page's values
-    for (int i = tid; i < 64 * pieces; i += 256) {
-        const int t = i / pieces, p = i - t * pieces;
-        if (to[t] >= 0) *(i32x4*)(a.st.kc + to[t] * row + 16 * p) = *(const i32x4*)(a.st.kc + from[t] * row + 16 * p);
-    }
-    // four tokens of a row of the values a thread, 16 threads a row: the destination's four bytes lie together (a page's values: row << shift bytes at (page * heads + head) << shift times row)
+    const int batch = min(kMoveRoom / groups, row);             // rows of the values at a time
+    // a page's values: row << shift bytes at (page * heads + head) << shift times row
     auto place = [&](int64_t at) { return a.st.vc + (at >> a.st.shift << a.st.shift) * row + (at & (P - 1)); };
+    // everything of the first batch is requested before anything is stored: rounds of waiting are what a block's time is made of
+    constexpr int AHEAD = kMoveRoom / 256, KEYS = BITS / 4;     // 16-byte pieces of a thread: values; keys, 64 * 128 * BITS / 8 / 16 / 256
+    i32x4 v[AHEAD], k[KEYS];
+    int kt[KEYS];
+    auto load = [&](int c0, int rows) {
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const int p = tid + 256 * i, c = p / groups, g = p - c * groups;
+            if (c < rows) v[i] = *(const i32x4*)(place(group[g] & ~(int64_t)15) + ((int64_t)(c0 + c) << a.st.shift));
+        }
+    };
+    load(0, batch);
+#pragma unroll
+    for (int i = 0; i < KEYS; ++i) {
+        const int p = tid + 256 * i;
+        kt[i] = p / pieces;
+        if (p < 64 * pieces && to[kt[i]] >= 0) k[i] = *(const i32x4*)(a.st.kc + from[kt[i]] * row + 16 * (p - kt[i] * pieces));
+    }
+    if (tid < 64 && to[tid] >= 0) {
+        a.st.ks[to[tid]] = ks;
+        a.st.vs[to[tid]] = vs;
+        if constexpr (BITS == 4) { a.st.kf[to[tid]] = kf; a.st.vf[to[tid]] = vf; }
+    }
+    // four tokens of a row a thread, 16 threads a row: the destination's four bytes lie together
     const int t0 = (tid & 15) * 4;
-    const bool any = to[t0] >= 0;                               // (the four stand on one page: the first of them tells)
-    const bool four = to[t0 + 3] >= 0;
+    const bool any = to[t0] >= 0, four = to[t0 + 3] >= 0;       // (the four stand on one page: the first of them tells)
     int8_t* const d = place(any ? to[t0] : 0);
-    const int8_t* f[4];
+    int at[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) f[j] = place(from[t0 + j] >= 0 ? from[t0 + j] : from[t0]);
-    if (!any) return;
-    constexpr int AHEAD = 4;
-    for (int c0 = tid >> 4; c0 < row; c0 += 16 * AHEAD) {
-        uint32_t x[AHEAD][4];
-#pragma unroll
-        for (int k = 0; k < AHEAD; ++k) {
-            const int64_t at = (int64_t)min(c0 + 16 * k, row - 1) << a.st.shift;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) x[k][j] = (uint8_t)f[j][at];
+    for (int j = 0; j < 4; ++j) at[j] = from[t0 + j] >= 0 ? which[t0 + j] * 16 + (int)(from[t0 + j] & 15) : 0;
+    for (int c0 = 0; c0 < row; c0 += batch) {
+        const int rows = min(batch, row - c0);
+        if (c0) {
+            load(c0, rows);
+            __syncthreads();
         }
 #pragma unroll
-        for (int k = 0; k < AHEAD; ++k) {
-            if (c0 + 16 * k >= row) break;
-            int8_t* const at = d + ((int64_t)(c0 + 16 * k) << a.st.shift);
-            if (four) *(uint32_t*)at = x[k][0] | x[k][1] << 8 | x[k][2] << 16 | x[k][3] << 24;
+        for (int i = 0; i < AHEAD; ++i)
+            if (tid + 256 * i < rows * groups) lds[tid + 256 * i] = v[i];
+        if (!c0) {
+#pragma unroll
+            for (int i = 0; i < KEYS; ++i) {
+                const int p = tid + 256 * i;
+                if (p < 64 * pieces && to[kt[i]] >= 0) *(i32x4*)(a.st.kc + to[kt[i]] * row + 16 * (p - kt[i] * pieces)) = k[i];
+            }
+        }
+        __syncthreads();
+        if (!any) continue;
+        for (int c = tid >> 4; c < rows; c += 16) {
+            const uint8_t* b = (const uint8_t*)lds + c * groups * 16;
+            int8_t* const to_row = d + ((int64_t)(c0 + c) << a.st.shift);
+            if (four) *(uint32_t*)to_row = b[at[0]] | b[at[1]] << 8 | b[at[2]] << 16 | (uint32_t)b[at[3]] << 24;
             else {
 #pragma unroll
                 for (int j = 0; j < 3; ++j)
-                    if (to[t0 + j] >= 0) at[j] = (int8_t)x[k][j];
+                    if (to[t0 + j] >= 0) to_row[j] = (int8_t)b[at[j]];
             }
         }
     }
