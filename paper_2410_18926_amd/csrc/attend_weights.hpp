@@ -21,7 +21,7 @@ struct WeightArgs {
     // many rows: rows of a sequence begin at a multiple of 32 (padded_row)
     int64_t padded;            // rows of a head
     f16x8* q16;                // [heads][padded / 32][D / 16][64]: operands of the matrix instructions, as the lanes hold them
-    float* back;               // [heads][padded]: what a product of such a row is to be multiplied by, scale log2 e included
+    float* back;               // [heads][padded]: what a product of such a row, times a key's step, is to be multiplied by: positive, scale log2 e included but for its sign
     float *row_m, *row_inv;    // [heads][padded]: m, 1 / l
 };
 
@@ -50,7 +50,7 @@ __device__ __forceinline__ f16x8 key_operand(const int8_t* row, int at, uint32_t
 // Few rows.  A block has up to 16 rows of one head and a range of keys; its wavefronts take tiles of 64 keys in turn, codes straight from memory into registers, the next tile's in flight
 // (as k_attend_rows).  A lane keeps a maximum and a sum of its own until the end.
 template <typename T, int D, int BITS>
-__global__ void __launch_bounds__(64 * kAttendWaves, 2) k_weights_scores(WeightArgs wa) {
+__global__ void __launch_bounds__(64 * kAttendWaves, 3) k_weights_scores(WeightArgs wa) {
     const AttendArgs& a = wa.a;
     constexpr int S32 = D / 32, ROW = D * BITS / 8;
     constexpr int PIECE = BITS == 8 ? 8 : 4;                    // bytes of a lane's eight codes
@@ -320,15 +320,17 @@ __global__ void __launch_bounds__(64) k_weights_queries(WeightArgs wa) {
         for (int j = 0; j < 8; ++j) q[j] = (_Float16)(f[j] * up);
         to[64 * i] = q;
     }
-    if (half == 0) wa.back[(int64_t)head * wa.padded + slot + n] = back * a.c;
+    if (half == 0) wa.back[(int64_t)head * wa.padded + slot + n] = fmaxf(back * fabsf(a.c), 0x1p-149f);      // (not 0: keys that are not there are -inf)
 }
 
-// Many rows: m and l.  A block has 128 rows of one head, a wavefront 32; keys pass by, 64 at a time, converted once for the block into LDS.
+// Many rows: m and l.  A block has 128 rows of one head, a wavefront 32; keys pass by, 64 at a time, converted once for the block into LDS.  The maximum is taken over x = product * step,
+// which the row's factor (positive) is applied to together with it: y - m = fma(x, back, -m), so a score costs five instructions and its exponential.
 template <int D, int BITS>
 __global__ void __launch_bounds__(256, 2) k_weights_rows(WeightArgs wa) {
     const AttendArgs& a = wa.a;
     constexpr int N = D / 16, KS = D + 8, ROW = D * BITS / 8;
-    constexpr int PIECES = kTileKeys * D / 8, PER = PIECES / 256;              // pieces of eight codes
+    constexpr int PIECES = kTileKeys * D / 16, PER = (PIECES + 255) / 256;      // pieces of 16 codes
+    typedef std::conditional_t<BITS == 4, i32x2, i32x4> Piece;
     __shared__ __align__(16) _Float16 lds_k[2][kTileKeys * KS];
     __shared__ __align__(16) float lds_step[2][2][kTileKeys];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, half = lane >> 5;
@@ -348,7 +350,7 @@ __global__ void __launch_bounds__(256, 2) k_weights_rows(WeightArgs wa) {
         if (any) q[i] = wa.q16[(slot / 32 * N + i) * 64 + lane];
         else q[i] = f16x8{0, 0, 0, 0, 0, 0, 0, 0};
     }
-    const float back = any ? wa.back[slot + n] : 0.0f;
+    const float back = any ? wa.back[slot + n] : 1.0f, sign = a.c < 0.0f ? -1.0f : 1.0f;
 
     const uint32_t page_bytes = (uint32_t)ROW << a.st.shift;
     int pg[PER], pg_step = 0;
@@ -356,11 +358,11 @@ __global__ void __launch_bounds__(256, 2) k_weights_rows(WeightArgs wa) {
     auto find_pages = [&](const KeyTile& kt) {
         if (!kt.have) return;
 #pragma unroll
-        for (int i = 0; i < PER; ++i) pg[i] = page_at(kt, (tid + i * 256) / (D / 8));
+        for (int i = 0; i < PER; ++i) pg[i] = page_at(kt, (tid + i * 256) / (D / 16) % kTileKeys);
         pg_step = page_at(kt, lane);
     };
     auto row_of = [&](int page) { return (uint64_t)(uint32_t)(((uint32_t)page < (uint64_t)a.st.pages ? page : 0) * a.st.heads + head); };
-    i32x2 ck[PER];
+    Piece ck[PER];
     uint32_t fk[PER];
     float rks = 0.0f;
     bool rhave = false;
@@ -368,15 +370,12 @@ __global__ void __launch_bounds__(256, 2) k_weights_rows(WeightArgs wa) {
         if (!kt.have) return;
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const int p = tid + i * 256, key = p / (D / 8), part = p % (D / 8);
+            const int p = tid + i * 256, key = p / (D / 16), part = p % (D / 16);
+            if (PIECES % 256 && p >= PIECES) break;
             const uint64_t r = row_of(pg[i]);
             const uint32_t at = (uint32_t)((kt.k + key) & (P - 1));
-            const int8_t* from = a.st.kc + r * page_bytes + at * ROW + part * BITS;
-            if constexpr (BITS == 8) ck[i] = *(const i32x2*)from;
-            else {
-                ck[i][0] = *(const int*)from;
-                fk[i] = a.st.kf[(r << a.st.shift) + at];
-            }
+            ck[i] = *(const Piece*)(a.st.kc + r * page_bytes + at * ROW + part * (int)sizeof(Piece));
+            if constexpr (BITS == 4) fk[i] = a.st.kf[(r << a.st.shift) + at];
         }
         if (wave == 0) {
             rhave = kt.k + lane < kt.length && (uint32_t)pg_step < (uint64_t)a.st.pages;
@@ -386,16 +385,22 @@ __global__ void __launch_bounds__(256, 2) k_weights_rows(WeightArgs wa) {
     auto stage = [&](int kb) {
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const int p = tid + i * 256, key = p / (D / 8), part = p % (D / 8);
-            f16x8 k, hi;
-            if constexpr (BITS == 8) codes_to_half(i32x4{ck[i][0], ck[i][1], 0, 0}, k, hi);
-            else k = codes4_to_half((uint32_t)ck[i][0]) * spread(factor_pair(fk[i], (uint32_t)part / 4));
+            const int p = tid + i * 256, key = p / (D / 16), part = p % (D / 16);
+            if (PIECES % 256 && p >= PIECES) break;
+            f16x8 lo, hi;
+            if constexpr (BITS == 8) codes_to_half(ck[i], lo, hi);
+            else {
+                const f16x8 r = spread(factor_pair(fk[i], (uint32_t)part / 2));
+                lo = codes4_to_half((uint32_t)ck[i][0]) * r;
+                hi = codes4_to_half((uint32_t)ck[i][1]) * r;
+            }
             // key 32 h + 16 b + 4 g + r is row 32 b + 8 g + 4 h + r of the product, whose 32 results of a lane are then consecutive keys
             const int krow = (key & 16) * 2 + (key >> 2 & 3) * 8 + (key >> 5) * 4 + (key & 3);
-            *(f16x8*)&lds_k[kb][krow * KS + 8 * part] = k;
+            *(f16x8*)&lds_k[kb][krow * KS + 16 * part] = lo;
+            *(f16x8*)&lds_k[kb][krow * KS + 16 * part + 8] = hi;
         }
         if (wave == 0) {
-            lds_step[kb][0][lane] = rhave ? rks : 0.0f;
+            lds_step[kb][0][lane] = rhave ? rks * sign : 0.0f;
             lds_step[kb][1][lane] = rhave ? 0.0f : -INFINITY;
         }
     };
@@ -413,7 +418,7 @@ __global__ void __launch_bounds__(256, 2) k_weights_rows(WeightArgs wa) {
     it.next(a, tile.s, behind);
     find_pages(it.t);
     int kb = 0;
-    float M = -INFINITY, L = 0.0f;
+    float X = -INFINITY, L = 0.0f;                              // largest x so far
     while (cur.have) {
         __syncthreads();                                        // tile `cur` is in buffer kb; the other has been read
         f32x16 s[2];
@@ -433,14 +438,13 @@ __global__ void __launch_bounds__(256, 2) k_weights_rows(WeightArgs wa) {
         fetch(after);
         it.next(a, tile.s, behind);
         find_pages(it.t);
-        float top = M;
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
                 const f32x4 sk = *(const f32x4*)&lds_step[kb][0][32 * half + 16 * b + 4 * g], lv = *(const f32x4*)&lds_step[kb][1][32 * half + 16 * b + 4 * g];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) s[b][4 * g + j] = fmaf(s[b][4 * g + j] * back, sk[j], lv[j]);
+                for (int j = 0; j < 4; ++j) s[b][4 * g + j] = fmaf(s[b][4 * g + j], sk[j], lv[j]);
             }
         if (cur.k + kTileKeys > cur.length - first_behind) {
             const int see = cur.length - see_after - cur.k - 32 * half;
@@ -449,22 +453,24 @@ __global__ void __launch_bounds__(256, 2) k_weights_rows(WeightArgs wa) {
 #pragma unroll
                 for (int j = 0; j < 16; ++j) s[b][j] = 16 * b + j < see ? s[b][j] : -INFINITY;
         }
+        float top = X;
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
             for (int j = 0; j < 16; ++j) top = fmaxf(top, s[b][j]);
-        const float use = top == -INFINITY ? 0.0f : top;
-        float l = L * __builtin_amdgcn_exp2f(M - use);
+        const float m = top == -INFINITY ? 0.0f : top * back;
+        float l[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
-            for (int j = 0; j < 16; ++j) l += __builtin_amdgcn_exp2f(s[b][j] - use);
-        L = l;
-        M = top;
+            for (int j = 0; j < 16; ++j) l[j & 3] += __builtin_amdgcn_exp2f(fmaf(s[b][j], back, -m));
+        L = L * __builtin_amdgcn_exp2f(fmaf(X, back, -m)) + ((l[0] + l[1]) + (l[2] + l[3]));
+        X = top;
         cur = nxt;
         nxt = after;
         kb ^= 1;
     }
+    float M = X * back;                                         // (-inf: no key)
     join_sums(M, L, __shfl_xor(M, 32, 64), __shfl_xor(L, 32, 64));
     if (!any || half) return;
     if (a.splits == 1) {
@@ -488,6 +494,18 @@ __global__ void __launch_bounds__(256) k_weights_join(WeightArgs wa) {
     wa.row_inv[i] = l == 0.0f ? 0.0f : 1.0f / l;
 }
 
+// 2 W values of a lane are W of its pair's (lanes W apart) added up, and so on: after all rounds lane n has value n of the 32 that each of 32 lanes had, added up.
+template <int W>
+__device__ __forceinline__ void add_over_lanes(float (&v)[32]) {
+    const bool upper = threadIdx.x & W;
+#pragma unroll
+    for (int j = 0; j < W; ++j) {
+        const float give = upper ? v[j] : v[j + W], keep = upper ? v[j + W] : v[j];
+        v[j] = keep + __shfl_xor(give, W, 64);
+    }
+    if constexpr (W > 1) add_over_lanes<W / 2>(v);
+}
+
 // Many rows: the sums.  A wavefront holds 64 keys as operands, rows pass by, 32 at a time.  SHARE: the block's four wavefronts have the same keys and take the rows in turn; else each
 // has keys of its own.  Blocks: (chunk of keys, head, sequence).
 template <int D, int BITS, bool SHARE>
@@ -495,6 +513,7 @@ __global__ void __launch_bounds__(256, 2) k_weights_keys(WeightArgs wa) {
     const AttendArgs& a = wa.a;
     constexpr int N = D / 16, ROW = D * BITS / 8;
     __shared__ float lds_sum[4][64];
+    __shared__ __align__(16) float lds_step[4][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 31, half = lane >> 5;
     const int head = blockIdx.y, s = blockIdx.z, P = 1 << a.st.shift;
     const int64_t k0 = ((int64_t)blockIdx.x * (SHARE ? 1 : 4) + (SHARE ? 0 : wave)) * 64;
@@ -502,9 +521,6 @@ __global__ void __launch_bounds__(256, 2) k_weights_keys(WeightArgs wa) {
     tokens_of(a, s, first, count);
     const int length = a.found ? min(max(a.lengths[s], 0), a.width << a.st.shift) : 0;
     const int rows = k0 < length ? count * a.group : 0;
-    // the lane's two keys as operands; of its 32 results the keys are 32 half + 16 b + 4 g + r, as in k_weights_rows: row 32 b + n of the product is that key
-    f16x8 k[2][N];
-    float step[2][16];
     const int32_t* pages = a.tables + (int64_t)s * a.width;
     auto row_at = [&](int key, uint64_t& r, uint32_t& at) -> bool {
         const int64_t j = k0 + key;
@@ -514,12 +530,18 @@ __global__ void __launch_bounds__(256, 2) k_weights_keys(WeightArgs wa) {
         at = (uint32_t)(j & (P - 1));
         return ok;
     };
+    // the lane's two keys as operands; of its 32 results the keys are 32 half + 16 b + j, as in k_weights_rows: row 32 b + n of the product is the key below
+    f16x8 k[2][N];
+    f32x4 step[2][4];
+    bool ok = false;                                            // the lane's own key is there
     if (rows > 0) {
+        uint64_t r;
+        uint32_t at;
+        ok = row_at(lane, r, at);
+        lds_step[wave][lane] = ok ? a.st.ks[(r << a.st.shift) + at] * (a.c < 0.0f ? -1.0f : 1.0f) : 0.0f;      // (of a key that is not there: any)
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
             const int key = 32 * (n >> 2 & 1) + 16 * b + 4 * (n >> 3) + (n & 3);
-            uint64_t r;
-            uint32_t at;
             row_at(key, r, at);
             const int8_t* from = a.st.kc + ((r << a.st.shift) + at) * ROW;
             uint32_t factors = 0;
@@ -527,61 +549,62 @@ __global__ void __launch_bounds__(256, 2) k_weights_keys(WeightArgs wa) {
 #pragma unroll
             for (int i = 0; i < N; ++i) k[b][i] = key_operand<D, BITS>(from, D / 2 * half + 8 * i, factors);
         }
-        // the step of the lane's own key, spread over the results (a key that is not there: a step of 0 and, below, no weight)
-        uint64_t r;
-        uint32_t at;
-        const bool ok = row_at(lane, r, at);
-        const float mine = ok ? a.st.ks[(r << a.st.shift) + at] : -INFINITY;
+        wave_lds_order();
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
-            for (int j = 0; j < 16; ++j) step[b][j] = __shfl(mine, 32 * half + 16 * b + j, 64);
+            for (int g = 0; g < 4; ++g) step[b][g] = *(const f32x4*)&lds_step[wave][32 * half + 16 * b + 4 * g];
     }
-    float sum[2][16];
+    float sum[32];
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int j = 0; j < 16; ++j) sum[b][j] = 0.0f;
+    for (int j = 0; j < 32; ++j) sum[j] = 0.0f;
     // the first row that sees key k0
     const int from_row = (int)max((int64_t)0, k0 - (length - count)) * a.group / 32 * 32;
     const int64_t base = (int64_t)head * wa.padded + padded_row((int64_t)first * a.group, s);
     const f16x8* q16 = wa.q16 + base / 32 * N * 64 + lane;
-    for (int r0 = from_row + (SHARE ? wave * 32 : 0); r0 < rows; r0 += SHARE ? 128 : 32) {
+    // the next 32 rows are requested before these are used
+    f16x8 q[N];
+    float back = 0.0f, m = 0.0f, inv = 0.0f;
+    auto fetch = [&](int r0) {
+        if (r0 >= rows) return;
+#pragma unroll
+        for (int i = 0; i < N; ++i) q[i] = q16[((int64_t)(r0 / 32) * N + i) * 64];
+        back = wa.back[base + r0 + n];
+        m = wa.row_m[base + r0 + n];
+        inv = wa.row_inv[base + r0 + n];
+    };
+    constexpr int STRIDE = SHARE ? 128 : 32;
+    int r0 = from_row + (SHARE ? wave * 32 : 0);
+    fetch(r0);
+    for (; r0 < rows; r0 += STRIDE) {
         f32x16 y[2];
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
             for (int j = 0; j < 16; ++j) y[b][j] = 0.0f;
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const f16x8 q = q16[((int64_t)(r0 / 32) * N + i) * 64];
+        for (int i = 0; i < N; ++i)
 #pragma unroll
-            for (int b = 0; b < 2; ++b) y[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k[b][i], q, y[b], 0, 0, 0);
-        }
+            for (int b = 0; b < 2; ++b) y[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k[b][i], q[i], y[b], 0, 0, 0);
         const int row = r0 + n;
-        const float back = wa.back[base + row], m = wa.row_m[base + row], inv = row < rows ? wa.row_inv[base + row] : 0.0f;
+        const float back_now = back, m_now = m, inv_now = inv;
+        __builtin_amdgcn_sched_barrier(0);
+        fetch(r0 + STRIDE);
+        __builtin_amdgcn_sched_barrier(0);
         const int see = row < rows ? (int)(length - count + row / a.group + 1 - k0) - 32 * half : 0;
-        const bool whole = __ballot(see < 32) == 0;             // every row sees all of the lane's keys
+        if (__ballot(see < 32) == 0) {                          // every row sees all of the lane's keys
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+            for (int j = 0; j < 32; ++j) sum[j] = fmaf(__builtin_amdgcn_exp2f(fmaf(y[j >> 4][j & 15] * step[j >> 4][j >> 2 & 3][j & 3], back_now, -m_now)), inv_now, sum[j]);
+        } else {
 #pragma unroll
-            for (int j = 0; j < 16; ++j) {
-                const float e = __builtin_amdgcn_exp2f(fmaf(y[b][j] * back, step[b][j], -m)) * inv;
-                if (whole) sum[b][j] += step[b][j] == -INFINITY ? 0.0f : e;
-                else sum[b][j] += 16 * b + j < see && step[b][j] != -INFINITY ? e : 0.0f;
+            for (int j = 0; j < 32; ++j) {
+                const float e = __builtin_amdgcn_exp2f(fmaf(y[j >> 4][j & 15] * step[j >> 4][j >> 2 & 3][j & 3], back_now, -m_now)) * inv_now;
+                sum[j] += j < see ? e : 0.0f;
             }
-    }
-    // the 32 rows of a lane's results, then the lane that has the key's place writes it
-    float mine = 0.0f;
-#pragma unroll
-    for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int j = 0; j < 16; ++j) {
-            float t = sum[b][j];
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) t += __shfl_xor(t, o, 64);
-            if (n == 16 * b + j) mine = t;
         }
+    }
+    add_over_lanes<16>(sum);                                    // (over the rows; lane n then has key n of its half)
+    float mine = ok ? sum[0] : 0.0f;
     const int64_t key = k0 + lane;
     if constexpr (SHARE) {
         lds_sum[wave][lane] = mine;

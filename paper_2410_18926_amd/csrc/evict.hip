@@ -16,7 +16,7 @@ struct WeightPlan {
 };
 
 // Rows per sequence and head (their mean over the call) up to which the scores are kept, and how much memory they may take: otherwise they are formed twice.
-constexpr int64_t kFewWeightRows = 32, kMostScores = (int64_t)1 << 30;
+constexpr int64_t kScoreBlocks = 4096, kFewWeightRows = 32, kMostScores = (int64_t)1 << 30;
 
 template <typename St>
 WeightPlan weight_plan(const St* st, const lorann_questions* qs, int32_t width) {
@@ -29,7 +29,7 @@ WeightPlan weight_plan(const St* st, const lorann_questions* qs, int32_t width) 
     p.many = mean_rows > kFewWeightRows || p.y > kMostScores;
     p.tiles = tiles_of(p.many ? 128 : kRows);
     const int64_t blocks = std::max<int64_t>(p.tiles * st->heads, 1);
-    const int64_t want = std::max<int64_t>(1, std::min(kBlocksWanted / blocks, ceil_div(keys, kKeysPerBlock)));
+    const int64_t want = std::max<int64_t>(1, std::min((p.many ? kBlocksWanted : kScoreBlocks) / blocks, ceil_div(keys, kKeysPerBlock)));
     const int64_t most = std::max(want, ceil_div(keys, p.many ? kMostTileKeys : kMostKeys));
     p.unit = (int32_t)(ceil_div(ceil_div(std::max<int64_t>(keys, 1), most), kKeysPerBlock) * kKeysPerBlock);
     p.splits = (int32_t)ceil_div(std::max<int64_t>(keys, 1), p.unit);
