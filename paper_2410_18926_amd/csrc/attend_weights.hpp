@@ -83,7 +83,6 @@ __global__ void __launch_bounds__(64 * kAttendWaves, 3) k_weights_scores(WeightA
     auto find_page = [&](const KeyTile& kt) {
         if (kt.have) page = kt.pages[min(kt.k + lane, kt.length - 1) >> a.st.shift];
     };
-    const int my_key = 16 * (n >> 2) + (n & 3);                 // (+ 4 b: a quarter's 16 results are 16 consecutive keys)
     const uint32_t page_bytes = (uint32_t)ROW << a.st.shift;
     uint32_t kr[4][S32][PIECE / 4], rkf[4];
     float rks = 0.0f;
@@ -96,7 +95,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, 3) k_weights_scores(WeightA
         rks = a.st.ks[((uint64_t)(uint32_t)row_of_key << a.st.shift) + (uint32_t)place];
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
-            const int key = my_key + 4 * b;
+            const int key = 16 * b + n;                         // (results: key 16 b + 4 quarter + j, so that a store of the four quarters fills 64 bytes of a row)
             const uint64_t r = (uint32_t)__shfl(row_of_key, key, 64);
             const uint32_t at = (uint32_t)((kt.k + key) & (P - 1));
             const int8_t* kp = a.st.kc + r * page_bytes + at * ROW + component(0) * BITS / 8;
@@ -142,7 +141,12 @@ __global__ void __launch_bounds__(64 * kAttendWaves, 3) k_weights_scores(WeightA
         }
     }
 
-    float* const y_row = wa.y + ((int64_t)head * a.tokens * a.group + (int64_t)tile.first * a.group + row) * wa.row_keys + 16 * quarter;
+    // The block's rows of scores as a buffer: what a row that is not there would store lies behind its end and is dropped, without a branch that the loads' waits would have to
+    // take into account.
+    const uint32_t row_bytes = (uint32_t)(wa.row_keys * 4);      // (16 rows of at most 2^30 bytes would not fit: kMostScores)
+    const auto y_rows = __builtin_amdgcn_make_buffer_rsrc(wa.y + ((int64_t)head * a.tokens * a.group + (int64_t)tile.first * a.group + tile.row0) * wa.row_keys, 0,
+                                                          min(rows - tile.row0, kRows) * row_bytes, 0x00027000);
+    const uint32_t y_at = live ? n * row_bytes + 16 * quarter : 0xffffe000u;
     float M = -INFINITY, L = 0.0f;
     while (cur.have) {
         wave_lds_order();                                       // the previous tile's steps have been read
@@ -172,21 +176,19 @@ __global__ void __launch_bounds__(64 * kAttendWaves, 3) k_weights_scores(WeightA
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
-            const f32x4 sk = *(const f32x4*)&lds_step[wave][0][16 * quarter + 4 * b], lv = *(const f32x4*)&lds_step[wave][1][16 * quarter + 4 * b];
+            const f32x4 sk = *(const f32x4*)&lds_step[wave][0][16 * b + 4 * quarter], lv = *(const f32x4*)&lds_step[wave][1][16 * b + 4 * quarter];
 #pragma unroll
             for (int j = 0; j < 4; ++j) s[b][j] = fmaf(s[b][j] * q_back, sk[j], lv[j]);
         }
         if (cur.k + kTileKeys > cur.length - first_behind) {    // some row may not see all of it
-            const int see = cur.length - see_after - cur.k - 16 * quarter;
+            const int see = cur.length - see_after - cur.k - 4 * quarter;
 #pragma unroll
             for (int b = 0; b < 4; ++b)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) s[b][j] = 4 * b + j < see ? s[b][j] : -INFINITY;
+                for (int j = 0; j < 4; ++j) s[b][j] = 16 * b + j < see ? s[b][j] : -INFINITY;
         }
-        if (live) {
 #pragma unroll
-            for (int b = 0; b < 4; ++b) *(f32x4*)(y_row + cur.k + 4 * b) = s[b];
-        }
+        for (int b = 0; b < 4; ++b) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(i32x4, s[b]), y_rows, live ? y_at + 4 * cur.k : y_at, 64 * b, 0);
         float top = M;
 #pragma unroll
         for (int b = 0; b < 4; ++b)
@@ -280,53 +282,10 @@ __global__ void __launch_bounds__(256) k_weights_add(WeightArgs wa) {
     for (int j = 0; j < 4; ++j) wa.sums[at + j] = sum[j] + more[j];
 }
 
-// Many rows: queries as operands.  A wavefront has 32 rows; lane n + 32 half holds components D / 2 half .. of row n.
-template <typename T, int D>
-__global__ void __launch_bounds__(64) k_weights_queries(WeightArgs wa) {
-    const AttendArgs& a = wa.a;
-    constexpr int N = D / 16;
-    const int head = blockIdx.y, lane = threadIdx.x, n = lane & 31, half = lane >> 5;
-    RowTile tile;
-    if (!find_tile<32, false>(a, blockIdx.x, tile)) return;
-    const int row = tile.row0 + n;
-    const bool live = row < tile.count * a.group;
-    const int tok = live ? row / a.group : 0, qh = head * a.group + (live ? row - tok * a.group : 0);
-    const int64_t at = (int64_t)(tile.first + tok) * a.q_token + (int64_t)qh * a.q_head + D / 2 * half;
-    i32x4 raw[N];
-    float top = 0.0f;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        raw[i] = load8_raw(a.q, at + 8 * i, a.q_wide);
-        if (!live) raw[i] = i32x4{0, 0, 0, 0};
-        float f[8];
-        widen8<T>(raw[i], f);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float m = fabsf(f[j]);
-            if (m <= 3.4028235e38f) top = fmaxf(top, m);
-        }
-    }
-    top = fmaxf(top, __shfl_xor(top, 32, 64));
-    float up, back;
-    row_power(top, up, back);
-    const int64_t slot = padded_row((int64_t)tile.first * a.group, tile.s) + tile.row0;          // a multiple of 32
-    f16x8* to = wa.q16 + ((int64_t)head * wa.padded + slot) / 32 * N * 64 + lane;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        float f[8];
-        widen8<T>(raw[i], f);
-        f16x8 q;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) q[j] = (_Float16)(f[j] * up);
-        to[64 * i] = q;
-    }
-    if (half == 0) wa.back[(int64_t)head * wa.padded + slot + n] = fmaxf(back * fabsf(a.c), 0x1p-149f);      // (not 0: keys that are not there are -inf)
-}
-
 // Many rows: m and l.  A block has 128 rows of one head, a wavefront 32; keys pass by, 64 at a time, converted once for the block into LDS.  The maximum is taken over x = product * step,
 // which the row's factor (positive) is applied to together with it: y - m = fma(x, back, -m), so a score costs five instructions and its exponential.
-template <int D, int BITS>
-__global__ void __launch_bounds__(256, 2) k_weights_rows(WeightArgs wa) {
+template <typename T, int D, int BITS>
+__global__ void __launch_bounds__(256, 3) k_weights_rows(WeightArgs wa) {
     const AttendArgs& a = wa.a;
     constexpr int N = D / 16, KS = D + 8, ROW = D * BITS / 8;
     constexpr int PIECES = kTileKeys * D / 16, PER = (PIECES + 255) / 256;      // pieces of 16 codes
@@ -344,13 +303,41 @@ __global__ void __launch_bounds__(256, 2) k_weights_rows(WeightArgs wa) {
     const int behind = tile.count - 1 - (min(rows, tile.row0 + 128) - 1) / a.group, first_behind = tile.count - 1 - tile.row0 / a.group;
     const int64_t slot = (int64_t)head * wa.padded + padded_row((int64_t)tile.first * a.group, tile.s) + tile.row0 + wave * 32;      // of the wavefront's first row
     const bool any = tile.row0 + wave * 32 < rows;              // (a wavefront without rows has no operands either)
+    // The rows as operands: lane n + 32 half holds components D / 2 half .. of row n.  The blocks of the first keys leave them for k_weights_keys.
     f16x8 q[N];
+    float back;
+    {
+        const int tok = live ? row / a.group : 0, qh = head * a.group + (live ? row - tok * a.group : 0);
+        const int64_t at = (int64_t)(tile.first + tok) * a.q_token + (int64_t)qh * a.q_head + D / 2 * half;
+        i32x4 raw[N];
+        float top = 0.0f;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        if (any) q[i] = wa.q16[(slot / 32 * N + i) * 64 + lane];
-        else q[i] = f16x8{0, 0, 0, 0, 0, 0, 0, 0};
+        for (int i = 0; i < N; ++i) {
+            raw[i] = load8_raw(a.q, at + 8 * i, a.q_wide);
+            if (!live) raw[i] = i32x4{0, 0, 0, 0};
+            float f[8];
+            widen8<T>(raw[i], f);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float m = fabsf(f[j]);
+                if (m <= 3.4028235e38f) top = fmaxf(top, m);
+            }
+        }
+        top = fmaxf(top, __shfl_xor(top, 32, 64));
+        float up;
+        row_power(top, up, back);
+        back = fmaxf(back * fabsf(a.c), 0x1p-149f);             // (not 0: keys that are not there are -inf)
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            float f[8];
+            widen8<T>(raw[i], f);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) q[i][j] = (_Float16)(f[j] * up);
+            if (any && split == 0) wa.q16[(slot / 32 * N + i) * 64 + lane] = q[i];
+        }
+        if (any && split == 0 && half == 0) wa.back[slot + n] = back;
     }
-    const float back = any ? wa.back[slot + n] : 1.0f, sign = a.c < 0.0f ? -1.0f : 1.0f;
+    const float sign = a.c < 0.0f ? -1.0f : 1.0f;
 
     const uint32_t page_bytes = (uint32_t)ROW << a.st.shift;
     int pg[PER], pg_step = 0;
@@ -483,13 +470,17 @@ __global__ void __launch_bounds__(256, 2) k_weights_rows(WeightArgs wa) {
     }
 }
 
-// Joins the splits of each row (rows of no sequence hold anything).
+// Joins the splits of each row, eight threads a row (rows of no sequence hold anything).
 __global__ void __launch_bounds__(256) k_weights_join(WeightArgs wa) {
     const AttendArgs& a = wa.a;
-    const int64_t all = a.st.heads * wa.padded, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= all) return;
+    const int64_t all = a.st.heads * wa.padded, i = (int64_t)blockIdx.x * 32 + (threadIdx.x >> 3);
+    const int part = threadIdx.x & 7;
     float m = -INFINITY, l = 0.0f;
-    for (int p = 0; p < a.splits; ++p) join_sums(m, l, a.part_m[p * all + i], a.part_l[p * all + i]);
+    if (i < all)
+        for (int p = part; p < a.splits; p += 8) join_sums(m, l, a.part_m[p * all + i], a.part_l[p * all + i]);
+#pragma unroll
+    for (int o = 1; o < 8; o <<= 1) join_sums(m, l, __shfl_xor(m, o, 64), __shfl_xor(l, o, 64));
+    if (i >= all || part) return;
     wa.row_m[i] = m == -INFINITY ? 0.0f : m;
     wa.row_inv[i] = l == 0.0f ? 0.0f : 1.0f / l;
 }

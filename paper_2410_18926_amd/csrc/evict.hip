@@ -10,13 +10,15 @@ namespace {
 
 struct WeightPlan {
     bool many;
-    int64_t tiles, tiles32, padded, row_keys;
+    int64_t tiles, padded, row_keys;
     int32_t unit, splits;
     int64_t y, parts, q16, rows, workspace;      // bytes: scores; m and l of the splits; operands; back, m, 1 / l of a row
 };
 
 // Rows per sequence and head (their mean over the call) up to which the scores are kept, and how much memory they may take: otherwise they are formed twice.
-constexpr int64_t kScoreBlocks = 4096, kFewWeightRows = 32, kMostScores = (int64_t)1 << 30;
+// Blocks wanted: of k_weights_scores many more than the GPU holds, since sequences differ in length and a split costs two numbers a row (64 tokens after up to 8192 keys, 8 heads, us with
+// 512 / 1024 / 2048 / 4096 / 8192: 102 / 101 / 104 / 89 / 96); of k_weights_rows 4 a CU (4 x 32 tokens after 16000 keys, 512 / 768 / 1024 / 1536 / 2048: 53 / 52 / 40 / 41 / 49).
+constexpr int64_t kScoreBlocks = 4096, kRowBlocks = 1024, kFewWeightRows = 32, kMostScores = (int64_t)1 << 30;
 
 template <typename St>
 WeightPlan weight_plan(const St* st, const lorann_questions* qs, int32_t width) {
@@ -29,12 +31,11 @@ WeightPlan weight_plan(const St* st, const lorann_questions* qs, int32_t width) 
     p.many = mean_rows > kFewWeightRows || p.y > kMostScores;
     p.tiles = tiles_of(p.many ? 128 : kRows);
     const int64_t blocks = std::max<int64_t>(p.tiles * st->heads, 1);
-    const int64_t want = std::max<int64_t>(1, std::min((p.many ? kBlocksWanted : kScoreBlocks) / blocks, ceil_div(keys, kKeysPerBlock)));
+    const int64_t want = std::max<int64_t>(1, std::min((p.many ? kRowBlocks : kScoreBlocks) / blocks, ceil_div(keys, kKeysPerBlock)));
     const int64_t most = std::max(want, ceil_div(keys, p.many ? kMostTileKeys : kMostKeys));
     p.unit = (int32_t)(ceil_div(ceil_div(std::max<int64_t>(keys, 1), most), kKeysPerBlock) * kKeysPerBlock);
     p.splits = (int32_t)ceil_div(std::max<int64_t>(keys, 1), p.unit);
     if (p.many) {
-        p.tiles32 = tiles_of(32);
         p.padded = ceil_div(rows, 32) * 32 + 32 * qs->sequences;
         p.y = 0;
         p.q16 = p.padded * st->heads * st->dim * 2;
@@ -62,11 +63,9 @@ void launch_weights(const WeightPlan& p, const WeightArgs& w, int32_t type, hipS
         else hipLaunchKernelGGL((k_weights_scores<__bf16, D, BITS>), grid, dim3(64 * kAttendWaves), 0, stream, w);
         return;
     }
-    const dim3 queries((unsigned)p.tiles32, (unsigned)a.st.heads);
-    if (type == LORANN_F16) hipLaunchKernelGGL((k_weights_queries<_Float16, D>), queries, dim3(64), 0, stream, w);
-    else hipLaunchKernelGGL((k_weights_queries<__bf16, D>), queries, dim3(64), 0, stream, w);
-    hipLaunchKernelGGL((k_weights_rows<D, BITS>), grid, dim3(256), 0, stream, w);
-    if (a.splits > 1) hipLaunchKernelGGL(k_weights_join, dim3((unsigned)ceil_div(a.st.heads * w.padded, 256)), dim3(256), 0, stream, w);
+    if (type == LORANN_F16) hipLaunchKernelGGL((k_weights_rows<_Float16, D, BITS>), grid, dim3(256), 0, stream, w);
+    else hipLaunchKernelGGL((k_weights_rows<__bf16, D, BITS>), grid, dim3(256), 0, stream, w);
+    if (a.splits > 1) hipLaunchKernelGGL(k_weights_join, dim3((unsigned)ceil_div(a.st.heads * w.padded, 32)), dim3(256), 0, stream, w);
     const bool share = ceil_div(w.keys, 256) * a.st.heads * a.sequences < kBlocksWanted;
     const dim3 chunks((unsigned)ceil_div(w.keys, share ? 64 : 256), (unsigned)a.st.heads, (unsigned)a.sequences);
     if (share) hipLaunchKernelGGL((k_weights_keys<D, BITS, true>), chunks, dim3(256), 0, stream, w);
