@@ -332,9 +332,10 @@ struct KeyTiles {
 // in-lane but for exchanges between the four quarters of the wavefront, and the weights are the second product's operand as they stand.
 // The next tile's keys are requested as soon as the first product has used this one's, its values after the second product, its page number one tile
 // earlier: a wavefront always has 8 to 16 KiB in flight.  WHOLE: pages of 64 tokens and more, a tile lies in one.
+// RT: tiles of 16 rows of a block, which share the converted codes.
 // BITS 4: a lane's piece of a key row has the 8 codes of each step (at 128 values, 32 consecutive ones: 16 bytes as well), a 16-byte piece of the values has two components; the
 // factors of a tile's keys and values go through LDS beside the steps.
-template <typename T, int D, bool WHOLE, int BITS>
+template <typename T, int D, bool WHOLE, int BITS, int RT>
 __global__ void __launch_bounds__(64 * kAttendWaves, 2) k_attend_rows(AttendArgs a) {
     constexpr int S32 = D / 32;                                 // steps of the first product, 32 values each
     constexpr int C = D / 64, ODD = S32 & 1;                    // 16-byte pieces of a lane's key row (two steps each), and one of 8 bytes
@@ -352,25 +353,33 @@ __global__ void __launch_bounds__(64 * kAttendWaves, 2) k_attend_rows(AttendArgs
     const BlockWork work = block_work(a);
     const int head = work.head, split = work.split;
     RowTile tile;
-    if (!find_tile<kRows, false>(a, work.tile, tile)) return;
+    if (!find_tile<kRows * RT, false>(a, work.tile, tile)) return;
     const int rows = tile.count * a.group;
-    const int row = tile.row0 + n;
-    const bool live = row < rows;
-    const int tok = live ? row / a.group : 0;
-    const int see_after = tile.count - 1 - tok;                 // tokens of the sequence that the lane's row does not see
-    const int behind = tile.count - 1 - (min(rows, tile.row0 + kRows) - 1) / a.group, first_behind = tile.count - 1 - tile.row0 / a.group;
+    bool live[RT];                                              // of the lane's row in each of the block's tiles of 16 rows
+    int tok[RT], see_after[RT];                                 // its token; tokens of the sequence that it does not see
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+        const int row = tile.row0 + kRows * t + n;
+        live[t] = row < rows;
+        tok[t] = live[t] ? row / a.group : 0;
+        see_after[t] = tile.count - 1 - tok[t];
+    }
+    const int behind = tile.count - 1 - (min(rows, tile.row0 + kRows * RT) - 1) / a.group, first_behind = tile.count - 1 - tile.row0 / a.group;
     const int P = 1 << a.st.shift;
 
     // What does not depend on lengths is requested first: the queries, and (chunk: one unit of the sequence's own table) the pages of the wavefront's first tile.
-    const int qh = head * a.group + (live ? row - tok * a.group : 0);
-    const int64_t q_at = (int64_t)(tile.first + tok) * a.q_token + (int64_t)qh * a.q_head;
     auto component = [&](int i) {                               // first of the lane's 8 in step i
         if (FOUR && D == 128) return 32 * quarter + 8 * i;
         return i < 2 * C ? 64 * (i >> 1) + 16 * quarter + 8 * (i & 1) : 64 * C + 8 * quarter;
     };
-    i32x4 raw[S32];
+    i32x4 raw[RT][S32];
 #pragma unroll
-    for (int i = 0; i < S32; ++i) raw[i] = load8_raw(a.q, q_at + component(i), a.q_wide);
+    for (int t = 0; t < RT; ++t) {
+        const int qh = head * a.group + (live[t] ? tile.row0 + kRows * t + n - tok[t] * a.group : 0);
+        const int64_t q_at = (int64_t)(tile.first + tok[t]) * a.q_token + (int64_t)qh * a.q_head;
+#pragma unroll
+        for (int i = 0; i < S32; ++i) raw[t][i] = load8_raw(a.q, q_at + component(i), a.q_wide);
+    }
     int page = 0;                                               // lane = key of a tile: its page
     const bool ahead = !a.ids && a.width > 0;
     if (ahead) page = a.tables[(int64_t)tile.s * a.width + min((split * a.unit + wave * kTileKeys + lane) >> a.st.shift, a.width - 1)];
@@ -462,15 +471,16 @@ __global__ void __launch_bounds__(64 * kAttendWaves, 2) k_attend_rows(AttendArgs
     fetch_values(cur.have, first_row_tile, first_row_key, first_place);
 
     // queries, normalised to binary16 by a power of two per row
-    f16x8 qf[S32];
-    float q_back;
-    {
+    f16x8 qf[RT][S32];
+    float q_back[RT];
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
         float top = 0.0f;
 #pragma unroll
         for (int i = 0; i < S32; ++i) {
-            if (!live) raw[i] = i32x4{0, 0, 0, 0};
+            if (!live[t]) raw[t][i] = i32x4{0, 0, 0, 0};
             float f[8];
-            widen8<T>(raw[i], f);
+            widen8<T>(raw[t][i], f);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const float m = fabsf(f[j]);
@@ -480,20 +490,25 @@ __global__ void __launch_bounds__(64 * kAttendWaves, 2) k_attend_rows(AttendArgs
         top = fmaxf(top, __shfl_xor(top, 32, 64));
         top = fmaxf(top, __shfl_xor(top, 16, 64));
         float up;
-        row_power(top, up, q_back);
+        row_power(top, up, q_back[t]);
 #pragma unroll
         for (int i = 0; i < S32; ++i) {
             float f[8];
-            widen8<T>(raw[i], f);
+            widen8<T>(raw[t][i], f);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) qf[i][j] = (_Float16)(f[j] * up);
+            for (int j = 0; j < 8; ++j) qf[t][i][j] = (_Float16)(f[j] * up);
         }
     }
 
-    f32x4 acc[DT];
+    f32x4 acc[RT][DT];
+    float M[RT], L[RT];
 #pragma unroll
-    for (int i = 0; i < DT; ++i) acc[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    float M = -INFINITY, L = 0.0f;
+    for (int t = 0; t < RT; ++t) {
+#pragma unroll
+        for (int i = 0; i < DT; ++i) acc[t][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        M[t] = -INFINITY;
+        L[t] = 0.0f;
+    }
     bool wild = false;                                          // some step so far is not tame
 
     while (cur.have) {
@@ -511,30 +526,37 @@ __global__ void __launch_bounds__(64 * kAttendWaves, 2) k_attend_rows(AttendArgs
             wild = wild || __ballot(ks.wild);
             wave_lds_order();
         }
-        f32x4 s[4];
+        f32x4 s[RT][4];
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
-            s[b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int t = 0; t < RT; ++t) s[t][b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
             if constexpr (FOUR) {
                 const uint32_t factors = lds_kf[wave][my_key + 4 * b];
                 f16x8 r;
 #pragma unroll
                 for (int i = 0; i < S32; ++i) {
                     if (i == 0 || (D != 128 && i == 2 * C)) r = spread(factor_pair(factors, (uint32_t)component(i) / 32));      // (128 values: the lane's 32 share one)
-                    s[b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes4_to_half((uint32_t)kr[b][0][i]) * r, qf[i], s[b], 0, 0, 0);
+                    const f16x8 k = codes4_to_half((uint32_t)kr[b][0][i]) * r;
+#pragma unroll
+                    for (int t = 0; t < RT; ++t) s[t][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, qf[t][i], s[t][b], 0, 0, 0);
                 }
             } else {
 #pragma unroll
                 for (int i = 0; i < C; ++i) {
                     f16x8 lo, hi;
                     codes_to_half(kr[b][i], lo, hi);
-                    s[b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo, qf[2 * i], s[b], 0, 0, 0);
-                    s[b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi, qf[2 * i + 1], s[b], 0, 0, 0);
+#pragma unroll
+                    for (int t = 0; t < RT; ++t) {
+                        s[t][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo, qf[t][2 * i], s[t][b], 0, 0, 0);
+                        s[t][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi, qf[t][2 * i + 1], s[t][b], 0, 0, 0);
+                    }
                 }
                 if constexpr (ODD) {
                     f16x8 lo, hi;
                     codes_to_half(i32x4{(int)ko[b].x, (int)ko[b].y, 0, 0}, lo, hi);
-                    s[b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo, qf[2 * C], s[b], 0, 0, 0);
+#pragma unroll
+                    for (int t = 0; t < RT; ++t) s[t][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo, qf[t][2 * C], s[t][b], 0, 0, 0);
                 }
             }
         }
@@ -544,55 +566,58 @@ __global__ void __launch_bounds__(64 * kAttendWaves, 2) k_attend_rows(AttendArgs
         it.skip(a, tile.s, behind, kAttendWaves);
         find_page(it.t);
         __builtin_amdgcn_sched_barrier(0);
-        float top = -INFINITY;
+        f16x8 w[RT][2];
 #pragma unroll
-        for (int b = 0; b < 4; ++b) {
-            const f32x4 sk = *(const f32x4*)&lds_step[wave][0][16 * quarter + 4 * b], lv = *(const f32x4*)&lds_step[wave][1][16 * quarter + 4 * b];
+        for (int t = 0; t < RT; ++t) {
+            float top = -INFINITY;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) s[b][j] = fmaf(s[b][j] * q_back, sk[j], lv[j]);
-        }
-        if (!a.ids && cur.k + kTileKeys > cur.length - first_behind) {       // some row may not see all of it
-            const int see = cur.length - see_after - cur.k - 16 * quarter;
+            for (int b = 0; b < 4; ++b) {
+                const f32x4 sk = *(const f32x4*)&lds_step[wave][0][16 * quarter + 4 * b], lv = *(const f32x4*)&lds_step[wave][1][16 * quarter + 4 * b];
 #pragma unroll
-            for (int b = 0; b < 4; ++b)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) s[b][j] = 4 * b + j < see ? s[b][j] : -INFINITY;
-        }
-#pragma unroll
-        for (int b = 0; b < 4; ++b)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) top = fmaxf(top, s[b][j]);
-        if (__ballot(top > M + (kSlack + kLift))) {
-            top = fmaxf(top, __shfl_xor(top, 32, 64));
-            top = fmaxf(top, __shfl_xor(top, 16, 64));
-            const float m_new = fmaxf(M, top - kLift), d = M - (m_new == -INFINITY ? 0.0f : m_new);
-            const float shrink = __builtin_amdgcn_exp2f(d);
-            L = times_exp2(L, d);
-            M = m_new;
-#pragma unroll
-            for (int i = 0; i < DT; ++i) acc[i] = acc[i] * shrink;
-        }
-        const float m_use = M == -INFINITY ? 0.0f : M;
-        float l = 0.0f;                                         // the tile's part of the sum: terms far below the sum so far would each be rounded away
-        if (wild) {
-#pragma unroll
-            for (int b = 0; b < 4; ++b)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) l += sum_term(s[b][j], m_use, lds_step[wave][2][16 * quarter + 4 * b + j]);
-        }
-        f16x8 w[2];
-#pragma unroll
-        for (int b = 0; b < 4; ++b) {
-            const f32x4 iv = *(const f32x4*)&lds_step[wave][2][16 * quarter + 4 * b];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float e = __builtin_amdgcn_exp2f(s[b][j] - m_use);
-                if (!wild) l = fmaf(e, iv[j], l);
-                w[b >> 1][FOUR ? token_place(4 * (b & 1) + j) : 4 * (b & 1) + j] = (_Float16)e;
+                for (int j = 0; j < 4; ++j) s[t][b][j] = fmaf(s[t][b][j] * q_back[t], sk[j], lv[j]);
             }
+            if (!a.ids && cur.k + kTileKeys > cur.length - first_behind) {       // some row may not see all of it
+                const int see = cur.length - see_after[t] - cur.k - 16 * quarter;
+#pragma unroll
+                for (int b = 0; b < 4; ++b)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) s[t][b][j] = 4 * b + j < see ? s[t][b][j] : -INFINITY;
+            }
+#pragma unroll
+            for (int b = 0; b < 4; ++b)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) top = fmaxf(top, s[t][b][j]);
+            if (__ballot(top > M[t] + (kSlack + kLift))) {
+                top = fmaxf(top, __shfl_xor(top, 32, 64));
+                top = fmaxf(top, __shfl_xor(top, 16, 64));
+                const float m_new = fmaxf(M[t], top - kLift), d = M[t] - (m_new == -INFINITY ? 0.0f : m_new);
+                const float shrink = __builtin_amdgcn_exp2f(d);
+                L[t] = times_exp2(L[t], d);
+                M[t] = m_new;
+#pragma unroll
+                for (int i = 0; i < DT; ++i) acc[t][i] = acc[t][i] * shrink;
+            }
+            const float m_use = M[t] == -INFINITY ? 0.0f : M[t];
+            float l = 0.0f;                                         // the tile's part of the sum: terms far below the sum so far would each be rounded away
+            if (wild) {
+#pragma unroll
+                for (int b = 0; b < 4; ++b)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) l += sum_term(s[t][b][j], m_use, lds_step[wave][2][16 * quarter + 4 * b + j]);
+            }
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+                const f32x4 iv = *(const f32x4*)&lds_step[wave][2][16 * quarter + 4 * b];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float e = __builtin_amdgcn_exp2f(s[t][b][j] - m_use);
+                    if (!wild) l = fmaf(e, iv[j], l);
+                    w[t][b >> 1][FOUR ? token_place(4 * (b & 1) + j) : 4 * (b & 1) + j] = (_Float16)e;
+                }
+            }
+            L[t] += l;
+            asm volatile("" : "+v"(L[t]));                             // (the sum is formed here: kept for later, its terms would fill the registers)
         }
-        L += l;
-        asm volatile("" : "+v"(L));                             // (the sum is formed here: kept for later, its terms would fill the registers)
         if constexpr (FOUR) {
 #pragma unroll
             for (int i = 0; i < VT; ++i)
@@ -601,61 +626,72 @@ __global__ void __launch_bounds__(64 * kAttendWaves, 2) k_attend_rows(AttendArgs
                     const f16x8 r = *(const f16x8*)&lds_vf[wave][i][16 * quarter + 8 * o];
                     uint32_t low, high;
                     split_values4((uint32_t)vr[i][2 * o], (uint32_t)vr[i][2 * o + 1], low, high);
-                    acc[2 * i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes4_to_half(low) * r, w[o], acc[2 * i], 0, 0, 0);
-                    acc[2 * i + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes4_to_half(high) * r, w[o], acc[2 * i + 1], 0, 0, 0);
+                    const f16x8 v0 = codes4_to_half(low) * r, v1 = codes4_to_half(high) * r;
+#pragma unroll
+                    for (int t = 0; t < RT; ++t) {
+                        acc[t][2 * i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, w[t][o], acc[t][2 * i], 0, 0, 0);
+                        acc[t][2 * i + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, w[t][o], acc[t][2 * i + 1], 0, 0, 0);
+                    }
                 }
         } else
 #pragma unroll
         for (int i = 0; i < DT; ++i) {
             f16x8 lo, hi;
             codes_to_half(vr[i], lo, hi);
-            acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo, w[0], acc[i], 0, 0, 0);
-            acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi, w[1], acc[i], 0, 0, 0);
+#pragma unroll
+            for (int t = 0; t < RT; ++t) {
+                acc[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lo, w[t][0], acc[t][i], 0, 0, 0);
+                acc[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(hi, w[t][1], acc[t][i], 0, 0, 0);
+            }
         }
         __builtin_amdgcn_sched_barrier(0);
         fetch_values(nxt.have, row_of_tile, row_of_key, place);
         cur = nxt;
     }
-    L += __shfl_xor(L, 32, 64);
-    L += __shfl_xor(L, 16, 64);
-
-    // join the wavefronts
-    if (quarter == 0) { lds_m[wave][n] = M; lds_l[wave][n] = L; }
-    __syncthreads();
-    float m_all = lds_m[0][n];
+    // join the wavefronts, a tile of rows at a time
 #pragma unroll
-    for (int w = 1; w < kAttendWaves; ++w) m_all = fmaxf(m_all, lds_m[w][n]);
-    {
-        const float f = __builtin_amdgcn_exp2f(M - (m_all == -INFINITY ? 0.0f : m_all));
+    for (int rt = 0; rt < RT; ++rt) {
+        float l_all = L[rt];
+        l_all += __shfl_xor(l_all, 32, 64);
+        l_all += __shfl_xor(l_all, 16, 64);
+        if (rt) __syncthreads();                                // (the last tile's have been read)
+        if (quarter == 0) { lds_m[wave][n] = M[rt]; lds_l[wave][n] = l_all; }
+        __syncthreads();
+        float m_all = lds_m[0][n];
 #pragma unroll
-        for (int i = 0; i < DT; ++i) *(f32x4*)&lds_acc[wave][n][16 * i + 4 * quarter] = acc[i] * f;
-    }
-    __syncthreads();
-    constexpr int Q = D / 4;
-    const int heads = a.st.heads * a.group;
-    for (int i = threadIdx.x; i < kRows * Q; i += 64 * kAttendWaves) {
-        const int rr = i / Q, d = (i - rr * Q) * 4;
-        const int grow = tile.row0 + rr;
-        if (grow >= rows) break;
-        float m = lds_m[0][rr];
+        for (int w = 1; w < kAttendWaves; ++w) m_all = fmaxf(m_all, lds_m[w][n]);
+        {
+            const float f = __builtin_amdgcn_exp2f(M[rt] - (m_all == -INFINITY ? 0.0f : m_all));
 #pragma unroll
-        for (int w = 1; w < kAttendWaves; ++w) m = fmaxf(m, lds_m[w][rr]);
-        const float m_use = m == -INFINITY ? 0.0f : m;
-        float l = 0.0f;
-        f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-        for (int w = 0; w < kAttendWaves; ++w) {
-            l += times_exp2(lds_l[w][rr], lds_m[w][rr] - m_use);
-            o += *(const f32x4*)&lds_acc[w][rr][d];
+            for (int i = 0; i < DT; ++i) *(f32x4*)&lds_acc[wave][n][16 * i + 4 * quarter] = acc[rt][i] * f;
         }
-        const int t = tile.first + grow / a.group, hq = head * a.group + grow % a.group;
-        if (a.splits == 1) {
-            const float inv = l == 0.0f ? 0.0f : kUnlift / l;
-            store4<T>(a.out, (int64_t)t * a.out_token + (int64_t)hq * a.out_head + d, a.out_wide, o * inv);
-        } else {
-            const int64_t at = ((int64_t)split * a.tokens + t) * heads + hq;
-            if (l != 0.0f) *(f32x4*)&a.part_acc[at * D + d] = o;       // (l = 0: no key was seen, and nothing is read there)
-            if (d == 0) { a.part_m[at] = m; a.part_l[at] = l; }
+        __syncthreads();
+        constexpr int Q = D / 4;
+        const int heads = a.st.heads * a.group;
+        for (int i = threadIdx.x; i < kRows * Q; i += 64 * kAttendWaves) {
+            const int rr = i / Q, d = (i - rr * Q) * 4;
+            const int grow = tile.row0 + kRows * rt + rr;
+            if (grow >= rows) break;
+            float m = lds_m[0][rr];
+#pragma unroll
+            for (int w = 1; w < kAttendWaves; ++w) m = fmaxf(m, lds_m[w][rr]);
+            const float m_use = m == -INFINITY ? 0.0f : m;
+            float l = 0.0f;
+            f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int w = 0; w < kAttendWaves; ++w) {
+                l += times_exp2(lds_l[w][rr], lds_m[w][rr] - m_use);
+                o += *(const f32x4*)&lds_acc[w][rr][d];
+            }
+            const int t = tile.first + grow / a.group, hq = head * a.group + grow % a.group;
+            if (a.splits == 1) {
+                const float inv = l == 0.0f ? 0.0f : kUnlift / l;
+                store4<T>(a.out, (int64_t)t * a.out_token + (int64_t)hq * a.out_head + d, a.out_wide, o * inv);
+            } else {
+                const int64_t at = ((int64_t)split * a.tokens + t) * heads + hq;
+                if (l != 0.0f) *(f32x4*)&a.part_acc[at * D + d] = o;       // (l = 0: no key was seen, and nothing is read there)
+                if (d == 0) { a.part_m[at] = m; a.part_l[at] = l; }
+            }
         }
     }
 }

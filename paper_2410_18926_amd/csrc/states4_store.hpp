@@ -147,7 +147,7 @@ __global__ void __launch_bounds__(256) k_states4_write(Store st, TokenRows k, To
         const bool bad = most >= 0x7f800000u, zero = bad || top < kTinyRow;
         const uint32_t r = factor_bits(zero ? 0.0f : __uint_as_float(group), zero ? 1.0f : top);
         code[i] = zero ? 0u : codes4_of<T>(f[i], __uint_as_float(r), zero ? 1.0f : top);
-        uint32_t factors = d < dim ? (r >> 20) - 896u << (8 * (lane >> 2)) : 0u;              // (the exponent moves from a float's offset to binary16's)
+        uint32_t factors = d < dim ? ((r >> 20) - 896u) << (8 * (lane >> 2)) : 0u;              // (the exponent moves from a float's offset to binary16's)
         factors |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)factors, 0x128, 0xf, 0xf, true);
         factors |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)factors, 0x124, 0xf, 0xf, true);
         const int64_t slot = bs.slot[t];

@@ -91,6 +91,7 @@ int check_tokens(const St* st, int32_t type, int64_t tokens) {
 
 struct Plan {
     int32_t waves;                   // wavefronts of a block of k_attend_tile (32 rows each); 0: k_attend_rows
+    int32_t row_tiles;               // tiles of 16 rows of a block of k_attend_rows
     int64_t tiles;                   // row tiles over all sequences, at most
     int32_t unit, units, splits, per_split;
     int64_t workspace;
@@ -107,6 +108,22 @@ constexpr int64_t kMostKeys = 16384, kMostTileKeys = 32768, kMostPartRows = 1 <<
 // The rows are the call's mean, one kernel takes all its sequences, and the figures are of sequences alike.  Pieces of prompts beside single tokens may do better in calls of
 // their own: 200 single tokens and a piece of 512, each over 2000 keys, 227 us together, 157 + 60 apart; 63 and 1024: 174, 44 + 83; 255 and 2048: 497, 189 + 153.
 constexpr int64_t kMostFewRows = 48;
+// 4 bits: a block of k_attend_rows may have two tiles of 16 rows, for which the codes are converted once, and is taken up to more rows.  us of k_attend_tile / one tile / two, over 32 sequences of
+// 4096 keys and over ten passages of 512 for each of 24:
+//   values, heads, page    32 rows                       48 rows                        64 rows                          96 rows
+//   64, 16, 16             140 72 60   156 71 71         144 99 110   160 110 114       143 126 109   159 130 114        150 185 160   160 187 170
+//   96, 8, 32              158 51 49   123 66 62         164 75 68    183 100 85        165 97 69     184 103 84         169 137 105   184 160 130
+//   128, 8, 64             133 59 59   115 72 71         136 86 79    154 108 95        134 110 81    152 111 96         140 156 119   154 169 146
+//   128, 8, 16             159 59 73   123 72 84         159 89 90    168 111 106       161 109 92    170 114 107        167 158 146   170 172 172
+// (Four tiles of 64 values: 125 at 64 rows, the registers spill.)
+constexpr int64_t kMostFewRows4 = 64, kMostWideRows4 = 96;      // up to 64 values, and above
+template <typename St>
+int32_t row_tiles4(const St* st, int64_t mean_rows) {
+    const int64_t tiles = ceil_div(mean_rows, kRows);
+    if (tiles <= 1) return 1;
+    if (st->dim <= 64) return tiles % 2 ? 1 : 2;
+    return tiles == 2 && st->dim == 128 && st->page_size < 64 ? 1 : 2;
+}
 // Blocks of k_attend_tile have 4 wavefronts, or 8 where they still fill the GPU and little of them is empty: then the codes are converted for 256 rows at once.
 // us of 4 / 8 wavefronts: 4096 tokens of 32 heads over 32768 keys 2336 / 2161, 16 x 256 tokens over 4352 keys 344 / 324; 8 heads of 96, 4096 tokens over 12288
 // keys 724 / 679; with 256 blocks only, 2048 tokens over 16384 keys, 610 / 595; at a dimension of 64, 4096 tokens over 16384 keys 769 / 729, but 16 x 512 over 2048
@@ -136,8 +153,10 @@ Plan plan_of(const St* st, const lorann_questions* qs, int32_t found, int32_t wi
     const int64_t group = qs->heads / st->heads;
     const int64_t sequences = std::max<int64_t>(qs->sequences, 1), mean_rows = qs->tokens * group / sequences;
     auto tiles_of = [&](int64_t rows) { return qs->q_start ? qs->tokens * group / rows + sequences : sequences * ceil_div(mean_rows, rows); };
-    p.waves = mean_rows <= kMostFewRows ? 0 : tiles_of(256) * st->heads >= kManyBlocks && mean_rows >= kManyRows && st->dim > kDimForFour ? 8 : 4;
-    p.tiles = tiles_of(p.waves ? 32 * p.waves : kRows);
+    constexpr bool four = std::is_same_v<St, lorann_states4>;
+    p.row_tiles = four ? row_tiles4(st, mean_rows) : 1;
+    p.waves = mean_rows <= (!four ? kMostFewRows : st->dim > kDimForFour ? kMostWideRows4 : kMostFewRows4) ? 0 : tiles_of(256) * st->heads >= kManyBlocks && mean_rows >= kManyRows && st->dim > kDimForFour ? 8 : 4;
+    p.tiles = tiles_of(p.waves ? 32 * p.waves : kRows * p.row_tiles);
     const int64_t table_keys = std::max<int64_t>((int64_t)width * st->page_size, 1), tables = std::max(found, 1), keys = tables * table_keys;
     const int64_t blocks = std::max<int64_t>(p.tiles * st->heads, 1), rows = std::max<int64_t>(qs->tokens * qs->heads, 1);
     const int64_t want = std::max(std::max<int64_t>(1, std::min(kBlocksWanted / blocks, ceil_div(keys, kKeysPerBlock))), std::min(ceil_div(keys, p.waves ? kMostTileKeys : kMostKeys), kMostPartRows / rows));
@@ -168,9 +187,12 @@ void launch_attend(const Plan& p, const AttendArgs& a, dim3 grid, dim3 block, hi
     } else if (p.waves) {
         if (whole) hipLaunchKernelGGL((k_attend_tile<T, D, 4, true, BITS>), grid, block, 0, stream, a);
         else hipLaunchKernelGGL((k_attend_tile<T, D, 4, false, BITS>), grid, block, 0, stream, a);
-    } else {
-        if (whole) hipLaunchKernelGGL((k_attend_rows<T, D, true, BITS>), grid, block, 0, stream, a);
-        else hipLaunchKernelGGL((k_attend_rows<T, D, false, BITS>), grid, block, 0, stream, a);
+    } else if (p.row_tiles == 1) {
+        if (whole) hipLaunchKernelGGL((k_attend_rows<T, D, true, BITS, 1>), grid, block, 0, stream, a);
+        else hipLaunchKernelGGL((k_attend_rows<T, D, false, BITS, 1>), grid, block, 0, stream, a);
+    } else if constexpr (BITS == 4) {
+        if (whole) hipLaunchKernelGGL((k_attend_rows<T, D, true, BITS, 2>), grid, block, 0, stream, a);
+        else hipLaunchKernelGGL((k_attend_rows<T, D, false, BITS, 2>), grid, block, 0, stream, a);
     }
     if (p.splits > 1) {
         constexpr int groups = 256 / (D / 4);
