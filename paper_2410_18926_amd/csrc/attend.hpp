@@ -415,18 +415,19 @@ __global__ void __launch_bounds__(64 * kAttendWaves, 2) k_attend_rows(AttendArgs
             rvf = a.st.vf[at];
         }
         if constexpr (FOUR) {
-            const int8_t* base = WHOLE ? a.st.kc + (uint64_t)(uint32_t)row_of_tile * page_bytes + (uint32_t)(place * ROW) : nullptr;
+            const int8_t* base = a.st.kc + (uint64_t)(uint32_t)row_of_tile * page_bytes + (uint32_t)(place * ROW);          // (WHOLE)
 #pragma unroll
             for (int b = 0; b < 4; ++b) {
                 const int key = my_key + 4 * b;
-                const int8_t* kp = WHOLE ? base + here(key * ROW) : a.st.kc + (uint64_t)(uint32_t)__shfl(row_of_key, key, 64) * page_bytes + (uint32_t)((key & (P - 1)) * ROW);
-                if constexpr (D == 128) kr[b][0] = *(const i32x4*)(kp + 16 * quarter);
+                const int8_t* kp = WHOLE ? base : a.st.kc + (uint64_t)(uint32_t)__shfl(row_of_key, key, 64) * page_bytes;
+                const uint32_t at = (uint32_t)((WHOLE ? key : key & (P - 1)) * ROW);          // (a scalar base and a vector offset where the tile lies in one page)
+                if constexpr (D == 128) kr[b][0] = *(const i32x4*)(kp + here(at + 16 * quarter));
                 if constexpr (C == 1) {
-                    const i32x2 two = *(const i32x2*)(kp + 8 * quarter);
+                    const i32x2 two = *(const i32x2*)(kp + here(at + 8 * quarter));
                     kr[b][0][0] = two[0];
                     kr[b][0][1] = two[1];
                 }
-                if constexpr (ODD) kr[b][0][2 * C] = *(const int*)(kp + 32 * C + 4 * quarter);
+                if constexpr (ODD) kr[b][0][2 * C] = *(const int*)(kp + here(at + 32 * C + 4 * quarter));
             }
         } else if constexpr (WHOLE) {
             const int8_t* base = a.st.kc + (uint64_t)(uint32_t)row_of_tile * page_bytes + (uint32_t)(place * D);
@@ -599,22 +600,26 @@ __global__ void __launch_bounds__(64 * kAttendWaves, 2) k_attend_rows(AttendArgs
             }
             const float m_use = M[t] == -INFINITY ? 0.0f : M[t];
             float l = 0.0f;                                         // the tile's part of the sum: terms far below the sum so far would each be rounded away
+            auto weigh = [&](auto with_sum) {
+#pragma unroll
+                for (int b = 0; b < 4; ++b) {
+                    const f32x4 iv = *(const f32x4*)&lds_step[wave][2][16 * quarter + 4 * b];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float e = __builtin_amdgcn_exp2f(s[t][b][j] - m_use);
+                        if (decltype(with_sum)::value && !(wild && !FOUR)) l = fmaf(e, iv[j], l);
+                        w[t][b >> 1][FOUR ? token_place(4 * (b & 1) + j) : 4 * (b & 1) + j] = (_Float16)e;
+                    }
+                }
+            };
             if (wild) {
 #pragma unroll
                 for (int b = 0; b < 4; ++b)
 #pragma unroll
                     for (int j = 0; j < 4; ++j) l += sum_term(s[t][b][j], m_use, lds_step[wave][2][16 * quarter + 4 * b + j]);
             }
-#pragma unroll
-            for (int b = 0; b < 4; ++b) {
-                const f32x4 iv = *(const f32x4*)&lds_step[wave][2][16 * quarter + 4 * b];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float e = __builtin_amdgcn_exp2f(s[t][b][j] - m_use);
-                    if (!wild) l = fmaf(e, iv[j], l);
-                    w[t][b >> 1][FOUR ? token_place(4 * (b & 1) + j) : 4 * (b & 1) + j] = (_Float16)e;
-                }
-            }
+            if (FOUR && wild) weigh(std::false_type{});             // (8 bits: one copy, with a select)
+            else weigh(std::true_type{});
             L[t] += l;
             asm volatile("" : "+v"(L[t]));                             // (the sum is formed here: kept for later, its terms would fill the registers)
         }
