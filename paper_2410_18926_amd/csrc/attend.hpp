@@ -127,31 +127,6 @@ __device__ __forceinline__ void codes_to_half(const i32x4 c, f16x8& lo, f16x8& h
     hi = b.h - off;
 }
 
-template <typename T> struct Bits16;
-template <> struct Bits16<_Float16> {
-    static __device__ __forceinline__ float widen(uint16_t u) { union { uint16_t u; _Float16 h; } x; x.u = u; return (float)x.h; }
-    static __device__ __forceinline__ uint16_t narrow(float f) { union { uint16_t u; _Float16 h; } x; x.h = (_Float16)f; return x.u; }
-};
-template <> struct Bits16<__bf16> {
-    static __device__ __forceinline__ float widen(uint16_t u) { return __uint_as_float((uint32_t)u << 16); }
-    static __device__ __forceinline__ uint16_t narrow(float f) { union { uint16_t u; __bf16 h; } x; x.h = (__bf16)f; return x.u; }
-};
-
-// Eight consecutive 16-bit elements, two to a register.
-__device__ __forceinline__ i32x4 load8_raw(const void* base, int64_t at, bool wide) {
-    const uint16_t* p = (const uint16_t*)base + at;
-    if (wide) return *(const i32x4*)p;
-    i32x4 v;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] = (int)((uint32_t)p[2 * j] | (uint32_t)p[2 * j + 1] << 16);
-    return v;
-}
-template <typename T>
-__device__ __forceinline__ void widen8(const i32x4 v, float (&f)[8]) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) f[j] = Bits16<T>::widen((uint16_t)((uint32_t)v[j >> 1] >> (16 * (j & 1))));
-}
-
 template <typename T>
 __device__ __forceinline__ void store4(void* base, int64_t at, bool wide, const f32x4 f) {
     uint16_t* p = (uint16_t*)base + at;

@@ -12,7 +12,7 @@ int lorann_states4_write(const lorann_states4* st, const void* k, const void* v,
     if ((rc = check_sizes(st)) || (rc = check_tokens(st, type, tokens))) return rc;
     if (tokens == 0) return LORANN_OK;
     if ((rc = check_rows(st, slots, k, v, type, true, gpu))) return rc;
-    const dim3 grid = rows_grid(st, tokens);
+    const dim3 grid = heads_grid(st, tokens);
     const TokenRows kr = rows_of(const_cast<void*>(k), k_token, k_head, type), vr = rows_of(const_cast<void*>(v), v_token, v_head, type);
     hipStream_t s = (hipStream_t)hip_stream;
     if (type == LORANN_F32) hipLaunchKernelGGL((k_states4_write<float>), grid, dim3(256), 0, s, view(st), kr, vr, slots, tokens, st->dim);

@@ -12,13 +12,55 @@ __device__ __forceinline__ uint32_t quad_max_u32(uint32_t v) {
 }
 __device__ __forceinline__ uint32_t other_pair(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4e, 0xf, 0xf, true); }
 
-// The smallest r = (1 + m / 8) 2^e >= 2^-13 with r * top >= group, as a float's bits.  group / top is rounded upwards to four bits; where the quotient's own rounding hid a
-// remainder, the product shows it (its sign is exact).
-__device__ __forceinline__ uint32_t factor_bits(float group, float top) {
-    const uint32_t q = max(__float_as_uint(group / top), 0x39000000u);
+// The smallest r = (1 + m / 8) 2^e >= 2^-13 with r * top >= group, as a float's bits; inv = 1 / top within a few units of the last place.  A quotient surely not above the exact one is
+// rounded upwards to four bits: that is r or the number below it, which the product shows (the sign of a fused sum is exact).
+__device__ __forceinline__ uint32_t factor_bits(float group, float top, float inv) {
+    const uint32_t q = max(__float_as_uint(group * inv * (1.0f - 0x1p-20f)), 0x39000000u);
     const uint32_t r = (q + 0xfffffu) & 0xfff00000u;
     return fmaf(__uint_as_float(r), top, -group) < 0.0f ? r + 0x100000u : r;
 }
+
+// top / 6, rounded as a division rounds: the product with the rounded reciprocal, corrected by its remainder once (top is 2^-100 or more).
+__device__ __forceinline__ float sixth(float top) {
+    const float q = top * (1.0f / 6.0f);
+    return fmaf(fmaf(-q, 6.0f, top), 1.0f / 6.0f, q);
+}
+
+// Eight consecutive elements of a row, and the bits of the largest magnitude among them as a float: infinities and NaN are above every number.  16-bit elements are compared two at a time as
+// they stand.
+template <typename T>
+struct Row8 {                                  // 16-bit elements, two to a register
+    i32x4 raw;
+    __device__ __forceinline__ void load(const T* p, bool wide) { raw = load8_raw(p, 0, wide); }
+    __device__ __forceinline__ void clear() { raw = i32x4{0, 0, 0, 0}; }
+    __device__ __forceinline__ uint32_t largest() const {
+        typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+        u16x2 m = {0, 0};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, (uint32_t)raw[j] & 0x7fff7fffu));
+        return __float_as_uint(Bits16<T>::widen(max(m[0], m[1])));
+    }
+    __device__ __forceinline__ void values(float (&f)[8]) const { widen8<T>(raw, f); }
+};
+template <>
+struct Row8<float> {
+    float f[8];
+    __device__ __forceinline__ void load(const float* p, bool wide) { Eight<float>::load(p, wide, f); }
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = 0.0f;
+    }
+    __device__ __forceinline__ uint32_t largest() const {
+        uint32_t m = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) m = max(m, __float_as_uint(f[j]) & 0x7fffffffu);
+        return m;
+    }
+    __device__ __forceinline__ void values(float (&to)[8]) const {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) to[j] = f[j];
+    }
+};
 
 // Eight codes of a row: nearest to 6 x / (r top), halfway to the even code, exactly.
 //   16-bit elements: 6 x (14 bits) and r top (15 bits) are exact floats.  The quotient is corrected by its remainder once, so that it is off by at most 2^-23 relative and is
@@ -99,38 +141,37 @@ __device__ __forceinline__ uint32_t from_value_rows(uint32_t own, int l) {
 // apart) are turned together: afterwards lane L holds, for the first of them in the lower half of the wavefront and for the second in the upper, the four tokens' bytes of two rows.
 __device__ __forceinline__ int turned_row(int lane) { return value_row(lane & 15) + (lane >> 4 & 1) * 2; }
 
+// Blocks: the heads' keys, then their values, of 64 tokens, then those of the next tokens: rows of a token lie side by side in the caller's projection (50000 tokens of 8 heads of 128, slices of
+// one of 48 heads: 93 us with the token blocks first, 73 so; reading back, where whole rows are written, 60 and 65).
 template <typename T>
 __global__ void __launch_bounds__(256) k_states4_write(Store st, TokenRows k, TokenRows v, const int64_t* __restrict__ slots, int64_t tokens, int dim) {
     __shared__ BlockSlots bs;
     __shared__ __align__(16) uint8_t lds[64 * kTokenStride + 16];
-    const int64_t token0 = (int64_t)blockIdx.x * kBlockTokens;
-    const int head = blockIdx.y;
-    const bool values = blockIdx.z;
+    const int64_t token0 = ((int64_t)blockIdx.z * gridDim.y + blockIdx.y) * kBlockTokens;
+    const bool values = blockIdx.x >= (unsigned)st.heads;
+    const int head = blockIdx.x - (values ? st.heads : 0);
+    if (token0 >= tokens) return;
     const TokenRows in = values ? v : k;
     const int lane = threadIdx.x & 15, d = lane * 8, P = 1 << st.shift, half = dim / 2;
     const int last = (int)min(tokens - 1 - token0, (int64_t)kBlockTokens - 1);
     // a group of 16 lanes per row, 16 rows at a time: all rows are requested first, without regard to their slots
-    float f[4][8];
+    Row8<T> f[4];
     {
         const T* x = (const T*)in.p + token0 * in.token + head * in.head + (d < dim ? d : 0);
         const int t = threadIdx.x >> 4;
         if (last >= 16) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) Eight<T>::load(x + min(i * 16 + t, last) * in.token, in.wide, f[i]);
+            for (int i = 0; i < 4; ++i) f[i].load(x + min(i * 16 + t, last) * in.token, in.wide);
         } else {                                               // (a few tokens: one row a group)
-            Eight<T>::load(x + min(t, last) * in.token, in.wide, f[0]);
+            f[0].load(x + min(t, last) * in.token, in.wide);
 #pragma unroll
-            for (int i = 1; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) f[i][j] = 0.0f;
+            for (int i = 1; i < 4; ++i) f[i].clear();
         }
     }
     load_slots(bs, st, slots, token0, tokens, values);
     if (d >= dim) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) f[i][j] = 0.0f;
+        for (int i = 0; i < 4; ++i) f[i].clear();
     }
     uint32_t code[4];
 #pragma unroll
@@ -138,16 +179,14 @@ __global__ void __launch_bounds__(256) k_states4_write(Store st, TokenRows k, To
         code[i] = 0;
         if (i > 0 && last < 16) continue;
         const int t = i * 16 + (threadIdx.x >> 4);
-        uint32_t group = 0;                                    // bits of the largest magnitude of 32: infinities and NaN are above every number
-#pragma unroll
-        for (int j = 0; j < 8; ++j) group = max(group, __float_as_uint(f[i][j]) & 0x7fffffffu);
-        group = quad_max_u32(group);
-        const uint32_t most = row_max_u32(group);
-        const float top = __uint_as_float(most);
-        const bool bad = most >= 0x7f800000u, zero = bad || top < kTinyRow;
-        const uint32_t r = factor_bits(zero ? 0.0f : __uint_as_float(group), zero ? 1.0f : top);
-        code[i] = zero ? 0u : codes4_of<T>(f[i], __uint_as_float(r), zero ? 1.0f : top);
-        uint32_t factors = d < dim ? ((r >> 20) - 896u) << (8 * (lane >> 2)) : 0u;              // (the exponent moves from a float's offset to binary16's)
+        const uint32_t group = quad_max_u32(f[i].largest()), most = row_max_u32(group);
+        const bool bad = most >= 0x7f800000u, zero = bad || __uint_as_float(most) < kTinyRow;
+        const float top = zero ? 1.0f : __uint_as_float(most);
+        const uint32_t r = factor_bits(zero ? 0.0f : __uint_as_float(group), top, __builtin_amdgcn_rcpf(top));
+        float x[8];
+        f[i].values(x);
+        code[i] = zero ? 0u : codes4_of<T>(x, __uint_as_float(r), top);
+        uint32_t factors = d < dim ? ((r >> 20) - 896u) << (8 * (lane >> 2)) : 0u;            // (the exponent moves from a float's offset to binary16's)
         factors |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)factors, 0x128, 0xf, 0xf, true);
         factors |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)factors, 0x124, 0xf, 0xf, true);
         const int64_t slot = bs.slot[t];
@@ -155,7 +194,7 @@ __global__ void __launch_bounds__(256) k_states4_write(Store st, TokenRows k, To
             const int64_t base = st.row(slot >> st.shift, head);
             const int off = (int)(slot & (P - 1));
             if (lane == 0) {
-                (values ? st.vs : st.ks)[base + off] = bad ? __int_as_float(0x7fc00000) : zero ? 0.0f : top / 6.0f;
+                (values ? st.vs : st.ks)[base + off] = bad ? __int_as_float(0x7fc00000) : zero ? 0.0f : sixth(top);
                 (values ? st.vf : st.kf)[base + off] = factors;
             }
             if (!values && d < dim) *(uint32_t*)(st.kc + (base + off) * half + d / 2) = code[i];

@@ -297,6 +297,12 @@ int check_rows(const St* st, const int64_t* slots, const void* k, const void* v,
 }
 template <typename St>
 dim3 rows_grid(const St* st, int64_t tokens) { return dim3((unsigned)ceil_div(tokens, kBlockTokens), (unsigned)st->heads, 2); }
+// Heads first, keys and values of the same tokens side by side (k_states4_write).
+template <typename St>
+dim3 heads_grid(const St* st, int64_t tokens) {
+    const int64_t blocks = ceil_div(tokens, kBlockTokens), y = std::min<int64_t>(blocks, 32768);
+    return dim3((unsigned)(2 * st->heads), (unsigned)y, (unsigned)ceil_div(blocks, y));
+}
 
 }  // namespace
 }  // namespace lorann

@@ -26,11 +26,15 @@ class States4(States):
         n, h, p, half = k_codes.shape
         self.pages, self.heads, self.page_size, self.dim = n, h, p, 2 * half
         self._gpu = k_codes.device.index if k_codes.is_cuda else None
-        at = [_array(t, dtype, torch.Size(shape), what) for t, dtype, shape, what in (
-            (k_codes, torch.uint8, (n, h, p, half), "k_codes"), (v_codes, torch.uint8, (n, h, half, p), "v_codes"),
-            (k_factors, torch.uint8, (n, h, p, 4), "k_factors"), (v_factors, torch.uint8, (n, h, p, 4), "v_factors"),
-            (k_scales, torch.float32, (n, h, p), "k_scales"), (v_scales, torch.float32, (n, h, p), "v_scales"))]
-        self._st = CStates4(*at, n, h, p, self.dim)
+        steps, factors = (n, h, p), (n, h, p, 4)
+        if not (k_codes.dtype is v_codes.dtype is k_factors.dtype is v_factors.dtype is torch.uint8 and k_scales.dtype is v_scales.dtype is torch.float32
+                and v_codes.shape == (n, h, half, p) and k_factors.shape == factors and v_factors.shape == factors and k_scales.shape == steps and v_scales.shape == steps
+                and k_codes.is_contiguous() and v_codes.is_contiguous() and k_factors.is_contiguous() and v_factors.is_contiguous() and k_scales.is_contiguous() and v_scales.is_contiguous()):
+            for t, dtype, shape, what in ((k_codes, torch.uint8, (n, h, p, half), "k_codes"), (v_codes, torch.uint8, (n, h, half, p), "v_codes"),
+                                          (k_factors, torch.uint8, factors, "k_factors"), (v_factors, torch.uint8, factors, "v_factors"),
+                                          (k_scales, torch.float32, steps, "k_scales"), (v_scales, torch.float32, steps, "v_scales")):
+                _array(t, dtype, shape, what)          # (says which)
+        self._st = CStates4(k_codes.data_ptr(), v_codes.data_ptr(), k_factors.data_ptr(), v_factors.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(), n, h, p, 2 * half)
 
     @classmethod
     def empty(cls, pages: int, heads: int, page_size: int, dim: int, device="cuda") -> "States4":
