@@ -160,7 +160,13 @@ constexpr float kTameLow = 0x1p-45f, kTameHigh = 0x1p10f, kNoStep = 0x1p-84f;
 // The reference M of the weights is raised only when a score passes it by more than kSlack, so the answer's registers are rarely rescaled.  Weights stay below
 // 2^kSlack, and the operands 2^kLift w below 2^15, the last power of two but one that binary16 holds.  (Without the lift, weights below 2^-14 would lose bits and those
 // below 2^-25 become 0 in the numerator alone: an answer of one key 20 to 26 octaves above 2^19 others was up to 1.8 % off.)  The kernels hold M - kLift, called M there.
+// The difference itself is compared: in logits of 2^24 and more, whose neighbours lie 2 to 16 apart, M + kSlack + kLift and top - kLift round, and an operand of 2^16 would be an infinity.
 constexpr float kSlack = 6.0f, kLift = 9.0f;
+__device__ __forceinline__ bool passes(float top, float m) { return top - m > kSlack + kLift; }
+__device__ __forceinline__ float raised(float top, float m) {
+    const float r = fmaxf(m, top - kLift);
+    return passes(top, r) ? top : r;
+}
 constexpr float kUnlift = 1.0f / 512;          // 2^-kLift
 struct KeySteps { float product, add, inverse; bool wild; };
 __device__ __forceinline__ KeySteps key_steps(float ks, float vs, float c, float bias, bool have) {
@@ -563,10 +569,10 @@ __global__ void __launch_bounds__(64 * kAttendWaves, 2) k_attend_rows(AttendArgs
             for (int b = 0; b < 4; ++b)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) top = fmaxf(top, s[t][b][j]);
-            if (__ballot(top > M[t] + (kSlack + kLift))) {
+            if (__ballot(passes(top, M[t]))) {
                 top = fmaxf(top, __shfl_xor(top, 32, 64));
                 top = fmaxf(top, __shfl_xor(top, 16, 64));
-                const float m_new = fmaxf(M[t], top - kLift), d = M[t] - (m_new == -INFINITY ? 0.0f : m_new);
+                const float m_new = raised(top, M[t]), d = M[t] - (m_new == -INFINITY ? 0.0f : m_new);
                 const float shrink = __builtin_amdgcn_exp2f(d);
                 L[t] = times_exp2(L[t], d);
                 M[t] = m_new;

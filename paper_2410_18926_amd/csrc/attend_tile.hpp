@@ -301,9 +301,9 @@ __global__ void __launch_bounds__(64 * NW, 2) k_attend_tile(AttendArgs a) {
     };
     // raises the reference where a row's largest score passes it by more than kSlack (M is kLift below it)
     auto raise = [&](float top) {
-        if (__ballot(top > M + (kSlack + kLift))) {
+        if (__ballot(passes(top, M))) {
             top = fmaxf(top, __shfl_xor(top, 32, 64));
-            const float m_new = fmaxf(M, top - kLift), d = M - (m_new == -INFINITY ? 0.0f : m_new);
+            const float m_new = raised(top, M), d = M - (m_new == -INFINITY ? 0.0f : m_new);
             const float shrink = __builtin_amdgcn_exp2f(d);
             L = times_exp2(L, d);
             M = m_new;
