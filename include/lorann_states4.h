@@ -28,6 +28,7 @@ extern "C" {
  *   v_codes    [pages][heads][dim / 2][page_size] bytes, 16-byte aligned: transposed inside a page, components 32 g + n (low four bits) and 32 g + 16 + n in row 16 g + n
  *   k_factors, v_factors  [pages][heads][page_size][4] bytes, 4-byte aligned: byte g is that of values 32 g .. 32 g + 31; bytes beyond dim / 32 are written as 0 and not used
  *   k_scales, v_scales    [pages][heads][page_size] float: the steps
+ * Bit 7 of a factor's byte is 0 and not looked at; what slots that were never written hold does not matter, as long as no length covers them.
  * A token's codes share no byte with another's: tokens of one call, or of calls on several streams, may be written in any order.
  */
 typedef struct lorann_states4 {

@@ -18,8 +18,10 @@ __device__ __forceinline__ f16x8 codes4_to_half(uint32_t w) {
     return x.h;
 }
 
-// Byte `g` of a row's factors as binary16, in both halves of a register.
+// Byte `g` of a row's factors as binary16, in both halves of a register.  A factor's top bit is 0: it is cleared, so that memory that was never written gives finite numbers too (a weight
+// of 0 times one is 0; the masked keys' steps are not used).
 __device__ __forceinline__ uint32_t factor_pair(uint32_t factors, uint32_t g) {
+    factors &= 0x7f7f7f7fu;
     return __builtin_amdgcn_perm(0u, factors, 0x000c000cu | g << 8 | g << 24) >> 1;          // (the byte at bits 8 .. 15 of each half, then moved down by one)
 }
 __device__ __forceinline__ f16x8 spread(uint32_t pair) {
@@ -29,7 +31,7 @@ __device__ __forceinline__ f16x8 spread(uint32_t pair) {
 }
 __device__ __forceinline__ _Float16 factor_half(uint32_t factors, int g) {
     union { uint16_t u; _Float16 h; } x;
-    x.u = (uint16_t)((factors >> (8 * g) & 255u) << 7);
+    x.u = (uint16_t)((factors >> (8 * g) & 127u) << 7);
     return x.h;
 }
 

@@ -195,6 +195,35 @@ def test_passages(S, new, found, stock, heads, group, dim, page, dtype, weighted
     assert torch.equal(got, st.attend_passages(q, dev(ids, torch.int64), dev(tables), dev(stock), q_start=dev(start), **args)), "two runs differ"
 
 
+@pytest.mark.parametrize("new,dim,page", [(1, 128, 64), (12, 96, 16), (60, 64, 32), (300, 128, 16)])
+def test_memory_that_was_never_written(S, new, dim, page):
+    """A store made over memory that holds anything (bytes of ones: as factors, NaN in binary16; NaN steps): what no length covers changes no answer and no sum."""
+    g = gen(new)
+    n, heads = 333, 2
+    pages = -(-n // page) + 1
+    k, v = randn(g, n, heads, dim), randn(g, n, heads, dim)
+    q = randn(g, new, 2 * heads, dim).to(BF16)
+    tables = torch.arange(pages + 1, dtype=torch.int32, device="cuda")[None].flip(1).contiguous()          # (pages .. 0: page 0, which stands in for pages that are not there, is not written either)
+    tables[0, 2] = 10 ** 6
+    at = torch.arange(n, device="cuda")
+    slots = tables[0, at // page].long() * page + at % page
+    got = []
+    for fill in (False, True):
+        st = S.States4.empty(pages + 1, heads, page, dim)
+        if fill:
+            for t in (st.k_codes, st.v_codes, st.k_factors, st.v_factors):
+                t.fill_(255)
+            st.k_scales.fill_(float("nan"))
+            st.v_scales.fill_(float("inf"))
+        st.write(k, v, slots)
+        lengths = dev([n])
+        ids, dists = dev([[0, 0, 0]], torch.int64), torch.zeros((1, 3), device="cuda")
+        got.append((st.attend_chunk(q, tables, lengths), st.attend_passages(q, ids, tables, lengths, scores=dists), st.attend_weights(q, tables, lengths),
+                    *st.read(torch.cat([slots, slots.new_tensor([-1, 10 ** 9])]))))
+        assert all(torch.isfinite(x).all() for x in got[-1])
+    assert all(torch.equal(x, y) for x, y in zip(*got))
+
+
 @pytest.mark.parametrize("new,dim,page", [(1, 128, 64), (40, 64, 16), (60, 96, 32)])
 def test_keys_that_hold_nothing_or_no_number(S, new, dim, page):
     """Rows of zeros take their share of the weights alone; a NaN reaches the queries that see its key and no others; pages outside the store are left out."""
