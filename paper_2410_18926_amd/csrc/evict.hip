@@ -169,7 +169,8 @@ int evict(const St* st, const int32_t* tables, int32_t width, const int32_t* len
     if ((rc = check_store(st, gpu))) return rc;
     if (width > 0 && ((rc = check_device(tables, "tables", gpu)) || (rc = check_device(sums, "sums", gpu)))) return rc;
     if ((rc = check_device(lengths, "lengths", gpu)) || (rc = check_device(kept_lengths, "kept_lengths", gpu))) return rc;
-    if (budget > 0 && ((rc = check_device(to_tables, "to_tables", gpu)) || (rc = check_device(kept, "kept", gpu)))) return rc;
+    if (budget > 0 && (rc = check_device(kept, "kept", gpu))) return rc;
+    if (to_width > 0 && (budget > 0 || kept_sums) && (rc = check_device(to_tables, "to_tables", gpu))) return rc;          // (where the move runs, it reads them)
     if (kept_sums && to_width > 0 && (rc = check_device(kept_sums, "kept_sums", gpu))) return rc;
     if (!aligned(sums, 4) || !aligned(kept, 4) || !aligned(kept_lengths, 4) || !aligned(kept_sums, 4)) return fail(LORANN_E_INVAL, "an array is not 4-byte aligned");
     const int64_t seats = sequences * st->heads, keys = (int64_t)width * st->page_size, room = evict_room(seats, keys), chunks = evict_chunks(keys);

@@ -216,6 +216,17 @@ def test_keep_nothing(B):
     assert all(np.array_equal(before[n], a, equal_nan=True) for n, a in arrays(st).items())
 
 
+def test_destinations_in_host_memory_are_refused(B):
+    """Also where no token is kept: the sums behind the last are written for their pages."""
+    from paper_2410_18926_amd.binding import LorannError
+    _, filled, _ = B
+    st = filled(6, 2, 16, 32)
+    tables, lengths, sums = dev([[0, 1], [2, 3]]), dev([20, 32]), torch.rand((2, 2, 32), device="cuda")
+    for budget in (0, 5):
+        with pytest.raises(LorannError, match="to_tables"):
+            st.evict(tables, lengths, sums, budget, torch.tensor([[4], [5]], dtype=torch.int32))
+
+
 def test_a_conversation_within_a_budget(B):
     """Prompt, its weights, eviction, further tokens behind what was kept, their weights, eviction again: as a decoder would, every step against the definitions."""
     Store, _, held = B
