@@ -150,7 +150,7 @@ constexpr int64_t kChooseKeys = 16 * kChooseThreads;
 int64_t evict_chunks(int64_t keys) { return ceil_div(keys, kChunk); }
 int64_t evict_room(int64_t seats, int64_t keys) {
     if (keys <= kChooseKeys) return 0;
-    return ceil_div(seats * evict_chunks(keys) * (2 * kBins + 1) * 4 + seats * 16, 16) * 16;
+    return ceil_div(seats * evict_chunks(keys) * (2 * kBins + 3) * 4 + seats * 16, 16) * 16;
 }
 
 template <typename St>
@@ -199,7 +199,8 @@ int evict(const St* st, const int32_t* tables, int32_t width, const int32_t* len
         c.chunks = (int32_t)chunks;
         c.hist[0] = (uint32_t*)workspace;
         c.hist[1] = c.hist[0] + seats * chunks * kBins;
-        c.place = c.hist[1] + seats * chunks * kBins;
+        c.there = (uint2*)(c.hist[1] + seats * chunks * kBins);
+        c.place = (uint32_t*)(c.there + seats * chunks);
         c.state = c.place + seats * chunks;
         const dim3 grid((unsigned)(seats * chunks)), block(kChooseThreads);
         hipLaunchKernelGGL(k_evict_chunks<0>, grid, block, 0, stream, c, wide);

@@ -53,6 +53,28 @@ __device__ __forceinline__ uint32_t block_prefix(uint32_t v, uint32_t* lds, uint
     return before + upto - v;
 }
 
+// The sum over the block of two numbers at once.  Two barriers.
+__device__ __forceinline__ uint2 block_sums(uint2 v, uint32_t* lds) {
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        v.x += __shfl_xor(v.x, o, 64);
+        v.y += __shfl_xor(v.y, o, 64);
+    }
+    if ((threadIdx.x & 63) == 0) {
+        lds[threadIdx.x >> 6] = v.x;
+        lds[kChooseWaves + (threadIdx.x >> 6)] = v.y;
+    }
+    __syncthreads();
+    uint2 all = {0, 0};
+#pragma unroll
+    for (int w = 0; w < kChooseWaves; ++w) {
+        all.x += lds[w];
+        all.y += lds[kChooseWaves + w];
+    }
+    __syncthreads();
+    return all;
+}
+
 // A sequence and head: where its arrays are, how long it is.
 struct Seat {
     int s, head, n, old;
@@ -76,17 +98,22 @@ struct Seat {
 struct Wanted {
     uint32_t all, olds, want, choose;
     __device__ __forceinline__ Wanted(const EvictArgs& a, const Seat& q, uint32_t* lds) {
-        uint32_t mine = 0, mine_old = 0;
+        uint2 mine = {0, 0};
         const int P = 1 << a.st.shift;
         for (int p = threadIdx.x; (int64_t)p << a.st.shift < q.n; p += kChooseThreads) {
             const int j = p << a.st.shift;
             if (q.there(a, j)) {
-                mine += min(P, q.n - j);
-                mine_old += min(P, max(q.old - j, 0));
+                mine.x += min(P, q.n - j);
+                mine.y += min(P, max(q.old - j, 0));
             }
         }
-        block_prefix(mine, lds, all);
-        block_prefix(mine_old, lds, olds);
+        mine = block_sums(mine, lds);
+        set(a, mine.x, mine.y);
+    }
+    __device__ __forceinline__ Wanted(const EvictArgs& a, uint32_t there, uint32_t old) { set(a, there, old); }
+    __device__ __forceinline__ void set(const EvictArgs& a, uint32_t there, uint32_t old) {
+        all = there;
+        olds = old;
         want = min(all, (uint32_t)a.budget);
         choose = want - min(all - olds, want);                  // (recent <= budget: the newest are at most `want`)
     }
@@ -168,7 +195,7 @@ __device__ __forceinline__ void find_bin(const uint32_t (&mine)[kBinsEach], uint
 // Tables of up to 1024 EACH keys: a block does it all for a sequence and head, keys in registers.  32 sequences of up to 6000 keys of 8 heads: bound by the latency of its steps.
 template <int EACH>
 __global__ void __launch_bounds__(kChooseThreads) k_evict_choose(EvictArgs a, bool wide) {
-    __shared__ uint32_t hist[kBins], part[kChooseWaves], found[2];
+    __shared__ uint32_t hist[kBins], part[2 * kChooseWaves], found[2];
     const Seat q(a, blockIdx.x);
     const int64_t j0 = (int64_t)threadIdx.x * EACH;
     const Mine<EACH> mine(a, q, j0, wide);
@@ -197,18 +224,20 @@ __global__ void __launch_bounds__(kChooseThreads) k_evict_choose(EvictArgs a, bo
 }
 
 // Longer tables: a block has a chunk of kChunk keys, the histograms of a sequence's chunks are joined by each of its blocks in the next of four launches (PASS 0 .. 3; the last one
-// writes).  Sums over the chunks before a block's own tell where its kept keys go.
+// writes).  Sums over the chunks before a block's own tell where its kept keys go.  Bound by the latency of its steps, barriers among them: how many keys a chunk has is counted by the first
+// launch, later ones add that up over the chunks in each wavefront for itself.
 constexpr int kChunkEach = 8, kChunk = kChooseThreads * kChunkEach;
 struct ChunkArgs {
     EvictArgs a;
     int32_t chunks;
     uint32_t* hist[2];         // [seats][chunks][kBins], of this and of the last pass in turn
     uint32_t* place;           // [seats][chunks]: old keys above the threshold so far in the chunks before
+    uint2* there;              // [seats][chunks]: keys of a chunk that are there, and the old ones among them
     uint32_t* state;           // [2][seats][2]: threshold so far, rank among the keys that begin with it, of this and of the last pass in turn
 };
 template <int PASS>
 __global__ void __launch_bounds__(kChooseThreads) k_evict_chunks(ChunkArgs c, bool wide) {
-    __shared__ uint32_t hist[kBins], part[kChooseWaves], found[2];
+    __shared__ uint32_t hist[kBins], part[2 * kChooseWaves], found[2];
     const EvictArgs& a = c.a;
     const int seats = gridDim.x / c.chunks, seat = blockIdx.x / c.chunks, chunk = blockIdx.x - seat * c.chunks;
     const Seat q(a, seat);
@@ -216,8 +245,27 @@ __global__ void __launch_bounds__(kChooseThreads) k_evict_chunks(ChunkArgs c, bo
     const int chunks = min(c.chunks, (int)((q.n + (int64_t)kChunk - 1) / kChunk));          // that hold keys
     if (chunk >= max(chunks, 1)) return;
     const Mine<kChunkEach> mine(a, q, j0, wide);
-    const Wanted w(a, q, part);
-    const bool all = w.choose == w.olds;                        // (nothing is to be searched for)
+    uint2 there = {0, 0}, there_before = {0, 0};                // of all chunks, and of those before
+    if constexpr (PASS == 0) {
+        const uint2 own = block_sums(make_uint2(__popc(mine.old | mine.fresh), __popc(mine.old)), part);
+        if (threadIdx.x == 0) c.there[(int64_t)seat * c.chunks + chunk] = own;
+    } else {
+        for (int k = threadIdx.x & 63; k < chunks; k += 64) {
+            const uint2 t = c.there[(int64_t)seat * c.chunks + k];
+            there.x += t.x;
+            there.y += t.y;
+            if (k < chunk) { there_before.x += t.x; there_before.y += t.y; }
+        }
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            there.x += __shfl_xor(there.x, o, 64);
+            there.y += __shfl_xor(there.y, o, 64);
+            there_before.x += __shfl_xor(there_before.x, o, 64);
+            there_before.y += __shfl_xor(there_before.y, o, 64);
+        }
+    }
+    const Wanted w(a, there.x, there.y);
+    const bool all = PASS > 0 && w.choose == w.olds;            // (nothing is to be searched for; the first launch does not know)
     uint32_t threshold = 0, rank = w.choose, above_before = 0, equal_before = 0;
     if (PASS > 0 && !all && w.choose > 0) {
         const uint32_t* last = c.hist[(PASS + 1) & 1] + (int64_t)seat * c.chunks * kBins;
@@ -254,8 +302,9 @@ __global__ void __launch_bounds__(kChooseThreads) k_evict_chunks(ChunkArgs c, bo
             if (b > bin) more += before[i];
             if (b == bin) same += before[i];
         }
-        block_prefix(more, part, above_before);
-        block_prefix(same, part, equal_before);
+        const uint2 before_own = block_sums(make_uint2(more, same), part);
+        above_before = before_own.x;
+        equal_before = before_own.y;
         uint32_t* place = c.place + (int64_t)seat * c.chunks + chunk;
         if (PASS > 1) above_before += *place;
         __syncthreads();
@@ -269,7 +318,7 @@ __global__ void __launch_bounds__(kChooseThreads) k_evict_chunks(ChunkArgs c, bo
         }
     }
     if constexpr (PASS < 3) {
-        if (all || w.choose == 0) return;
+        if (PASS > 0 && (all || w.choose == 0)) return;
 #pragma unroll
         for (int i = 0; i < kBinsEach; ++i) hist[threadIdx.x + i * kChooseThreads] = 0;
         __syncthreads();
@@ -280,18 +329,7 @@ __global__ void __launch_bounds__(kChooseThreads) k_evict_chunks(ChunkArgs c, bo
         for (int i = 0; i < kBinsEach; ++i) to[threadIdx.x + i * kChooseThreads] = hist[threadIdx.x + i * kChooseThreads];
     } else {
         // keys there before the chunk: the newest count as kept, the old ones where all of them are
-        uint32_t mine_new = 0, mine_old = 0, news, olds;
-        const int first = chunk * kChunk, P = 1 << a.st.shift;
-        for (int p = threadIdx.x; p << a.st.shift < min(first, q.n); p += kChooseThreads) {
-            const int j = p << a.st.shift;
-            if (q.there(a, j)) {
-                const int o = min(P, max(q.old - j, 0));
-                mine_old += o;
-                mine_new += min(P, q.n - j) - o;
-            }
-        }
-        block_prefix(mine_new, part, news);
-        block_prefix(mine_old, part, olds);
+        const uint32_t olds = there_before.y, news = there_before.x - olds;
         if (w.choose == 0) { threshold = ~0u; rank = 0; }       // (as in k_evict_choose)
         else if (all) { rank = ~0u; above_before = olds; }      // all old keys, those that equal the threshold (0) among them
         mine.write(q, j0, threshold, rank, above_before + news, equal_before, part);
