@@ -192,7 +192,7 @@ __device__ __forceinline__ void find_bin(const uint32_t (&mine)[kBinsEach], uint
     __syncthreads();
 }
 
-// Tables of up to 1024 EACH keys: a block does it all for a sequence and head, keys in registers.  32 sequences of up to 6000 keys of 8 heads: bound by the latency of its steps.
+// Tables of up to 1024 EACH keys: a block does it all for a sequence and head, keys in registers.  32 sequences of up to 6000 keys of 8 heads: 12 us, bound by the latency of its steps.
 template <int EACH>
 __global__ void __launch_bounds__(kChooseThreads) k_evict_choose(EvictArgs a, bool wide) {
     __shared__ uint32_t hist[kBins], part[2 * kChooseWaves], found[2];
@@ -225,7 +225,7 @@ __global__ void __launch_bounds__(kChooseThreads) k_evict_choose(EvictArgs a, bo
 
 // Longer tables: a block has a chunk of kChunk keys, the histograms of a sequence's chunks are joined by each of its blocks in the next of four launches (PASS 0 .. 3; the last one
 // writes).  Sums over the chunks before a block's own tell where its kept keys go.  Bound by the latency of its steps, barriers among them: how many keys a chunk has is counted by the first
-// launch, later ones add that up over the chunks in each wavefront for itself.
+// launch, later ones add that up over the chunks in each wavefront for itself (one sequence of 100000 keys of 8 heads: 6 + 9 + 9.5 + 11 us; each walking the tables itself, 6 + 10 + 10.5 + 12).
 constexpr int kChunkEach = 8, kChunk = kChooseThreads * kChunkEach;
 struct ChunkArgs {
     EvictArgs a;
@@ -340,7 +340,7 @@ __global__ void __launch_bounds__(kChooseThreads) k_evict_chunks(ChunkArgs c, bo
 
 // Moves the kept tokens: a block has 64 consecutive ones of a sequence and head, at the destination's keys 64 blockIdx.x on.  Their keys are rows of their own.  Their values lie byte by
 // byte in rows of components: the 16-byte groups that hold any of the 64 are read into LDS (in order, so that lanes read neighbouring groups) and the bytes picked there - each
-// byte read from memory by a lane of its own costs a cycle of the address unit, whatever the cache holds (32 sequences of up to 6000 keys cut to 2048, 4 bits, 8 heads of 128: 64 us).
+// byte read from memory by a lane of its own costs a cycle of the address unit, whatever the cache holds (32 sequences of up to 6000 keys cut to 2048, 4 bits, 8 heads of 128: 64 us so, 40 to 53 as built).
 // Bound by memory: where few keys are kept, most lines of the source's values are read all the same.
 constexpr int kMoveRoom = 1024;        // 16-byte groups in LDS
 template <int BITS>
