@@ -19,9 +19,10 @@ struct WeightArgs {
     float* sums;
     int64_t keys;              // of a table
     // many rows: rows of a sequence begin at a multiple of 32 (padded_row)
+    float step_c, back_c;      // scale log2 e = step_c back_c, the second a power of two
     int64_t padded;            // rows of a head
     f16x8* q16;                // [heads][padded / 32][D / 16][64]: operands of the matrix instructions, as the lanes hold them
-    float* back;               // [heads][padded]: what a product of such a row, times a key's step, is to be multiplied by: positive, scale log2 e included but for its sign
+    float* back;               // [heads][padded]: what a product of such a row, times a key's step and step_c, is to be multiplied by: a power of two
     float *row_m, *row_inv;    // [heads][padded]: m, 1 / l
 };
 
@@ -284,7 +285,7 @@ __global__ void __launch_bounds__(256) k_weights_add(WeightArgs wa) {
 }
 
 // Many rows: m and l.  A block has 128 rows of one head, a wavefront 32; keys pass by, 64 at a time, converted once for the block into LDS.  The maximum is taken over x = product * step,
-// which the row's factor (positive) is applied to together with it: y - m = fma(x, back, -m), so a score costs five instructions and its exponential.
+// which the row's factor (a power of two: m = x back is exact, and no term is above 1 however large logits are) is applied to together with it: y - m = fma(x, back, -m), so a score costs five instructions and its exponential.
 // 4 x 32 tokens after 16000 keys, 32 heads on 8 of 128, 4 bits: 41 us, the matrix instructions alone 7; 45 % of the cycles are vector instructions, half of those convert codes and find addresses.
 // (Four wavefronts a SIMD instead of three: 17 registers spill, 92 us for the call instead of 86.)
 template <typename T, int D, int BITS>
@@ -329,7 +330,7 @@ __global__ void __launch_bounds__(256, 3) k_weights_rows(WeightArgs wa) {
         top = fmaxf(top, __shfl_xor(top, 32, 64));
         float up;
         row_power(top, up, back);
-        back = fmaxf(back * fabsf(a.c), 0x1p-149f);             // (not 0: keys that are not there are -inf)
+        back = fminf(fmaxf(back * wa.back_c, 0x1p-149f), 0x1p127f);     // (not 0: keys that are not there are -inf)
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             float f[8];
@@ -340,8 +341,6 @@ __global__ void __launch_bounds__(256, 3) k_weights_rows(WeightArgs wa) {
         }
         if (any && split == 0 && half == 0) wa.back[slot + n] = back;
     }
-    const float sign = a.c < 0.0f ? -1.0f : 1.0f;
-
     const uint32_t page_bytes = (uint32_t)ROW << a.st.shift;
     int pg[PER], pg_step = 0;
     auto page_at = [&](const KeyTile& kt, int key) { return kt.pages[min(kt.k + key, kt.length - 1) >> a.st.shift]; };
@@ -390,7 +389,7 @@ __global__ void __launch_bounds__(256, 3) k_weights_rows(WeightArgs wa) {
             *(f16x8*)&lds_k[kb][krow * KS + 16 * part + 8] = hi;
         }
         if (wave == 0) {
-            lds_step[kb][0][lane] = rhave ? rks * sign : 0.0f;
+            lds_step[kb][0][lane] = rhave ? rks * wa.step_c : 0.0f;
             lds_step[kb][1][lane] = rhave ? 0.0f : -INFINITY;
         }
     };
@@ -532,7 +531,7 @@ __global__ void __launch_bounds__(256, 2) k_weights_keys(WeightArgs wa) {
         uint64_t r;
         uint32_t at;
         ok = row_at(lane, r, at);
-        lds_step[wave][lane] = ok ? a.st.ks[(r << a.st.shift) + at] * (a.c < 0.0f ? -1.0f : 1.0f) : 0.0f;      // (of a key that is not there: any)
+        lds_step[wave][lane] = ok ? a.st.ks[(r << a.st.shift) + at] * wa.step_c : 0.0f;      // (of a key that is not there: any)
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
             const int key = 32 * (n >> 2 & 1) + 16 * b + 4 * (n >> 3) + (n & 3);

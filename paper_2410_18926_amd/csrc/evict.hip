@@ -109,6 +109,9 @@ int attend_weights(const St* st, const lorann_questions* qs, const int32_t* tabl
     a.found = 1;
     a.unit = p.unit; a.units = a.splits = p.splits; a.per_split = 1;
     a.q_wide = aligned(qs->q, 16) && qs->q_token % 8 == 0 && qs->q_head % 8 == 0;
+    int power = 0;
+    w.step_c = std::frexp(a.c, &power);
+    w.back_c = std::ldexp(1.0f, power);
     w.before = before; w.sums = sums; w.keys = (int64_t)width * st->page_size; w.row_keys = p.row_keys; w.padded = p.padded;
     char* at = (char*)workspace;
     if (p.many) {

@@ -69,6 +69,57 @@ def test_weights_of_uneven_sequences(B, new, lengths, heads, group, dim, page, d
     check_weights(B, new, lengths, heads, group, dim, page, dtype)
 
 
+@pytest.mark.parametrize("new", [3, 50])
+@pytest.mark.parametrize("scale", [-0.2, 0.0, 0.3])
+def test_weights_of_queries_laid_out_otherwise(B, new, scale):
+    """Queries that are slices of a fused projection, at odd distances and addresses, one token for all (distance 0), heads before tokens; negative and zero scales."""
+    _, filled, held = B
+    g = gen(new)
+    lengths, heads, group, dim, page = [210, 77], 2, 3, 64, 32
+    st = filled(12, heads, page, dim, seed=5)
+    tables = make_tables(g, lengths, 12, page)
+    tokens, many = 2 * new, heads * group
+    fused = randn(g, tokens, 3 * many, dim).to(BF16)
+    odd = randn(g, tokens * (many * (dim + 1) + 3) + 1).to(F16)
+    for q in (fused[:, many:2 * many], odd[1:].view(tokens, -1)[:, :many * (dim + 1)].unflatten(1, (many, dim + 1))[:, :, 1:], fused[:1, :many].expand(tokens, -1, -1),
+              randn(g, many, tokens, dim).to(BF16).transpose(0, 1)):
+        want, tol = E.weights(held(st), q, tables, lengths, [0, new, tokens], scale)
+        R.assert_close(st.attend_weights(q, dev(tables), dev(lengths), scale=scale), want, tol, str(q.stride()))
+
+
+@pytest.mark.parametrize("new,dim", [(1, 64), (40, 128), (300, 32)])
+def test_weights_of_large_logits(B, new, dim):
+    """Logits of 2^20 to 2^60, keys that differ by little among them: weights stay between 0 and 1 and a row's add up to 1 (900 terms of up to 2^-22 each)."""
+    Store, _, _ = B
+    g, n, page, heads = gen(new), 900, 64, 2
+    st = Store.empty(15, heads, page, dim)
+    t = torch.arange(n, device="cuda")
+    for power in (20, 24, 28, 31, 34, 45, 60):
+        k = torch.zeros((n, heads, dim), device="cuda")
+        k[:, :, 5] = 2.0 ** (power - 10) * (1 + (t + torch.randint(0, 40, (n,), generator=g, device="cuda"))[:, None] * 2.0 ** -23)
+        k[::7, :, 3] = 2.0 ** (power - 30)
+        st.write(k, k, t)
+        q = randn(g, new, 4 * heads, dim)
+        q[:, :, 5] = 2.0 ** 10
+        for scale in (1.0, -0.7):
+            got = st.attend_weights(q.to(BF16), dev([list(range(15))]), dev([n]), scale=scale).double()
+            assert (got >= 0).all() and (got <= 4 * new * (1 + 2.0 ** -12)).all(), (power, scale)
+            assert (got.sum(2) / (4 * new) - 1).abs().max() < 2.0 ** -11, (power, scale)
+
+
+@pytest.mark.parametrize("new", [2, 40])
+@pytest.mark.parametrize("size", [-90, -40, 40, 90])
+def test_weights_of_small_and_large_queries(B, new, size):
+    """Queries of 2^size under a scale of 2^-size: logits of ordinary size."""
+    _, filled, held = B
+    g = gen(new)
+    st = filled(12, 2, 32, 64, seed=6)
+    tables = make_tables(g, [300], 12, 32)
+    q = (randn(g, new, 4, 64) * 2.0 ** size).to(BF16)
+    want, tol = E.weights(held(st), q, tables, [300], [0, new], 0.3 * 2.0 ** -size)
+    R.assert_close(st.attend_weights(q, dev(tables), dev([300]), scale=0.3 * 2.0 ** -size), want, tol)
+
+
 def test_weights_sum_to_the_rows(B):
     """Many blocks of keys: every row's weights add up to 1, within the error of each (2^-20 of it)."""
     _, filled, _ = B
