@@ -15,10 +15,27 @@ struct WeightPlan {
     int64_t y, parts, q16, rows, workspace;      // bytes: scores; m and l of the splits; operands; back, m, 1 / l of a row
 };
 
-// Rows per sequence and head (their mean over the call) up to which the scores are kept, and how much memory they may take: otherwise they are formed twice.
+// Rows per sequence and head (their mean over the call) up to which the scores are kept, and how much memory they may take: otherwise they are formed twice.  us kept / formed twice:
+//   rows                                                     4          16         32         48         64         128
+//   32 sequences, 4096 keys, 8 heads of 128, 8 bits     45 / 117   52 / 114   96 / 114  144 / 127  200 / 125  400 / 149
+//   the same, 4 bits                                    43 / 114   44 / 113   65 / 110  117 / 126  171 / 124  360 / 152
+//   16 sequences, 4000 keys, 16 heads of 64, 8 bits                           59 / 88   114 / 99   162 / 98
+//   one sequence, 16000 keys, 8 heads of 128, 8 bits    20 / 42    26 / 44    39 / 43               64 / 44
+//   two sequences, 9000 keys, 4 heads of 64, 4 bits                           32 / 28    43 / 29    54 / 29
 // Blocks wanted: of k_weights_scores many more than the GPU holds, since sequences differ in length and a split costs two numbers a row (64 tokens after up to 8192 keys, 8 heads, us with
 // 512 / 1024 / 2048 / 4096 / 8192: 102 / 101 / 104 / 89 / 96); of k_weights_rows 4 a CU (4 x 32 tokens after 16000 keys, 512 / 768 / 1024 / 1536 / 2048: 53 / 52 / 40 / 41 / 49).
 constexpr int64_t kScoreBlocks = 4096, kRowBlocks = 1024, kFewWeightRows = 32, kMostScores = (int64_t)1 << 30;
+
+// Keys of a block of k_weights_keys: 256, each wavefront with 64 of its own and all rows, or 64 that its wavefronts share with a quarter of the rows each (four times the blocks).  512 blocks are on
+// the GPU at a time, and what a wavefront does before its first rows takes as long as 11 steps of 32 rows.  us of a call, 64 shared / 256 apart, one sequence, 8 heads of 128, 8 bits:
+//   rows    1000 keys    4000       8000       16000      60000
+//   64      23 / 23      23 / 24    29 / 24
+//   400     26 / 32      37 / 38    52 / 48
+//   1200    36 / 55      60 / 69    95 / 107   161 / 152  497 / 477
+bool share_keys(int64_t blocks_apart, int64_t mean_rows) {
+    const double fill = 512, before = 11, steps = (double)mean_rows / 32;
+    return std::max(1.0, 4 * blocks_apart / fill) * (before + steps / 4) < std::max(1.0, blocks_apart / fill) * (before + steps);
+}
 
 template <typename St>
 WeightPlan weight_plan(const St* st, const lorann_questions* qs, int32_t width) {
@@ -66,7 +83,7 @@ void launch_weights(const WeightPlan& p, const WeightArgs& w, int32_t type, hipS
     if (type == LORANN_F16) hipLaunchKernelGGL((k_weights_rows<_Float16, D, BITS>), grid, dim3(256), 0, stream, w);
     else hipLaunchKernelGGL((k_weights_rows<__bf16, D, BITS>), grid, dim3(256), 0, stream, w);
     if (a.splits > 1) hipLaunchKernelGGL(k_weights_join, dim3((unsigned)ceil_div(a.st.heads * w.padded, 32)), dim3(256), 0, stream, w);
-    const bool share = ceil_div(w.keys, 256) * a.st.heads * a.sequences < kBlocksWanted;
+    const bool share = share_keys(ceil_div(w.keys, 256) * a.st.heads * a.sequences, a.tokens * a.group / a.sequences);
     const dim3 chunks((unsigned)ceil_div(w.keys, share ? 64 : 256), (unsigned)a.st.heads, (unsigned)a.sequences);
     if (share) hipLaunchKernelGGL((k_weights_keys<D, BITS, true>), chunks, dim3(256), 0, stream, w);
     else hipLaunchKernelGGL((k_weights_keys<D, BITS, false>), chunks, dim3(256), 0, stream, w);
