@@ -487,14 +487,32 @@ __global__ void __launch_bounds__(256) k_weights_join(WeightArgs wa) {
     wa.row_inv[i] = l == 0.0f ? 0.0f : 1.0f / l;
 }
 
+// v of the lane W away (W < 16), in the registers' own crossings: through LDS (a permute), the 31 exchanges below make up a tenth of a wavefront's instructions and wait for each round.
+template <int W>
+__device__ __forceinline__ float lane_across(float v) {
+    const int x = __float_as_int(v);
+    if constexpr (W == 8) return __int_as_float(__builtin_amdgcn_update_dpp(0, x, 0x128, 0xf, 0xf, true));            // row_ror:8
+    else if constexpr (W == 4)                                                                                     // row_half_mirror, then quad_perm 3 2 1 0
+        return __int_as_float(__builtin_amdgcn_update_dpp(0, __builtin_amdgcn_update_dpp(0, x, 0x141, 0xf, 0xf, true), 0x1b, 0xf, 0xf, true));
+    else if constexpr (W == 2) return __int_as_float(__builtin_amdgcn_update_dpp(0, x, 0x4e, 0xf, 0xf, true));        // quad_perm 2 3 0 1
+    else return __int_as_float(__builtin_amdgcn_update_dpp(0, x, 0xb1, 0xf, 0xf, true));                              // quad_perm 1 0 3 2
+}
 // 2 W values of a lane are W of its pair's (lanes W apart) added up, and so on: after all rounds lane n has value n of the 32 that each of 32 lanes had, added up.
 template <int W>
 __device__ __forceinline__ void add_over_lanes(float (&v)[32]) {
-    const bool upper = threadIdx.x & W;
+    if constexpr (W == 16) {
 #pragma unroll
-    for (int j = 0; j < W; ++j) {
-        const float give = upper ? v[j] : v[j + W], keep = upper ? v[j + W] : v[j];
-        v[j] = keep + __shfl_xor(give, W, 64);
+        for (int j = 0; j < W; ++j) {                           // rows of 16 lanes: the odd ones of the first change places with the even ones of the second
+            const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v[j]), __float_as_uint(v[j + W]), false, false);
+            v[j] = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+        }
+    } else {
+        const bool upper = threadIdx.x & W;
+#pragma unroll
+        for (int j = 0; j < W; ++j) {
+            const float give = upper ? v[j] : v[j + W], keep = upper ? v[j + W] : v[j];
+            v[j] = keep + lane_across<W>(give);
+        }
     }
     if constexpr (W > 1) add_over_lanes<W / 2>(v);
 }
