@@ -48,6 +48,31 @@ __device__ __forceinline__ f16x8 key_operand(const int8_t* row, int at, uint32_t
     }
 }
 
+// The largest finite magnitude of a lane's elements: of 16-bit magnitudes as they stand, two at a time; element by element only where one is an infinity or NaN.  (All of them as floats took 350
+// instructions of a wavefront of k_weights_rows, which has some 2500 in all where a block has 8 tiles of keys: 41.9 us, 41.3 so.)
+template <typename T, int N>
+__device__ __forceinline__ float largest_finite(const i32x4 (&raw)[N]) {
+    typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+    constexpr uint32_t infinity = std::is_same_v<T, _Float16> ? 0x7c00 : 0x7f80;
+    u16x2 m = {0, 0};
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, (uint32_t)raw[i][j] & 0x7fff7fffu));
+    uint32_t most = max((uint32_t)m[0], (uint32_t)m[1]);
+    if (__ballot(most >= infinity)) {
+        most = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const uint32_t u = (uint32_t)raw[i][j >> 1] >> (16 * (j & 1)) & 0x7fffu;
+                most = u < infinity ? max(most, u) : most;
+            }
+    }
+    return Bits16<T>::widen((uint16_t)most);
+}
+
 // Few rows.  A block has up to 16 rows of one head and a range of keys; its wavefronts take tiles of 64 keys in turn, codes straight from memory into registers, the next tile's in flight
 // (as k_attend_rows).  A lane keeps a maximum and a sum of its own until the end.  64 single tokens after up to 8192 keys, 32 heads on 8 of 128, 8 bits: 89 us for 352 MB of keys and 43 of
 // scores, 4.4 TB/s.
@@ -118,18 +143,10 @@ __global__ void __launch_bounds__(64 * kAttendWaves, 3) k_weights_scores(WeightA
     f16x8 qf[S32];
     float q_back;
     {
-        float top = 0.0f;
 #pragma unroll
-        for (int i = 0; i < S32; ++i) {
+        for (int i = 0; i < S32; ++i)
             if (!live) raw[i] = i32x4{0, 0, 0, 0};
-            float f[8];
-            widen8<T>(raw[i], f);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float m = fabsf(f[j]);
-                if (m <= 3.4028235e38f) top = fmaxf(top, m);
-            }
-        }
+        float top = largest_finite<T>(raw);
         top = fmaxf(top, __shfl_xor(top, 32, 64));
         top = fmaxf(top, __shfl_xor(top, 16, 64));
         float up;
@@ -272,6 +289,13 @@ __global__ void __launch_bounds__(256) k_weights_add(WeightArgs wa) {
                 if (see <= 0) continue;
                 const f32x4 v = *(const f32x4*)(y + r * wa.row_keys);
                 const float m = lds_m[r], inv = lds_inv[r];
+                if (inv != inv) {                               // (a row whose sum is no number: keys that are there, logits of -infinity among them, get none)
+                    if ((uint32_t)a.tables[(int64_t)s * a.width + (j0 >> a.st.shift)] < (uint64_t)a.st.pages)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            if (j < see) more[j] = inv;
+                    continue;
+                }
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
                     if (j < see && v[j] != -INFINITY) more[j] = fmaf(__builtin_amdgcn_exp2f(v[j] - m), inv, more[j]);
@@ -286,7 +310,7 @@ __global__ void __launch_bounds__(256) k_weights_add(WeightArgs wa) {
 
 // Many rows: m and l.  A block has 128 rows of one head, a wavefront 32; keys pass by, 64 at a time, converted once for the block into LDS.  The maximum is taken over x = product * step,
 // which the row's factor (a power of two: m = x back is exact, and no term is above 1 however large logits are) is applied to together with it: y - m = fma(x, back, -m), so a score costs five instructions and its exponential.
-// 4 x 32 tokens after 16000 keys, 32 heads on 8 of 128, 4 bits: 41 us, the matrix instructions alone 7; 45 % of the cycles are vector instructions, half of those convert codes and find addresses.
+// 4 x 32 tokens after 16000 keys, 32 heads on 8 of 128, 4 bits: 41 us, the matrix instructions alone 7; some 40 % of the cycles are vector instructions, a third of those convert codes and find addresses.
 // (Four wavefronts a SIMD instead of three: 17 registers spill, 92 us for the call instead of 86.)
 template <typename T, int D, int BITS>
 __global__ void __launch_bounds__(256, 3) k_weights_rows(WeightArgs wa) {
@@ -314,19 +338,12 @@ __global__ void __launch_bounds__(256, 3) k_weights_rows(WeightArgs wa) {
         const int tok = live ? row / a.group : 0, qh = head * a.group + (live ? row - tok * a.group : 0);
         const int64_t at = (int64_t)(tile.first + tok) * a.q_token + (int64_t)qh * a.q_head + D / 2 * half;
         i32x4 raw[N];
-        float top = 0.0f;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             raw[i] = load8_raw(a.q, at + 8 * i, a.q_wide);
             if (!live) raw[i] = i32x4{0, 0, 0, 0};
-            float f[8];
-            widen8<T>(raw[i], f);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float m = fabsf(f[j]);
-                if (m <= 3.4028235e38f) top = fmaxf(top, m);
-            }
         }
+        float top = largest_finite<T>(raw);
         top = fmaxf(top, __shfl_xor(top, 32, 64));
         float up;
         row_power(top, up, back);
@@ -518,7 +535,7 @@ __device__ __forceinline__ void add_over_lanes(float (&v)[32]) {
 }
 
 // Many rows: the sums.  A wavefront holds 64 keys as operands, rows pass by, 32 at a time.  SHARE: the block's four wavefronts have the same keys and take the rows in turn; else each
-// has keys of its own.  Blocks: (chunk of keys, head, sequence).  The case of k_weights_rows: 41 us, bound in the same way.
+// has keys of its own.  Blocks: (chunk of keys, head, sequence).  The case of k_weights_rows: 39.5 us, bound in the same way.
 template <int D, int BITS, bool SHARE>
 __global__ void __launch_bounds__(256, 2) k_weights_keys(WeightArgs wa) {
     const AttendArgs& a = wa.a;

@@ -120,6 +120,24 @@ def test_weights_of_small_and_large_queries(B, new, size):
     R.assert_close(st.attend_weights(q, dev(tables), dev([300]), scale=0.3 * 2.0 ** -size), want, tol)
 
 
+@pytest.mark.parametrize("new,dtype", [(3, BF16), (3, F16), (40, BF16), (300, F16)])
+@pytest.mark.parametrize("what", [float("nan"), float("inf"), -float("inf")])
+def test_weights_of_queries_that_are_no_numbers(B, new, dtype, what):
+    """A query that holds an infinity (its logits are infinities of both signs) or NaN makes the sums of the keys that it sees NaN, in its head; other heads, keys and sequences are as they would be."""
+    _, filled, _ = B
+    g = gen(new)
+    lengths, page = [400, 333], 64
+    st = filled(20, 2, page, 64, seed=8)
+    tables = make_tables(g, lengths, 20, page)
+    q = randn(g, 2 * new, 4, 64).to(dtype)
+    clean = st.attend_weights(q, dev(tables), dev(lengths))
+    q[new - 2, 1, 17] = what                               # the last query but one of the first sequence, head 0 of the store
+    got = st.attend_weights(q, dev(tables), dev(lengths))
+    assert torch.isnan(got[0, 0, :lengths[0] - 1]).all()
+    got[0, 0, :lengths[0] - 1] = clean[0, 0, :lengths[0] - 1]
+    assert torch.equal(got, clean)
+
+
 def test_weights_sum_to_the_rows(B):
     """Many blocks of keys: every row's weights add up to 1, within the error of each (2^-20 of it)."""
     _, filled, _ = B
