@@ -182,7 +182,9 @@ __global__ void __launch_bounds__(256) k_states4_write(Store st, TokenRows k, To
         const uint32_t group = quad_max_u32(f[i].largest()), most = row_max_u32(group);
         const bool bad = most >= 0x7f800000u, zero = bad || __uint_as_float(most) < kTinyRow;
         const float top = zero ? 1.0f : __uint_as_float(most);
-        const uint32_t r = factor_bits(zero ? 0.0f : __uint_as_float(group), top, __builtin_amdgcn_rcpf(top));
+        // (above 2^126 the reciprocal would not be a normal float: both are scaled down by the same power of two, which leaves their ratio; a group that this makes inexact is below every factor)
+        const float keep = top > kHugeRow ? kHugeDown : 1.0f, low = top * keep;
+        const uint32_t r = factor_bits(zero ? 0.0f : __uint_as_float(group) * keep, low, __builtin_amdgcn_rcpf(low));
         float x[8];
         f[i].values(x);
         code[i] = zero ? 0u : codes4_of<T>(x, __uint_as_float(r), top);
