@@ -586,8 +586,8 @@ __global__ void __launch_bounds__(256, 2) k_weights_keys(WeightArgs wa) {
     float sum[32];
 #pragma unroll
     for (int j = 0; j < 32; ++j) sum[j] = 0.0f;
-    // the first row that sees key k0
-    const int from_row = (int)max((int64_t)0, k0 - (length - count)) * a.group / 32 * 32;
+    // the first row that sees key k0, or behind the last one (the product passes 32 bits where a long table meets a large group)
+    const int from_row = (int)min(max((int64_t)0, k0 - (length - count)) * a.group / 32 * 32, (int64_t)rows);
     const int64_t base = (int64_t)head * wa.padded + padded_row((int64_t)first * a.group, s);
     const f16x8* q16 = wa.q16 + base / 32 * N * 64 + lane;
     // the next 32 rows are requested before these are used
