@@ -3,7 +3,7 @@
 Tensors live on the GPU and are handed over as pointers with their strides; nothing is copied or converted here, a tensor of another type or
 layout than asked for is refused.  Work is enqueued on torch's current stream of the current device and the calls return.
 
-There are no gradients: the store holds rounded codes.  An answer to queries (or scores) that require one can be used forwards, a backward pass that
+There are no gradients: the store holds rounded codes.  An answer to queries (or scores), or sums from queries or sums, that require one can be used forwards, a backward pass that
 reaches it raises; what is written into the store is cut off from its graph, as a cast to integers is.
 """
 from __future__ import annotations
@@ -315,4 +315,4 @@ class States:
                                 _array(left, torch.int32, shapes[1], "out[1]"), _array(kept_sums, torch.float32, shapes[2], "out[2]"), ws, size, self._stream())
         if rc:
             _raise(rc)
-        return kept, left, kept_sums
+        return kept, left, _no_gradient(kept_sums, sums) if sums.requires_grad else kept_sums
