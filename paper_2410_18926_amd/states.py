@@ -4,7 +4,8 @@ Tensors live on the GPU and are handed over as pointers with their strides; noth
 layout than asked for is refused.  Work is enqueued on torch's current stream of the current device and the calls return.
 
 There are no gradients: the store holds rounded codes.  An answer to queries (or scores), or sums from queries or sums, that require one can be used forwards, a backward pass that
-reaches it raises; what is written into the store is cut off from its graph, as a cast to integers is.
+reaches it raises, and so does one through a buffer of the caller's that a call has written to; a leaf that requires a gradient is refused as such a buffer before anything is written.
+What is written into the store is cut off from its graph, as a cast to integers is.
 """
 from __future__ import annotations
 
@@ -97,6 +98,14 @@ class _NoGradient(torch.autograd.Function):
         raise NotImplementedError("attention over the state store has no gradient (the store holds rounded codes): detach its inputs, or call it under torch.no_grad()")
 
 
+def _check_given(*outs):
+    """Refuses, before anything is enqueued, a caller's buffer that autograd lets nothing write to."""
+    if torch.is_grad_enabled():
+        for out in outs:
+            if out.requires_grad and (out.is_leaf or (out._base is not None and out._base.is_leaf)):
+                raise ValueError("a leaf that requires a gradient (or a view of one) cannot be written to: detach it, or call under torch.no_grad()")
+
+
 def _no_gradient(out, *inputs):
     if not torch.is_grad_enabled():
         return out
@@ -178,6 +187,7 @@ class States:
             v = torch.empty_like(k)
         else:
             k, v = out
+            _check_given(k, v)
         kt, kh = self._rows(k, n, "out[0]")
         vt, vh = self._rows(v, n, "out[1]")
         if k.dtype != v.dtype or k.dtype not in _TYPE:
@@ -185,7 +195,7 @@ class States:
         rc = self._run("read")(self._st, _array(slots, torch.int64, (n,), "slots"), n, k.data_ptr(), v.data_ptr(), _TYPE[k.dtype], kt, kh, vt, vh, self._stream())
         if rc:
             _raise(rc)
-        return k, v
+        return tuple(_no_gradient(x) if x.requires_grad else x for x in (k, v))
 
     def _questions(self, q, q_start, sequences, scale, out):
         tokens, heads, dim = q.shape
@@ -195,6 +205,8 @@ class States:
             out = torch.empty_like(q, memory_format=torch.contiguous_format)
         elif out.shape != q.shape or out.dtype is not q.dtype:
             raise ValueError(f"out must be {tuple(q.shape)} {q.dtype}, got {tuple(out.shape)} {out.dtype}")
+        elif out.requires_grad:
+            _check_given(out)
         qt, qh = _strides(q, "q")
         ot, oh = _strides(out, "out")
         return CQuestions(q.data_ptr(), out.data_ptr(), _TYPE.get(q.dtype, -1), heads, tokens, sequences, qt, qh, ot, oh,
@@ -237,7 +249,7 @@ class States:
                                        ws, size, self._stream())
         if rc:
             _raise(rc)
-        return _no_gradient(out, q) if q.requires_grad else out
+        return _no_gradient(out, q) if q.requires_grad or out.requires_grad else out
 
     def attend_passages(self, q, ids, tables, lengths, q_start=None, scores=None, score_weight=1.0, scale=None, out=None, workspace=None):
         """The queries of each sequence attend to all tokens of the passages found for it.
@@ -255,7 +267,7 @@ class States:
                                           ws, size, self._stream())
         if rc:
             _raise(rc)
-        return _no_gradient(out, q, scores) if q.requires_grad or (scores is not None and scores.requires_grad) else out
+        return _no_gradient(out, q, scores) if q.requires_grad or out.requires_grad or (scores is not None and scores.requires_grad) else out
 
     def _weight_questions(self, q, q_start, sequences, scale):
         tokens, heads, dim = q.shape
@@ -282,12 +294,14 @@ class States:
         shape = (n, self.heads, width * self.page_size)
         if out is None:
             out = torch.empty(shape, dtype=torch.float32, device=self.k_codes.device)
+        else:
+            _check_given(out)
         ws, size, keep = self._room(workspace, lambda: self._run("weights_workspace")(self._st, qs, width))
         rc = self._run("weights")(self._st, qs, _array(tables, torch.int32, (n, width), "tables"), width, _array(lengths, torch.int32, (n,), "lengths"),
                                   None if before is None else _array(before, torch.float32, shape, "before"), _array(out, torch.float32, shape, "out"), ws, size, self._stream())
         if rc:
             _raise(rc)
-        return _no_gradient(out, q, before) if q.requires_grad or (before is not None and before.requires_grad) else out
+        return _no_gradient(out, q, before) if q.requires_grad or out.requires_grad or (before is not None and before.requires_grad) else out
 
     def evict_workspace_bytes(self, sequences: int, width: int) -> int:
         """Bytes of `workspace` that evict with tables of these sizes needs."""
@@ -307,6 +321,8 @@ class States:
         shapes = (n, self.heads, budget), (n,), (n, self.heads, to_width * self.page_size)
         if out is None:
             out = tuple(torch.empty(s, dtype=t, device=self.k_codes.device) for s, t in zip(shapes, (torch.int32, torch.int32, torch.float32)))
+        else:
+            _check_given(out[2])
         kept, left, kept_sums = out
         ws, size, keep = self._room(workspace, lambda: lib().lorann_evict_workspace(self.heads, width * self.page_size, n))
         rc = self._run("evict")(self._st, _array(tables, torch.int32, (n, width), "tables"), width, _array(lengths, torch.int32, (n,), "lengths"), n,
@@ -315,4 +331,4 @@ class States:
                                 _array(left, torch.int32, shapes[1], "out[1]"), _array(kept_sums, torch.float32, shapes[2], "out[2]"), ws, size, self._stream())
         if rc:
             _raise(rc)
-        return kept, left, _no_gradient(kept_sums, sums) if sums.requires_grad else kept_sums
+        return kept, left, _no_gradient(kept_sums, sums) if sums.requires_grad or kept_sums.requires_grad else kept_sums

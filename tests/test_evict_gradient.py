@@ -1,4 +1,4 @@
-"""Answers, sums of weights and kept sums have no gradient: a backward pass that reaches one raises."""
+"""Sums of weights, kept sums and buffers of the caller's have no gradient: a backward pass that reaches one raises, and a leaf that requires a gradient is refused before it is written to."""
 import pytest
 import torch
 
@@ -55,3 +55,44 @@ def test_a_backward_pass_raises(store, name):
     with torch.no_grad():
         assert not call(x, None).requires_grad
     assert not call(given, None).requires_grad
+
+
+@pytest.mark.parametrize("name", NAMES)
+def test_a_leaf_is_refused_before_it_is_written(store, name):
+    given, call, like = calls(store)[name]
+    for grad in (False, True):
+        x = None if given is None else given.clone().requires_grad_(grad)
+        wide = torch.full((2, *like.shape), 7.0, dtype=like.dtype, device=store.on, requires_grad=True)
+        leaf = torch.full_like(like, 7.0).requires_grad_()
+        for out in (leaf, wide[1]):
+            before = len(store.called)
+            with pytest.raises(ValueError, match="leaf"):
+                call(x, out)
+            assert (out == 7).all() and len(store.called) == before
+        with torch.no_grad():
+            call(x, leaf)
+
+
+def test_sums_that_are_added_to_in_place(store):
+    """before and out the same leaf: refused; the same result of another operation: written, and a backward pass raises."""
+    t, n = tables(store)
+    q = torch.ones((1, 4, 64), dtype=torch.bfloat16, device=store.on)
+    leaf = torch.full((1, 2, 32), 7.0, device=store.on, requires_grad=True)
+    with pytest.raises(ValueError, match="leaf"):
+        store.attend_weights(q, t, n, before=leaf, out=leaf)
+    assert (leaf == 7).all()
+    sums = leaf * 1
+    assert store.attend_weights(q, t, n, before=sums, out=sums) is sums
+    with pytest.raises(NotImplementedError, match="no gradient"):
+        sums.sum().backward()
+
+
+@pytest.mark.parametrize("name", NAMES)
+def test_a_buffer_with_a_graph_of_its_own(store, name):
+    """What stood in the buffer is gone: the gradient of what was there before must not be taken for the answer's."""
+    given, call, like = calls(store)[name]
+    leaf = torch.full_like(like, 2.0).requires_grad_()
+    out = leaf * 1
+    y = call(given, out)
+    with pytest.raises(NotImplementedError, match="no gradient"):
+        y.float().sum().backward()
