@@ -121,8 +121,9 @@ class States:
     k_scales  [pages, heads, page_size] float32         v_scales  the same
     The tensors stay the caller's; slot = page * page_size + place in the page."""
 
-    _call = dict(write="lorann_states_write", read="lorann_states_read", chunk="lorann_attend_chunk", passages="lorann_attend_passages", workspace="lorann_attend_workspace",
-                 weights="lorann_attend_weights", weights_workspace="lorann_attend_weights_workspace", evict="lorann_states_evict")
+    # the library's names of the calls (looked up as attributes: a dictionary of them and a method to ask it took 0.7 us of a call's 8 to 11)
+    _write, _read, _chunk, _passages, _attend_room = "lorann_states_write", "lorann_states_read", "lorann_attend_chunk", "lorann_attend_passages", "lorann_attend_workspace"
+    _weights, _weights_room, _evict = "lorann_attend_weights", "lorann_attend_weights_workspace", "lorann_states_evict"
 
     def __init__(self, k_codes, v_codes, k_scales, v_scales):
         self.k_codes, self.v_codes, self.k_scales, self.v_scales = k_codes, v_codes, k_scales, v_scales
@@ -138,9 +139,6 @@ class States:
                                           (k_scales, torch.float32, steps, "k_scales"), (v_scales, torch.float32, steps, "v_scales")):
                 _array(t, dtype, shape, what)          # (says which)
         self._st = CStates(k_codes.data_ptr(), v_codes.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(), n, h, p, d)
-
-    def _run(self, what):
-        return getattr(lib(), self._call[what])
 
     @property
     def device(self):
@@ -174,7 +172,7 @@ class States:
         vt, vh = self._rows(v, n, "v")
         if k.dtype != v.dtype or k.dtype not in _TYPE:
             raise ValueError(f"k and v must both be float32, float16 or bfloat16, got {k.dtype} and {v.dtype}")
-        rc = self._run("write")(self._st, k.data_ptr(), v.data_ptr(), _TYPE[k.dtype], n, kt, kh, vt, vh, _array(slots, torch.int64, (n,), "slots"), self._stream())
+        rc = getattr(lib(), self._write)(self._st, k.data_ptr(), v.data_ptr(), _TYPE[k.dtype], n, kt, kh, vt, vh, _array(slots, torch.int64, (n,), "slots"), self._stream())
         if rc:
             _raise(rc)
 
@@ -192,10 +190,10 @@ class States:
         vt, vh = self._rows(v, n, "out[1]")
         if k.dtype != v.dtype or k.dtype not in _TYPE:
             raise ValueError(f"keys and values are read as float32, float16 or bfloat16, got {k.dtype} and {v.dtype}")
-        rc = self._run("read")(self._st, _array(slots, torch.int64, (n,), "slots"), n, k.data_ptr(), v.data_ptr(), _TYPE[k.dtype], kt, kh, vt, vh, self._stream())
+        rc = getattr(lib(), self._read)(self._st, _array(slots, torch.int64, (n,), "slots"), n, k.data_ptr(), v.data_ptr(), _TYPE[k.dtype], kt, kh, vt, vh, self._stream())
         if rc:
             _raise(rc)
-        return tuple(_no_gradient(x) if x.requires_grad else x for x in (k, v))
+        return _no_gradient(k) if k.requires_grad else k, _no_gradient(v) if v.requires_grad else v
 
     def _questions(self, q, q_start, sequences, scale, out):
         tokens, heads, dim = q.shape
@@ -212,26 +210,24 @@ class States:
         return CQuestions(q.data_ptr(), out.data_ptr(), _TYPE.get(q.dtype, -1), heads, tokens, sequences, qt, qh, ot, oh,
                           None if q_start is None else _array(q_start, torch.int32, (sequences + 1,), "q_start"), dim ** -0.5 if scale is None else scale), out
 
-    def _workspace(self, qs, found, width, workspace):
-        return self._room(workspace, lambda: self._run("workspace")(self._st, qs, found, width))
+    def _given_room(self, workspace):
+        if not workspace.is_contiguous():          # (its size would not be the memory it has)
+            raise ValueError("workspace must be contiguous")
+        return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
 
-    def _room(self, workspace, needed):
-        if workspace is not None:
-            if not workspace.is_contiguous():          # (its size would not be the memory it has)
-                raise ValueError("workspace must be contiguous")
-            return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
-        need = needed()
-        if need < 0:
-            _raise(need)
+    def _room(self, need):
+        """Memory of a call's own: address, bytes, and what keeps it."""
         if not need:
             return None, 0, None
+        if need < 0:
+            _raise(need)
         workspace = torch.empty(need, dtype=torch.uint8, device=self.k_codes.device)
         return workspace.data_ptr(), need, workspace
 
     def workspace_bytes(self, q, sequences: int, width: int, found: int = 0, ragged: bool = False) -> int:
         """Bytes of `workspace` that a call with these queries and sizes needs (found = 0: attend_chunk; ragged: with q_start)."""
         qs = CQuestions(None, None, _TYPE.get(q.dtype, -1), q.shape[1], q.shape[0], sequences, 0, 0, 0, 0, 1 if ragged else None, 1.0)
-        need = self._run("workspace")(self._st, qs, found, width)
+        need = getattr(lib(), self._attend_room)(self._st, qs, found, width)
         if need < 0:
             _raise(need)
         return need
@@ -244,8 +240,9 @@ class States:
         workspace: a tensor to work in (workspace_bytes), for callers that allocate nothing.  Returns out [tokens, heads, dim]."""
         n, width = tables.shape
         qs, out = self._questions(q, q_start, n, scale, out)
-        ws, size, keep = self._workspace(qs, 0, width, workspace)
-        rc = self._run("chunk")(self._st, qs, _array(tables, torch.int32, (n, width), "tables"), width, _array(lengths, torch.int32, (n,), "lengths"),
+        L = lib()
+        ws, size, keep = self._room(getattr(L, self._attend_room)(self._st, qs, 0, width)) if workspace is None else self._given_room(workspace)
+        rc = getattr(L, self._chunk)(self._st, qs, _array(tables, torch.int32, (n, width), "tables"), width, _array(lengths, torch.int32, (n,), "lengths"),
                                        ws, size, self._stream())
         if rc:
             _raise(rc)
@@ -260,8 +257,9 @@ class States:
         n, found = ids.shape
         passages, width = tables.shape
         qs, out = self._questions(q, q_start, n, scale, out)
-        ws, size, keep = self._workspace(qs, found, width, workspace)
-        rc = self._run("passages")(self._st, qs, _array(ids, torch.int64, (n, found), "ids"), found,
+        L = lib()
+        ws, size, keep = self._room(getattr(L, self._attend_room)(self._st, qs, found, width)) if workspace is None else self._given_room(workspace)
+        rc = getattr(L, self._passages)(self._st, qs, _array(ids, torch.int64, (n, found), "ids"), found,
                                           None if scores is None else _array(scores, torch.float32, (n, found), "scores"), score_weight,
                                           _array(tables, torch.int32, (passages, width), "tables"), width, _array(lengths, torch.int32, (passages,), "lengths"), passages,
                                           ws, size, self._stream())
@@ -280,7 +278,7 @@ class States:
     def weights_workspace_bytes(self, q, sequences: int, width: int, ragged: bool = False) -> int:
         """Bytes of `workspace` that attend_weights with these queries and sizes needs (ragged: with q_start)."""
         qs = CQuestions(None, None, _TYPE.get(q.dtype, -1), q.shape[1], q.shape[0], sequences, 0, 0, 0, 0, 1 if ragged else None, 1.0)
-        need = self._run("weights_workspace")(self._st, qs, width)
+        need = getattr(lib(), self._weights_room)(self._st, qs, width)
         if need < 0:
             _raise(need)
         return need
@@ -296,8 +294,9 @@ class States:
             out = torch.empty(shape, dtype=torch.float32, device=self.k_codes.device)
         else:
             _check_given(out)
-        ws, size, keep = self._room(workspace, lambda: self._run("weights_workspace")(self._st, qs, width))
-        rc = self._run("weights")(self._st, qs, _array(tables, torch.int32, (n, width), "tables"), width, _array(lengths, torch.int32, (n,), "lengths"),
+        L = lib()
+        ws, size, keep = self._room(getattr(L, self._weights_room)(self._st, qs, width)) if workspace is None else self._given_room(workspace)
+        rc = getattr(L, self._weights)(self._st, qs, _array(tables, torch.int32, (n, width), "tables"), width, _array(lengths, torch.int32, (n,), "lengths"),
                                   None if before is None else _array(before, torch.float32, shape, "before"), _array(out, torch.float32, shape, "out"), ws, size, self._stream())
         if rc:
             _raise(rc)
@@ -324,8 +323,8 @@ class States:
         else:
             _check_given(out[2])
         kept, left, kept_sums = out
-        ws, size, keep = self._room(workspace, lambda: lib().lorann_evict_workspace(self.heads, width * self.page_size, n))
-        rc = self._run("evict")(self._st, _array(tables, torch.int32, (n, width), "tables"), width, _array(lengths, torch.int32, (n,), "lengths"), n,
+        ws, size, keep = self._room(lib().lorann_evict_workspace(self.heads, width * self.page_size, n)) if workspace is None else self._given_room(workspace)
+        rc = getattr(lib(), self._evict)(self._st, _array(tables, torch.int32, (n, width), "tables"), width, _array(lengths, torch.int32, (n,), "lengths"), n,
                                 _array(sums, torch.float32, (n, self.heads, width * self.page_size), "sums"), budget, recent,
                                 _array(to_tables, torch.int32, (n, to_width), "to_tables"), to_width, _array(kept, torch.int32, shapes[0], "out[0]"),
                                 _array(left, torch.int32, shapes[1], "out[1]"), _array(kept_sums, torch.float32, shapes[2], "out[2]"), ws, size, self._stream())

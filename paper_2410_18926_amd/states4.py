@@ -16,8 +16,8 @@ class States4(States):
     k_scales   [pages, heads, page_size] float32            v_scales   the same
     The tensors stay the caller's; slot = page * page_size + place in the page.  Calls and arguments are those of States."""
 
-    _call = dict(write="lorann_states4_write", read="lorann_states4_read", chunk="lorann_attend4_chunk", passages="lorann_attend4_passages", workspace="lorann_attend4_workspace",
-                 weights="lorann_attend4_weights", weights_workspace="lorann_attend4_weights_workspace", evict="lorann_states4_evict")
+    _write, _read, _chunk, _passages, _attend_room = "lorann_states4_write", "lorann_states4_read", "lorann_attend4_chunk", "lorann_attend4_passages", "lorann_attend4_workspace"
+    _weights, _weights_room, _evict = "lorann_attend4_weights", "lorann_attend4_weights_workspace", "lorann_states4_evict"
 
     def __init__(self, k_codes, v_codes, k_factors, v_factors, k_scales, v_scales):
         self.k_codes, self.v_codes, self.k_factors, self.v_factors, self.k_scales, self.v_scales = k_codes, v_codes, k_factors, v_factors, k_scales, v_scales
