@@ -19,12 +19,16 @@ struct WeightArgs {
     float* sums;
     int64_t keys;              // of a table
     // many rows: rows of a sequence begin at a multiple of 32 (padded_row)
-    float step_c, back_c;      // scale log2 e = step_c back_c, the second a power of two
+    float step_c, back_c;      // scale log2 e = step_c back_c, the second a power of two that leaves `back` a normal float
     int64_t padded;            // rows of a head
     f16x8* q16;                // [heads][padded / 32][D / 16][64]: operands of the matrix instructions, as the lanes hold them
     float* back;               // [heads][padded]: what a product of such a row, times a key's step and step_c, is to be multiplied by: a power of two
     float *row_m, *row_inv;    // [heads][padded]: m, 1 / l
 };
+
+// Many rows: while keys' steps (times step_c) are up to this, a product (below 2^29) times one is no infinity.  Where a block meets a larger one, steps take the row's factor first, a power of
+// two: the same bits where both are finite.  (Always first, a score takes one instruction more; chosen tile by tile inside the loop, 300 tokens after 60000 keys took 489 us instead of 476.)
+constexpr float kMostStep = 0x1p98f;
 
 // Sequence s's rows begin here: ru(x) + ru(y) <= ru(x + y) + 32, so no two sequences' tiles of 32 overlap.
 __device__ __forceinline__ int64_t padded_row(int64_t first_row, int s) { return (first_row + 31) / 32 * 32 + 32 * (int64_t)s; }
@@ -310,6 +314,7 @@ __global__ void __launch_bounds__(256) k_weights_add(WeightArgs wa) {
 
 // Many rows: m and l.  A block has 128 rows of one head, a wavefront 32; keys pass by, 64 at a time, converted once for the block into LDS.  The maximum is taken over x = product * step,
 // which the row's factor (a power of two: m = x back is exact, and no term is above 1 however large logits are) is applied to together with it: y - m = fma(x, back, -m), so a score costs five instructions and its exponential.
+// A block that has met a key above kMostStep begins again, x = product * (step * back), y - m = fma(x, 1, -m).
 // 4 x 32 tokens after 16000 keys, 32 heads on 8 of 128, 4 bits: 41 us, the matrix instructions alone 7; some 40 % of the cycles are vector instructions, a third of those convert codes and find addresses.
 // (Four wavefronts a SIMD instead of three: 17 registers spill, 92 us for the call instead of 86.)
 template <typename T, int D, int BITS>
@@ -320,6 +325,7 @@ __global__ void __launch_bounds__(256, 3) k_weights_rows(WeightArgs wa) {
     typedef std::conditional_t<BITS == 4, i32x2, i32x4> Piece;
     __shared__ __align__(16) _Float16 lds_k[2][kTileKeys * KS];
     __shared__ __align__(16) float lds_step[2][2][kTileKeys];
+    __shared__ int lds_large;                                   // a key is above kMostStep
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, half = lane >> 5;
     const BlockWork work = block_work(a);
     const int head = work.head, split = work.split;
@@ -347,7 +353,7 @@ __global__ void __launch_bounds__(256, 3) k_weights_rows(WeightArgs wa) {
         top = fmaxf(top, __shfl_xor(top, 32, 64));
         float up;
         row_power(top, up, back);
-        back = fminf(fmaxf(back * wa.back_c, 0x1p-149f), 0x1p127f);     // (not 0: keys that are not there are -inf)
+        back *= wa.back_c;                                      // (a normal float: keys that are not there are -inf, which 0 would make NaN)
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             float f[8];
@@ -388,6 +394,7 @@ __global__ void __launch_bounds__(256, 3) k_weights_rows(WeightArgs wa) {
             rks = a.st.ks[(row_of(pg_step) << a.st.shift) + (uint32_t)((kt.k + lane) & (P - 1))];
         }
     };
+    float largest = 0.0f;                                       // (first wavefront) of the lane's steps
     auto stage = [&](int kb) {
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
@@ -406,77 +413,96 @@ __global__ void __launch_bounds__(256, 3) k_weights_rows(WeightArgs wa) {
             *(f16x8*)&lds_k[kb][krow * KS + 16 * part + 8] = hi;
         }
         if (wave == 0) {
-            lds_step[kb][0][lane] = rhave ? rks * wa.step_c : 0.0f;
+            const float step = rhave ? rks * wa.step_c : 0.0f;
+            lds_step[kb][0][lane] = step;
             lds_step[kb][1][lane] = rhave ? 0.0f : -INFINITY;
+            largest = fmaxf(largest, fabsf(step));
         }
     };
-    KeyTiles it;
-    it.start(a, tile.s, split);
-    it.next(a, tile.s, behind);
-    KeyTile cur = it.t;
-    find_pages(cur);
-    fetch(cur);
-    it.next(a, tile.s, behind);
-    find_pages(it.t);
-    if (cur.have) stage(0);
-    KeyTile nxt = it.t;
-    fetch(nxt);
-    it.next(a, tile.s, behind);
-    find_pages(it.t);
-    int kb = 0;
-    float X = -INFINITY, L = 0.0f;                              // largest x so far
-    while (cur.have) {
-        __syncthreads();                                        // tile `cur` is in buffer kb; the other has been read
-        f32x16 s[2];
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int j = 0; j < 16; ++j) s[b][j] = 0.0f;
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-#pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                const f16x8 k = *(const f16x8*)&lds_k[kb][(32 * b + n) * KS + D / 2 * half + 8 * i];
-                s[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, q[i], s[b], 0, 0, 0);
-            }
-        if (nxt.have) stage(kb ^ 1);
-        const KeyTile after = it.t;
-        fetch(after);
+    float M = -INFINITY, L = 0.0f;
+    auto pass = [&](auto first) {                               // first: steps take the row's factor first
+        KeyTiles it;
+        it.start(a, tile.s, split);
+        it.next(a, tile.s, behind);
+        KeyTile cur = it.t;
+        find_pages(cur);
+        fetch(cur);
         it.next(a, tile.s, behind);
         find_pages(it.t);
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const f32x4 sk = *(const f32x4*)&lds_step[kb][0][32 * half + 16 * b + 4 * g], lv = *(const f32x4*)&lds_step[kb][1][32 * half + 16 * b + 4 * g];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) s[b][4 * g + j] = fmaf(s[b][4 * g + j], sk[j], lv[j]);
-            }
-        if (cur.k + kTileKeys > cur.length - first_behind) {
-            const int see = cur.length - see_after - cur.k - 32 * half;
+        if (cur.have) stage(0);
+        KeyTile nxt = it.t;
+        fetch(nxt);
+        it.next(a, tile.s, behind);
+        find_pages(it.t);
+        int kb = 0;
+        float left = decltype(first)::value ? 1.0f : back;      // what x is still to be multiplied by
+        if constexpr (decltype(first)::value) asm("" : "+v"(left));       // (a product also where it is 1: x is rounded before m is taken off it)
+        while (cur.have) {
+            __syncthreads();                                    // tile `cur` is in buffer kb; the other has been read
+            f32x16 s[2];
 #pragma unroll
             for (int b = 0; b < 2; ++b)
 #pragma unroll
-                for (int j = 0; j < 16; ++j) s[b][j] = 16 * b + j < see ? s[b][j] : -INFINITY;
+                for (int j = 0; j < 16; ++j) s[b][j] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    const f16x8 k = *(const f16x8*)&lds_k[kb][(32 * b + n) * KS + D / 2 * half + 8 * i];
+                    s[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, q[i], s[b], 0, 0, 0);
+                }
+            if (nxt.have) stage(kb ^ 1);
+            const KeyTile after = it.t;
+            fetch(after);
+            it.next(a, tile.s, behind);
+            find_pages(it.t);
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    f32x4 sk = *(const f32x4*)&lds_step[kb][0][32 * half + 16 * b + 4 * g];
+                    const f32x4 lv = *(const f32x4*)&lds_step[kb][1][32 * half + 16 * b + 4 * g];
+                    if constexpr (decltype(first)::value) sk = sk * back;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) s[b][4 * g + j] = fmaf(s[b][4 * g + j], sk[j], lv[j]);
+                }
+            if (cur.k + kTileKeys > cur.length - first_behind) {
+                const int see = cur.length - see_after - cur.k - 32 * half;
+#pragma unroll
+                for (int b = 0; b < 2; ++b)
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) s[b][j] = 16 * b + j < see ? s[b][j] : -INFINITY;
+            }
+            float top = M;                                      // (of x, as M until the end)
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) top = fmaxf(top, s[b][j]);
+            const float m = top == -INFINITY ? 0.0f : top * left;
+            float l[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) l[j & 3] += __builtin_amdgcn_exp2f(fmaf(s[b][j], left, -m));
+            L = L * __builtin_amdgcn_exp2f(fmaf(M, left, -m)) + ((l[0] + l[1]) + (l[2] + l[3]));
+            M = top;
+            cur = nxt;
+            nxt = after;
+            kb ^= 1;
         }
-        float top = X;
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int j = 0; j < 16; ++j) top = fmaxf(top, s[b][j]);
-        const float m = top == -INFINITY ? 0.0f : top * back;
-        float l[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int j = 0; j < 16; ++j) l[j & 3] += __builtin_amdgcn_exp2f(fmaf(s[b][j], back, -m));
-        L = L * __builtin_amdgcn_exp2f(fmaf(X, back, -m)) + ((l[0] + l[1]) + (l[2] + l[3]));
-        X = top;
-        cur = nxt;
-        nxt = after;
-        kb ^= 1;
+        M *= left;                                              // (-inf: no key)
+    };
+    pass(std::false_type{});
+    if (wave == 0) {
+        const int met = __ballot(largest > kMostStep) != 0;
+        if (lane == 0) lds_large = met;
     }
-    float M = X * back;                                         // (-inf: no key)
+    __syncthreads();
+    if (__builtin_amdgcn_readfirstlane(lds_large)) {
+        M = -INFINITY;
+        L = 0.0f;
+        pass(std::true_type{});
+    }
     join_sums(M, L, __shfl_xor(M, 32, 64), __shfl_xor(L, 32, 64));
     if (!any || half) return;
     if (a.splits == 1) {
@@ -561,12 +587,14 @@ __global__ void __launch_bounds__(256, 2) k_weights_keys(WeightArgs wa) {
     // the lane's two keys as operands; of its 32 results the keys are 32 half + 16 b + j, as in k_weights_rows: row 32 b + n of the product is the key below
     f16x8 k[2][N];
     f32x4 step[2][4];
-    bool ok = false;                                            // the lane's own key is there
+    bool ok = false, large = false;                             // the lane's own key is there; a key of the wavefront is above kMostStep
     if (rows > 0) {
         uint64_t r;
         uint32_t at;
         ok = row_at(lane, r, at);
-        lds_step[wave][lane] = ok ? a.st.ks[(r << a.st.shift) + at] * wa.step_c : 0.0f;      // (of a key that is not there: any)
+        const float own = ok ? a.st.ks[(r << a.st.shift) + at] * wa.step_c : 0.0f;           // (of a key that is not there: any)
+        lds_step[wave][lane] = own;
+        large = __ballot(fabsf(own) > kMostStep) != 0;
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
             const int key = 32 * (n >> 2 & 1) + 16 * b + 4 * (n >> 3) + (n & 3);
@@ -603,6 +631,28 @@ __global__ void __launch_bounds__(256, 2) k_weights_keys(WeightArgs wa) {
     };
     constexpr int STRIDE = SHARE ? 128 : 32;
     int r0 = from_row + (SHARE ? wave * 32 : 0);
+    if (large) {                                                // (as in k_weights_rows; nothing in flight, so that the registers hold it)
+        float one = 1.0f;
+        asm("" : "+v"(one));                                    // (a product also where it is 1: x is rounded before m is taken off it)
+#pragma unroll 1
+        for (; r0 < rows; r0 += STRIDE) {
+            fetch(r0);
+            const int row = r0 + n, see = row < rows ? (int)(length - count + row / a.group + 1 - k0) - 32 * half : 0;
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                f32x16 y;
+#pragma unroll
+                for (int j = 0; j < 16; ++j) y[j] = 0.0f;
+#pragma unroll
+                for (int i = 0; i < N; ++i) y = __builtin_amdgcn_mfma_f32_32x32x16_f16(k[b][i], q[i], y, 0, 0, 0);
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    const float e = __builtin_amdgcn_exp2f(fmaf(y[j] * (step[b][j >> 2][j & 3] * back), one, -m)) * inv;
+                    sum[16 * b + j] += 16 * b + j < see ? e : 0.0f;
+                }
+            }
+        }
+    }
     fetch(r0);
     for (; r0 < rows; r0 += STRIDE) {
         f32x16 y[2];

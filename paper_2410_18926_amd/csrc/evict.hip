@@ -126,9 +126,12 @@ int attend_weights(const St* st, const lorann_questions* qs, const int32_t* tabl
     a.found = 1;
     a.unit = p.unit; a.units = a.splits = p.splits; a.per_split = 1;
     a.q_wide = aligned(qs->q, 16) && qs->q_token % 8 == 0 && qs->q_head % 8 == 0;
+    // as much of the scale's power of two goes with the rows as leaves their factors (2^-114 .. 2^113: row_power) normal floats, the rest with the keys' steps
     int power = 0;
-    w.step_c = std::frexp(a.c, &power);
-    w.back_c = std::ldexp(1.0f, power);
+    const float part = std::frexp(a.c, &power);
+    const int with_rows = std::min(std::max(power, -12), 14);
+    w.step_c = std::ldexp(part, power - with_rows);
+    w.back_c = std::ldexp(1.0f, with_rows);
     w.before = before; w.sums = sums; w.keys = (int64_t)width * st->page_size; w.row_keys = p.row_keys; w.padded = p.padded;
     char* at = (char*)workspace;
     if (p.many) {
