@@ -556,7 +556,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, 2) k_attend_rows(AttendArgs
             for (int b = 0; b < 4; ++b) {
                 const f32x4 sk = *(const f32x4*)&lds_step[wave][0][16 * quarter + 4 * b], lv = *(const f32x4*)&lds_step[wave][1][16 * quarter + 4 * b];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) s[t][b][j] = fmaf(s[t][b][j] * q_back[t], sk[j], lv[j]);
+                for (int j = 0; j < 4; ++j) s[t][b][j] = fmaf(s[t][b][j], sk[j] * q_back[t], lv[j]);          // (the product by itself, up to 2^29, times a row's factor of 2^113 would be an infinity)
             }
             if (!a.ids && cur.k + kTileKeys > cur.length - first_behind) {       // some row may not see all of it
                 const int see = cur.length - see_after[t] - cur.k - 16 * quarter;

@@ -201,7 +201,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, 3) k_weights_scores(WeightA
         for (int b = 0; b < 4; ++b) {
             const f32x4 sk = *(const f32x4*)&lds_step[wave][0][16 * b + 4 * quarter], lv = *(const f32x4*)&lds_step[wave][1][16 * b + 4 * quarter];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) s[b][j] = fmaf(s[b][j] * q_back, sk[j], lv[j]);
+            for (int j = 0; j < 4; ++j) s[b][j] = fmaf(s[b][j], sk[j] * q_back, lv[j]);          // (in this order: as in k_attend_rows)
         }
         if (cur.k + kTileKeys > cur.length - first_behind) {    // some row may not see all of it
             const int see = cur.length - see_after - cur.k - 4 * quarter;

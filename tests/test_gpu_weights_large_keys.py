@@ -12,7 +12,7 @@ pytestmark = pytest.mark.gpu
 
 
 @pytest.mark.parametrize("new", [2, 40, 300])
-@pytest.mark.parametrize("keys,queries", [(123, -99), (110, -100), (110, -60), (100, -100), (-97, 100), (60, -60)])
+@pytest.mark.parametrize("keys,queries", [(123, -99), (110, -100), (110, -60), (100, -100), (-97, 100), (-90, 120), (60, -60)])
 @pytest.mark.parametrize("mixed", [False, True])
 def test_weights_of_large_and_small_keys(B, new, keys, queries, mixed):  # noqa: F811
     """Keys of 2^keys, queries of 2^queries, a scale that makes their logits ordinary; mixed: beside keys of ordinary size and tiny ones, whose logits are next to nothing or far away."""
