@@ -155,7 +155,8 @@ __device__ __forceinline__ void row_power(float top, float& to_half, float& back
 //     1, one zero row with a logit of 10 among values of 0.01 put answers off by 20 times their rounding and more).  Keys of step s keep their 11 bits up to a logit of log2(s) + 107 octaves below its.
 //   - A NaN step of the values acts through add alone: rows that do not see the key multiply `inverse` by 0.
 // While all steps of the values are within 2^-45 .. 2^10 ("tame") or 0, the operand 2^kLift w of a key whose share of the sum is 2^-40 of the largest is still a normal
-// float, whatever the two keys' steps are, and operand * inverse is the sum's term.  Beyond that the terms are computed by an exponential of their own (sum_term).
+// float, whatever the two keys' steps are, and operand * inverse is the sum's term.  From the first tile on that has a step beyond that ("wild"), the terms are exponentials of their own,
+// relative to the largest of them so far (WildSum): between values of 2^-100 and 2^127 an operand's term may be 2^-125 or 2^107 times it, and terms next to 2^-126 would be lost.
 constexpr float kTameLow = 0x1p-45f, kTameHigh = 0x1p10f, kNoStep = 0x1p-84f;
 // The reference M of the weights is raised only when a score passes it by more than kSlack, so the answer's registers are rarely rescaled.  Weights stay below
 // 2^kSlack, and the operands 2^kLift w below 2^15, the last power of two but one that binary16 holds.  (Without the lift, weights below 2^-14 would lose bits and those
@@ -168,7 +169,7 @@ __device__ __forceinline__ float raised(float top, float m) {
     return passes(top, r) ? top : r;
 }
 constexpr float kUnlift = 1.0f / 512;          // 2^-kLift
-struct KeySteps { float product, add, inverse; bool wild; };
+struct KeySteps { float product, add, inverse, log_inverse; bool wild; };
 __device__ __forceinline__ KeySteps key_steps(float ks, float vs, float c, float bias, bool have) {
     const bool wild = vs != 0.0f && (vs < kTameLow || vs > kTameHigh);
     vs = vs == 0.0f ? kNoStep : vs < 0x1p-120f ? 0x1p-120f : vs;
@@ -177,13 +178,9 @@ __device__ __forceinline__ KeySteps key_steps(float ks, float vs, float c, float
     k.product = have ? ks * c : 0.0f;
     k.add = have ? lg + bias : -INFINITY;
     k.inverse = (have && vs == vs ? __builtin_amdgcn_rcpf(vs) : 1.0f) * kUnlift;       // (1 ulp)
+    k.log_inverse = -lg - kLift;                                // takes the place of `inverse` in a tile with a wild key: that may be no normal float
     k.wild = have && wild;
     return k;
-}
-
-// The sum's term of a key in units of the weights', where steps span more than a float's exponent.  m: the operands' reference (M - kLift in the formulas).
-__device__ __forceinline__ float sum_term(float y, float m, float inverse) {
-    return y == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(y - m + __log2f(inverse));
 }
 
 // x * 2^d where 2^d may be below the normal floats and the product is not.
@@ -191,6 +188,31 @@ __device__ __forceinline__ float times_exp2(float x, float d) {
     const float h = __builtin_amdgcn_exp2f(0.5f * d);
     return x * h * h;
 }
+
+// A row's sum over wild tiles: terms 2^t, t = y + log2 inverse, relative to their largest so far.  sum 2^(ref - M) is what L holds otherwise.
+struct WildSum {
+    float ref;
+    __device__ __forceinline__ void begin(float& l, float m) {         // (M may have been raised far above the terms so far)
+        ref = l == 0.0f ? -INFINITY : m + (float)__builtin_amdgcn_frexp_expf(l);
+        l = __builtin_amdgcn_frexp_mantf(l);
+    }
+    // Four keys' terms; logs: log_inverse stands in the place of `inverse`.
+    __device__ __forceinline__ void add(float& l, bool logs, float y0, float y1, float y2, float y3, const f32x4 inverse) {
+        float t[4] = {y0, y1, y2, y3}, top = ref;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            t[j] = t[j] == -INFINITY ? t[j] : t[j] + (logs ? inverse[j] : __log2f(inverse[j]));
+            top = fmaxf(top, t[j]);
+        }
+        const float use = top == -INFINITY ? 0.0f : top;
+        l *= __builtin_amdgcn_exp2f(ref - use);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) l += __builtin_amdgcn_exp2f(t[j] - use);
+        ref = top;
+        __builtin_amdgcn_sched_barrier(0);          // (four by four: together, a tile's terms would fill the registers)
+    }
+    __device__ __forceinline__ float end(float l, float m) const { return l == 0.0f ? 0.0f : times_exp2(l, ref - m); }
+};
 
 // A 32-bit offset that is widened where it is used (scalar base + vector offset in one instruction) instead of being kept as 64 bits.
 __device__ __forceinline__ uint32_t here(uint32_t x) {
@@ -492,20 +514,22 @@ __global__ void __launch_bounds__(64 * kAttendWaves, 2) k_attend_rows(AttendArgs
         L[t] = 0.0f;
     }
     bool wild = false;                                          // some step so far is not tame
+    WildSum terms[RT];
 
     while (cur.have) {
+        bool logs;                                              // some step of this tile is not tame
         {
             wave_lds_order();                                   // the previous tile's steps have been read
             const KeySteps ks = key_steps(rks, rvs, a.c, cur.bias, rhave);
             lds_step[wave][0][lane] = ks.product;
             lds_step[wave][1][lane] = ks.add;
-            lds_step[wave][2][lane] = ks.inverse;
+            logs = __ballot(ks.wild);
+            lds_step[wave][2][lane] = logs ? ks.log_inverse : ks.inverse;
             if constexpr (FOUR) {
                 lds_kf[wave][lane] = rkf;
 #pragma unroll
                 for (int g = 0; g < S32; ++g) lds_vf[wave][g][(lane & ~7) + token_place(lane & 7)] = factor_half(rvf, g);
             }
-            wild = wild || __ballot(ks.wild);
             wave_lds_order();
         }
         f32x4 s[RT][4];
@@ -549,6 +573,8 @@ __global__ void __launch_bounds__(64 * kAttendWaves, 2) k_attend_rows(AttendArgs
         find_page(it.t);
         __builtin_amdgcn_sched_barrier(0);
         f16x8 w[RT][2];
+        const bool was_wild = wild;
+        wild = wild || logs;
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
             float top = -INFINITY;
@@ -574,7 +600,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, 2) k_attend_rows(AttendArgs
                 top = fmaxf(top, __shfl_xor(top, 16, 64));
                 const float m_new = raised(top, M[t]), d = M[t] - (m_new == -INFINITY ? 0.0f : m_new);
                 const float shrink = __builtin_amdgcn_exp2f(d);
-                L[t] = times_exp2(L[t], d);
+                if (!was_wild) L[t] = times_exp2(L[t], d);
                 M[t] = m_new;
 #pragma unroll
                 for (int i = 0; i < DT; ++i) acc[t][i] = acc[t][i] * shrink;
@@ -594,10 +620,9 @@ __global__ void __launch_bounds__(64 * kAttendWaves, 2) k_attend_rows(AttendArgs
                 }
             };
             if (wild) {
+                if (!was_wild) terms[t].begin(L[t], M[t]);
 #pragma unroll
-                for (int b = 0; b < 4; ++b)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) l += sum_term(s[t][b][j], m_use, lds_step[wave][2][16 * quarter + 4 * b + j]);
+                for (int b = 0; b < 4; ++b) terms[t].add(L[t], logs, s[t][b][0], s[t][b][1], s[t][b][2], s[t][b][3], *(const f32x4*)&lds_step[wave][2][16 * quarter + 4 * b]);
             }
             if (FOUR && wild) weigh(std::false_type{});             // (8 bits: one copy, with a select)
             else weigh(std::true_type{});
@@ -637,7 +662,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, 2) k_attend_rows(AttendArgs
     // join the wavefronts, a tile of rows at a time
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-        float l_all = L[rt];
+        float l_all = wild ? terms[rt].end(L[rt], M[rt]) : L[rt];
         l_all += __shfl_xor(l_all, 32, 64);
         l_all += __shfl_xor(l_all, 16, 64);
         if (rt) __syncthreads();                                // (the last tile's have been read)

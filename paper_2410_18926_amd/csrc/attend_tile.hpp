@@ -238,12 +238,12 @@ __global__ void __launch_bounds__(64 * NW, 2) k_attend_tile(AttendArgs a) {
         const KeySteps ks = key_steps(rks, rvs, c, kt.bias, rhave);
         lds_step[vb][0][lane] = ks.product;
         lds_step[vb][1][lane] = ks.add;
-        lds_step[vb][2][lane] = ks.inverse;
+        const int w = __ballot(ks.wild) != 0;
+        lds_step[vb][2][lane] = w ? ks.log_inverse : ks.inverse;
         if constexpr (FOUR) {
 #pragma unroll
             for (int g = 0; g < C; ++g) lds_vf[vb][g][(lane & ~7) + token_place(lane & 7)] = factor_half(rvf, g);
         }
-        const int w = __ballot(ks.wild) != 0;
         if (lane == 0) lds_wild[vb] = w;
     };
 
@@ -300,12 +300,12 @@ __global__ void __launch_bounds__(64 * NW, 2) k_attend_tile(AttendArgs a) {
         return top;
     };
     // raises the reference where a row's largest score passes it by more than kSlack (M is kLift below it)
-    auto raise = [&](float top) {
+    auto raise = [&](float top, bool wild_now) {
         if (__ballot(passes(top, M))) {
             top = fmaxf(top, __shfl_xor(top, 32, 64));
             const float m_new = raised(top, M), d = M - (m_new == -INFINITY ? 0.0f : m_new);
             const float shrink = __builtin_amdgcn_exp2f(d);
-            L = times_exp2(L, d);
+            if (!wild_now) L = times_exp2(L, d);
             M = m_new;
 #pragma unroll
             for (int i = 0; i < C; ++i)
@@ -313,7 +313,7 @@ __global__ void __launch_bounds__(64 * NW, 2) k_attend_tile(AttendArgs a) {
                 for (int j = 0; j < 16; ++j) acc[i][j] *= shrink;
         }
     };
-    // the weights of a tile and their sum
+    // the weights of a tile and their sum (wild: WildSum's)
     auto weights = [&](int vb, const f32x16 (&y)[2], f16x8 (&w)[2][2], bool wild_now) {
         const float m_use = M == -INFINITY ? 0.0f : M;
         float l = 0.0f;                  // the tile's part of the sum: terms far below the sum so far would each be rounded away
@@ -325,7 +325,7 @@ __global__ void __launch_bounds__(64 * NW, 2) k_attend_tile(AttendArgs a) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const float e = __builtin_amdgcn_exp2f(y[b][4 * g + j] - m_use);
-                    l = wild_now ? l + sum_term(y[b][4 * g + j], m_use, iv[j]) : fmaf(e, iv[j], l);
+                    if (!wild_now) l = fmaf(e, iv[j], l);
                     w[b][g >> 1][place_of(4 * (g & 1) + j)] = (_Float16)e;
                 }
             }
@@ -394,7 +394,7 @@ __global__ void __launch_bounds__(64 * NW, 2) k_attend_tile(AttendArgs a) {
         scores(0, y);
         logits(0, d0, y, false);
         float top = top_of(y);
-        raise(top);
+        raise(top, false);
         int wild_now = lds_wild[0];
         __syncthreads();
         while (d0.have && !__builtin_amdgcn_readfirstlane(wild_now)) {
@@ -493,7 +493,7 @@ __global__ void __launch_bounds__(64 * NW, 2) k_attend_tile(AttendArgs a) {
                 top = top_of(s);
             }
             advance();
-            if (d0.have) raise(top);
+            if (d0.have) raise(top, false);
 #pragma unroll
             for (int b = 0; b < 2; ++b) y[b] = s[b];
             __syncthreads();
@@ -501,16 +501,24 @@ __global__ void __launch_bounds__(64 * NW, 2) k_attend_tile(AttendArgs a) {
     }
     // Queries of very different sizes in one block, or steps of the values that are not tame (key_steps): the same step by step, for the tiles that are left.
     bool wild = false;
+    WildSum terms;
     while (d0.have) {
         const int v1 = vb == 2 ? 0 : vb + 1, v2 = v1 == 2 ? 0 : v1 + 1;
-        wild = wild || __builtin_amdgcn_readfirstlane(lds_wild[vb]);
+        const bool logs = __builtin_amdgcn_readfirstlane(lds_wild[vb]);
+        if (logs && !wild) terms.begin(L, M);
+        wild = wild || logs;
         f32x16 s[2];
         f16x8 w[2][2];
         scores(kb, s);
         logits(vb, d0, s, true);
         float top = top_of(s);
-        raise(top);
+        raise(top, wild);
         weights(vb, s, w, wild);
+        if (wild)
+#pragma unroll
+            for (int g = 0; g < 8; ++g)
+                terms.add(L, logs, s[g >> 2][4 * (g & 3)], s[g >> 2][4 * (g & 3) + 1], s[g >> 2][4 * (g & 3) + 2], s[g >> 2][4 * (g & 3) + 3],
+                          *(const f32x4*)&lds_step[vb][2][32 * half + 16 * (g >> 2) + 4 * (g & 3)]);
         gather(kb, w);
         __syncthreads();
 #pragma unroll
@@ -521,6 +529,7 @@ __global__ void __launch_bounds__(64 * NW, 2) k_attend_tile(AttendArgs a) {
     }
 
     const int heads = a.st.heads * a.group;
+    if (wild) L = terms.end(L, M);
     const float l = L + __shfl_xor(L, 32, 64);
     const int row = tile.row0 + wave * 32 + n;
     if (row >= rows) return;
