@@ -27,9 +27,12 @@ class PageAllocator:
     def __init__(self, pages: int):
         self.free = list(range(pages))
 
-    def take(self, n: int) -> list:
+    def check(self, n: int):
         if n > len(self.free):
             raise RuntimeError(f"the store has no {n} free pages left")
+
+    def take(self, n: int) -> list:
+        self.check(n)
         taken, self.free = self.free[:n], self.free[n:]
         return taken
 
@@ -72,12 +75,15 @@ class Reader:
         kv = (torch.cat(passages).to(device, dtype) @ self.cross_kv).view(-1, 2 * heads, dim)
         self.states.write(kv[:, :heads], kv[:, heads:], slots.to(device))
 
-    def start(self, conversations: int, tokens: int):
+    def start(self, conversations: int, tokens: int, longest=None):
         """Pages for conversations of up to `tokens` tokens each (with a budget: at a time).  Those of the conversations before are given back (what reads them has been enqueued on the
-        same stream): step() goes on with the new ones."""
+        same stream): step() goes on with the new ones.  Conversations that are to be cut need as many pages once more while they move: what the store has no room for is refused here.
+        longest: tokens that they will have in all (None: any number); where they stay within `tokens`, none is cut."""
         self.pages.give_back(self.taken)
         self.taken, self.past, self.most = [], 0, 0
         width = -(-tokens // self.page_size)
+        if self.budget is not None and self.budget < tokens and (longest is None or longest > tokens):
+            self.pages.check(2 * conversations * width)
         self.own = self._own_pages(conversations, width)
         if self.budget is not None:
             self.sums = torch.zeros((conversations, self.heads, width * self.page_size), device=self.device)
@@ -127,7 +133,7 @@ def answer(index: binding.Index, reader: Reader, question, embed, steps: int, k:
     index.use_torch_stream()
     ids, dists = index.search(embed(question.mean(1)).float().contiguous(), k, w, m, asynchronous=True)
     tokens = question.shape[1] + steps
-    reader.start(question.shape[0], tokens if reader.budget is None else min(tokens, max(question.shape[1], reader.budget) + reader.page_size))
+    reader.start(question.shape[0], tokens if reader.budget is None else min(tokens, max(question.shape[1], reader.budget) + reader.page_size), longest=tokens)
     out = [reader.step(question, ids, dists)]
     for _ in range(steps):
         out.append(reader.step(out[-1][:, -1:], ids, dists))
