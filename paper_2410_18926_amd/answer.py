@@ -107,10 +107,12 @@ class Reader:
         """Hidden states [conversations, new tokens, width] of the newest tokens -> the same after the layer.  ids, dists [conversations, found] as the
         search returned them."""
         n, new, _ = hidden.shape
-        if self.budget is not None and self.past > self.budget and self.past + new > self.most:
+        cut = self.budget is not None and self.past > self.budget and self.past + new > self.most
+        past = self.budget if cut else self.past
+        if past + new > self.most:
+            raise ValueError(f"conversations of {past + new} tokens: started for {self.most}")
+        if cut:
             self._cut()
-        if self.past + new > self.most:
-            raise ValueError(f"conversations of {self.past + new} tokens: started for {self.most}")
         x = hidden.reshape(n * new, self.width)
         at = torch.arange(self.past, self.past + new, device=self.device)
         slots = (self.own[:, at // self.page_size].long() * self.page_size + at % self.page_size).reshape(-1)

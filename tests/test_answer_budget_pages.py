@@ -62,3 +62,14 @@ def test_a_budget_that_holds_all_tokens_needs_no_second_set():
     r.start(1, 64)
     grow(r, 64)
     assert r.states.cut == 0
+
+
+def test_tokens_that_do_not_fit_even_after_a_cut_leave_the_conversation_as_it_was():
+    r = budget_reader(12, 64)
+    r.width = 8
+    r.start(1, 96)
+    grow(r, 90)
+    own = r.own.clone()
+    with pytest.raises(ValueError, match="started for 96"):
+        r.step(torch.zeros(1, 33, 8), None, None)
+    assert r.states.cut == 0 and r.past == 90 and torch.equal(r.own, own) and len(r.pages.free) == 6
