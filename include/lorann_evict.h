@@ -22,8 +22,8 @@ extern "C" {
  *   qs        as for lorann_attend_chunk; `out` and its distances are not used
  *   before    [sequences][heads][width * page_size] float, or NULL for zeros; may be `sums` itself
  *   sums      the same shape: every element is written, those of keys that no query sees with what was there before
- * A query without a key adds nothing.  A query with a logit that is NaN or +infinity (a key's states hold a NaN, the query a NaN or an infinity) makes the sums of all keys NaN that it
- * sees.  Products are exact, their sums and everything after them float.  Two runs give the same bits.
+ * A query without a key adds nothing, nor does one whose logits are all -infinity (the query holds an infinity, all keys that it sees have the other sign there).  A query with a logit that
+ * is NaN or +infinity (a key's states hold a NaN, the query a NaN or another infinity) makes the sums of all keys NaN that it sees.  Products are exact, their sums and everything after them float.  Two runs give the same bits.
  *   workspace      lorann_attend_weights_workspace() bytes of device memory, 16-byte aligned; calls that may overlap need one each
  */
 int lorann_attend_weights(const lorann_states *st, const lorann_questions *qs, const int32_t *tables, int32_t width, const int32_t *lengths,
