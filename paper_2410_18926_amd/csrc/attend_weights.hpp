@@ -518,7 +518,7 @@ __global__ void __launch_bounds__(256, 3) k_weights_rows(WeightArgs wa) {
 // Joins the splits of each row, eight threads a row (rows of no sequence hold anything).
 __global__ void __launch_bounds__(256) k_weights_join(WeightArgs wa) {
     const AttendArgs& a = wa.a;
-    const int64_t all = a.st.heads * wa.padded, i = (int64_t)blockIdx.x * 32 + (threadIdx.x >> 3);
+    const int64_t all = a.st.heads * wa.padded, i = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 32 + (threadIdx.x >> 3);
     const int part = threadIdx.x & 7;
     float m = -INFINITY, l = 0.0f;
     if (i < all)

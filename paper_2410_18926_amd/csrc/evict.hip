@@ -82,7 +82,10 @@ void launch_weights(const WeightPlan& p, const WeightArgs& w, int32_t type, hipS
     }
     if (type == LORANN_F16) hipLaunchKernelGGL((k_weights_rows<_Float16, D, BITS>), grid, dim3(256), 0, stream, w);
     else hipLaunchKernelGGL((k_weights_rows<__bf16, D, BITS>), grid, dim3(256), 0, stream, w);
-    if (a.splits > 1) hipLaunchKernelGGL(k_weights_join, dim3((unsigned)ceil_div(a.st.heads * w.padded, 32)), dim3(256), 0, stream, w);
+    if (a.splits > 1) {
+        const int64_t blocks = ceil_div(a.st.heads * w.padded, 32), x = std::min<int64_t>(blocks, 4096);          // (one dimension would pass 2^32 threads from 2^29 rows and heads on)
+        hipLaunchKernelGGL(k_weights_join, dim3((unsigned)x, (unsigned)ceil_div(blocks, x)), dim3(256), 0, stream, w);
+    }
     const bool share = share_keys(ceil_div(w.keys, 256) * a.st.heads * a.sequences, a.tokens * a.group / a.sequences);
     const dim3 chunks((unsigned)ceil_div(w.keys, share ? 64 : 256), (unsigned)a.st.heads, (unsigned)a.sequences);
     if (share) hipLaunchKernelGGL((k_weights_keys<D, BITS, true>), chunks, dim3(256), 0, stream, w);
