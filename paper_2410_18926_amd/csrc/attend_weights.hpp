@@ -315,7 +315,7 @@ __global__ void __launch_bounds__(256) k_weights_add(WeightArgs wa) {
 // Many rows: m and l.  A block has 128 rows of one head, a wavefront 32; keys pass by, 64 at a time, converted once for the block into LDS.  The maximum is taken over x = product * step,
 // which the row's factor (a power of two: m = x back is exact, and no term is above 1 however large logits are) is applied to together with it: y - m = fma(x, back, -m), so a score costs five instructions and its exponential.
 // A block that has met a key above kMostStep begins again, x = product * (step * back), y - m = fma(x, 1, -m).
-// 4 x 32 tokens after 16000 keys, 32 heads on 8 of 128, 4 bits: 41 us, the matrix instructions alone 7; some 40 % of the cycles are vector instructions, a third of those convert codes and find addresses.
+// 4 x 32 tokens after 16000 keys, 32 heads on 8 of 128, 4 bits: 42 us, the matrix instructions alone 7; some 40 % of the cycles are vector instructions, a third of those convert codes and find addresses.
 // (Four wavefronts a SIMD instead of three: 17 registers spill, 92 us for the call instead of 86.)
 template <typename T, int D, int BITS>
 __global__ void __launch_bounds__(256, 3) k_weights_rows(WeightArgs wa) {
@@ -561,7 +561,7 @@ __device__ __forceinline__ void add_over_lanes(float (&v)[32]) {
 }
 
 // Many rows: the sums.  A wavefront holds 64 keys as operands, rows pass by, 32 at a time.  SHARE: the block's four wavefronts have the same keys and take the rows in turn; else each
-// has keys of its own.  Blocks: (chunk of keys, head, sequence).  The case of k_weights_rows: 39.5 us, bound in the same way.
+// has keys of its own.  Blocks: (chunk of keys, head, sequence).  The case of k_weights_rows: 40 us, bound in the same way.
 template <int D, int BITS, bool SHARE>
 __global__ void __launch_bounds__(256, 2) k_weights_keys(WeightArgs wa) {
     const AttendArgs& a = wa.a;

@@ -22,8 +22,11 @@ struct WeightPlan {
 //   16 sequences, 4000 keys, 16 heads of 64, 8 bits                           59 / 88   114 / 99   162 / 98
 //   one sequence, 16000 keys, 8 heads of 128, 8 bits    20 / 42    26 / 44    39 / 43               64 / 44
 //   two sequences, 9000 keys, 4 heads of 64, 4 bits                           32 / 28    43 / 29    54 / 29
+// The memory follows from the tables' width, whatever the lengths are: very wide tables of many sequences lose the better way.  64 single tokens of 32 heads after 4096 keys, 8 heads of 128,
+// 8 / 4 bits, in tables of 4096 keys 78 / 54, of 65536 235 / 175, of 131072 (1 GiB of scores) 288 / 229 (more sums are read and written), of 131136, formed twice, 1129 / 1109.
 // Blocks wanted: of k_weights_scores many more than the GPU holds, since sequences differ in length and a split costs two numbers a row (64 tokens after up to 8192 keys, 8 heads, us with
-// 512 / 1024 / 2048 / 4096 / 8192: 102 / 101 / 104 / 89 / 96); of k_weights_rows 4 a CU (4 x 32 tokens after 16000 keys, 512 / 768 / 1024 / 1536 / 2048: 53 / 52 / 40 / 41 / 49).
+// 512 / 1024 / 2048 / 4096 / 8192: 102 / 101 / 104 / 89 / 96); of k_weights_rows 4 a CU (4 x 32 tokens after 16000 keys, 512 / 768 / 1024 / 1536 / 2048: 53 / 52 / 40 / 41 / 49; with 1536 calls of
+// 16 x 64 tokens after 4000 and of 300 after 60000 were 5 to 7 % faster, of 12 x 200 after 6000 2 % slower).
 constexpr int64_t kScoreBlocks = 4096, kRowBlocks = 1024, kFewWeightRows = 32, kMostScores = (int64_t)1 << 30;
 
 // Keys of a block of k_weights_keys: 256, each wavefront with 64 of its own and all rows, or 64 that its wavefronts share with a quarter of the rows each (four times the blocks).  512 blocks are on

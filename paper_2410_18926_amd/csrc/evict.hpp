@@ -340,7 +340,7 @@ __global__ void __launch_bounds__(kChooseThreads) k_evict_chunks(ChunkArgs c, bo
 
 // Moves the kept tokens: a block has 64 consecutive ones of a sequence and head, at the destination's keys 64 blockIdx.x on.  Their keys are rows of their own.  Their values lie byte by
 // byte in rows of components: the 16-byte groups that hold any of the 64 are read into LDS (in order, so that lanes read neighbouring groups) and the bytes picked there - each
-// byte read from memory by a lane of its own costs a cycle of the address unit, whatever the cache holds (32 sequences of up to 6000 keys cut to 2048, 4 bits, 8 heads of 128: 64 us so, 40 to 53 as built).
+// byte read from memory by a lane of its own costs a cycle of the address unit, whatever the cache holds (32 sequences of up to 6000 keys cut to 2048, 4 bits, 8 heads of 128: 64 us so, 42 to 53 as built).
 // Bound by memory: where few keys are kept, most lines of the source's values are read all the same.
 constexpr int kMoveRoom = 1024;        // 16-byte groups in LDS
 template <int BITS>
