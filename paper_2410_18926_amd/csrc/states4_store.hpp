@@ -75,7 +75,7 @@ __device__ __forceinline__ uint32_t codes4_of(const float (&x)[8], float r, floa
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const float y = x[j] * (6.0f * keep), q0 = y * inv;
-            q[j] = fmaf(fmaf(-q0, unit, y), inv, q0);
+            q[j] = fmaf(-fmaf(q0, unit, -y), inv, q0);          // (the remainder's signs so that -0 stays -0: -0 unit + 0 = +0, and -0 inv - 0 = -0)
         }
         c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, q[0], q[1], 1.0f, 0);
         c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, q[2], q[3], 1.0f, 1);
