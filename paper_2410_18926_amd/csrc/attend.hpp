@@ -156,7 +156,9 @@ __device__ __forceinline__ void row_power(float top, float& to_half, float& back
 //   - A NaN step of the values acts through add alone: rows that do not see the key multiply `inverse` by 0.
 // While all steps of the values are within 2^-45 .. 2^10 ("tame") or 0, the operand 2^kLift w of a key whose share of the sum is 2^-40 of the largest is still a normal
 // float, whatever the two keys' steps are, and operand * inverse is the sum's term.  From the first tile on that has a step beyond that ("wild"), the terms are exponentials of their own,
-// relative to the largest of them so far (WildSum): between values of 2^-100 and 2^127 an operand's term may be 2^-125 or 2^107 times it, and terms next to 2^-126 would be lost.
+// relative to the largest of them so far (WildSum): between values of 2^-100 and 2^127 an operand's term may be 2^-125 or 2^107 times it, and terms next to 2^-126 would be lost.  (The same cases
+// with values 2^14 times as large: 64 tokens after up to 8192 keys 150 instead of 140 us, over 4 bits 107 instead of 89; 4096 tokens after 28672 3.2 ms instead of 2.2.  In k_attend_rows the wild
+// sums stay beside the others in one loop, marked unlikely: with a loop of their own, 48 tokens over passages took 54 instead of 51 us, over 4 bits 53 instead of 48.)
 constexpr float kTameLow = 0x1p-45f, kTameHigh = 0x1p10f, kNoStep = 0x1p-84f;
 // The reference M of the weights is raised only when a score passes it by more than kSlack, so the answer's registers are rarely rescaled.  Weights stay below
 // 2^kSlack, and the operands 2^kLift w below 2^15, the last power of two but one that binary16 holds.  (Without the lift, weights below 2^-14 would lose bits and those
@@ -178,7 +180,7 @@ __device__ __forceinline__ KeySteps key_steps(float ks, float vs, float c, float
     k.product = have ? ks * c : 0.0f;
     k.add = have ? lg + bias : -INFINITY;
     k.inverse = (have && vs == vs ? __builtin_amdgcn_rcpf(vs) : 1.0f) * kUnlift;       // (1 ulp)
-    k.log_inverse = -lg - kLift;                                // takes the place of `inverse` in a tile with a wild key: that may be no normal float
+    k.log_inverse = have && vs == vs ? -lg - kLift : 0.0f;      // takes the place of `inverse` from a tile with a wild key on: that may be no normal float
     k.wild = have && wild;
     return k;
 }
@@ -196,20 +198,22 @@ struct WildSum {
         ref = l == 0.0f ? -INFINITY : m + (float)__builtin_amdgcn_frexp_expf(l);
         l = __builtin_amdgcn_frexp_mantf(l);
     }
-    // Four keys' terms; logs: log_inverse stands in the place of `inverse`.
-    __device__ __forceinline__ void add(float& l, bool logs, float y0, float y1, float y2, float y3, const f32x4 inverse) {
-        float t[4] = {y0, y1, y2, y3}, top = ref;
+    // The lane's keys of a tile.  each(f): f(y, log_inverse) for every four of them, both as f32x4; twice, so that their sums stay out of the registers between.
+    template <typename F>
+    __device__ __forceinline__ void add(float& l, F&& each) {
+        float top = ref;
+        each([&](const f32x4 y, const f32x4 log_inverse) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            t[j] = t[j] == -INFINITY ? t[j] : t[j] + (logs ? inverse[j] : __log2f(inverse[j]));
-            top = fmaxf(top, t[j]);
-        }
+            for (int j = 0; j < 4; ++j) top = fmaxf(top, y[j] + log_inverse[j]);
+        });
         const float use = top == -INFINITY ? 0.0f : top;
         l *= __builtin_amdgcn_exp2f(ref - use);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) l += __builtin_amdgcn_exp2f(t[j] - use);
         ref = top;
-        __builtin_amdgcn_sched_barrier(0);          // (four by four: together, a tile's terms would fill the registers)
+        asm volatile("" ::: "memory");
+        each([&](const f32x4 y, const f32x4 log_inverse) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) l += __builtin_amdgcn_exp2f(y[j] + log_inverse[j] - use);
+        });
     }
     __device__ __forceinline__ float end(float l, float m) const { return l == 0.0f ? 0.0f : times_exp2(l, ref - m); }
 };
@@ -517,14 +521,15 @@ __global__ void __launch_bounds__(64 * kAttendWaves, 2) k_attend_rows(AttendArgs
     WildSum terms[RT];
 
     while (cur.have) {
-        bool logs;                                              // some step of this tile is not tame
+        bool now_wild;                                          // ... with this tile's
         {
             wave_lds_order();                                   // the previous tile's steps have been read
             const KeySteps ks = key_steps(rks, rvs, a.c, cur.bias, rhave);
             lds_step[wave][0][lane] = ks.product;
             lds_step[wave][1][lane] = ks.add;
-            logs = __ballot(ks.wild);
-            lds_step[wave][2][lane] = logs ? ks.log_inverse : ks.inverse;
+            now_wild = wild | (__ballot(ks.wild) != 0);
+            lds_step[wave][2][lane] = ks.inverse;
+            if (__builtin_expect(now_wild, 0)) lds_step[wave][2][lane] = ks.log_inverse;
             if constexpr (FOUR) {
                 lds_kf[wave][lane] = rkf;
 #pragma unroll
@@ -574,7 +579,7 @@ __global__ void __launch_bounds__(64 * kAttendWaves, 2) k_attend_rows(AttendArgs
         __builtin_amdgcn_sched_barrier(0);
         f16x8 w[RT][2];
         const bool was_wild = wild;
-        wild = wild || logs;
+        wild = now_wild;
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
             float top = -INFINITY;
@@ -619,12 +624,14 @@ __global__ void __launch_bounds__(64 * kAttendWaves, 2) k_attend_rows(AttendArgs
                     }
                 }
             };
-            if (wild) {
+            if (__builtin_expect(wild, 0)) {
                 if (!was_wild) terms[t].begin(L[t], M[t]);
+                terms[t].add(L[t], [&](auto&& f) {
 #pragma unroll
-                for (int b = 0; b < 4; ++b) terms[t].add(L[t], logs, s[t][b][0], s[t][b][1], s[t][b][2], s[t][b][3], *(const f32x4*)&lds_step[wave][2][16 * quarter + 4 * b]);
+                    for (int b = 0; b < 4; ++b) f(s[t][b], *(const f32x4*)&lds_step[wave][2][16 * quarter + 4 * b]);
+                });
             }
-            if (FOUR && wild) weigh(std::false_type{});             // (8 bits: one copy, with a select)
+            if (FOUR && __builtin_expect(wild, 0)) weigh(std::false_type{});             // (8 bits: one copy, with a select)
             else weigh(std::true_type{});
             L[t] += l;
             asm volatile("" : "+v"(L[t]));                             // (the sum is formed here: kept for later, its terms would fill the registers)

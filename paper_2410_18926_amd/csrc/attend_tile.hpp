@@ -233,12 +233,12 @@ __global__ void __launch_bounds__(64 * NW, 2) k_attend_tile(AttendArgs a) {
     };
     // where the weight of key j of eight stands
     auto place_of = [](int j) { return FOUR ? token_place(j) : j; };
-    auto stage_steps = [&](int vb, const KeyTile& kt) {         // (by the wavefront that requested them: tiles go round)
+    auto stage_steps = [&](int vb, const KeyTile& kt, bool wild_now) {          // (by the wavefront that requested them: tiles go round)
         if (wave != vb) return;
         const KeySteps ks = key_steps(rks, rvs, c, kt.bias, rhave);
         lds_step[vb][0][lane] = ks.product;
         lds_step[vb][1][lane] = ks.add;
-        const int w = __ballot(ks.wild) != 0;
+        const int w = wild_now || __ballot(ks.wild) != 0;
         lds_step[vb][2][lane] = w ? ks.log_inverse : ks.inverse;
         if constexpr (FOUR) {
 #pragma unroll
@@ -357,7 +357,7 @@ __global__ void __launch_bounds__(64 * NW, 2) k_attend_tile(AttendArgs a) {
     fetch_values();
 #pragma unroll
     for (int i = 0; i < PER; ++i) stage_keys(0, i);
-    stage_steps(0, d0);
+    stage_steps(0, d0, false);
     if constexpr (FOUR) __syncthreads();                        // (the values' factors)
 #pragma unroll
     for (int i = 0; i < PER; ++i) stage_values(0, i, 0);
@@ -368,7 +368,7 @@ __global__ void __launch_bounds__(64 * NW, 2) k_attend_tile(AttendArgs a) {
     fetch_values();
 #pragma unroll
     for (int i = 0; i < PER; ++i) stage_keys(1, i);
-    stage_steps(1, d1);
+    stage_steps(1, d1, false);
     it.next(a, tile.s, behind);
     d2 = it.t;
     find_pages(d2);
@@ -488,7 +488,7 @@ __global__ void __launch_bounds__(64 * NW, 2) k_attend_tile(AttendArgs a) {
                     __builtin_amdgcn_sched_barrier(0);
                 });
             }
-            stage_steps(v2, d2);
+            stage_steps(v2, d2, false);
             if (hide(d1, s)) {
                 top = top_of(s);
             }
@@ -514,16 +514,25 @@ __global__ void __launch_bounds__(64 * NW, 2) k_attend_tile(AttendArgs a) {
         float top = top_of(s);
         raise(top, wild);
         weights(vb, s, w, wild);
-        if (wild)
+        if (wild) {
+            if (!logs) {                                        // (staged before the first wild tile was met)
+                __syncthreads();
+                if (tid < kTileKeys) lds_step[vb][2][tid] = __log2f(lds_step[vb][2][tid]);
+                __syncthreads();
+            }
+            terms.add(L, [&](auto&& f) {
 #pragma unroll
-            for (int g = 0; g < 8; ++g)
-                terms.add(L, logs, s[g >> 2][4 * (g & 3)], s[g >> 2][4 * (g & 3) + 1], s[g >> 2][4 * (g & 3) + 2], s[g >> 2][4 * (g & 3) + 3],
-                          *(const f32x4*)&lds_step[vb][2][32 * half + 16 * (g >> 2) + 4 * (g & 3)]);
+                for (int g = 0; g < 8; ++g) {
+                    const f32x16& y = s[g >> 2];
+                    f(f32x4{y[4 * (g & 3)], y[4 * (g & 3) + 1], y[4 * (g & 3) + 2], y[4 * (g & 3) + 3]}, *(const f32x4*)&lds_step[vb][2][32 * half + 16 * (g >> 2) + 4 * (g & 3)]);
+                }
+            });
+        }
         gather(kb, w);
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < PER; ++i) { stage_keys(kb, i); stage_values(kb ^ 1, i, v1); }
-        stage_steps(v2, d2);
+        stage_steps(v2, d2, wild);
         advance();
         __syncthreads();
     }
